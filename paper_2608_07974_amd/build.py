@@ -18,7 +18,8 @@ BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["gemm_kk.hip", "gemm_kn.hip", "gemm_mn.hip", "gemm_mk.hip", "gemm_f32.hip",
            "gemm_skinny.hip", "gemm.hip",
            "attention.hip", "attention_mfma.hip", "rowops.hip",
-           "objective.hip", "optim.hip", "zl.cpp", "runtime.cpp", "noalloc.hip"]
+           "objective.hip", "optim.hip", "layer.hip", "block_norm.hip", "wgrad_packed.hip",
+           "layer.cpp", "zl.cpp", "runtime.cpp", "noalloc.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,341 @@
+"""Layer operators on torch device tensors (include/zl_layer.h).
+
+Activations saved in 8 bits (pack, unpack) and their use in the backward
+(mlp_act, mlp_act_bwd, wgrad), the norms around a block with gate and residual
+scale (block_norm, block_norm_bwd), rotary positions with several axes
+(rotary).  torch provides memory and streams; the kernels are libzl's.
+
+Tensors are 2-D [T, columns], rows contiguous (any row stride that is a
+multiple of 8), bf16 or fp32, all on one GPU; work goes to that GPU's current
+stream.  Shapes, types and placement are checked here (the kernels take them
+on trust), the rest by the library, which raises zl.ZlError.  Output tensors
+may be given (and are returned); else they are made.
+"""
+from collections import namedtuple
+
+import torch
+
+from . import zl
+
+_DT = {torch.float32: zl.ZL_F32, torch.bfloat16: zl.ZL_BF16}
+_KIND = {"swiglu": zl.ZL_MLP_SWIGLU, "gelu": zl.ZL_MLP_GELU}
+_NONE = zl.zl_packed(None, None, 0, 0)
+
+
+def _up(n, m):
+    return (n + m - 1) // m * m
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _check_device(dev, *named):
+    if dev.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, not {dev}")
+    for name, t in named:
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} must be on {dev}, not {t.device}")
+
+
+def _rows(name, t, T, n, dtypes):
+    """Row stride of a [T, n] matrix with contiguous rows."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != n:
+        raise ValueError(f"{name} must be [{T}, {n}], not {list(t.shape)}")
+    if n > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    ld = t.stride(0) if T > 1 else _up(n, 8)
+    if T > 1 and ld < n:
+        raise ValueError(f"{name} must not overlap itself")
+    return ld
+
+
+def _vec(name, t, n):
+    if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous fp32 vector of {n}")
+    return _ptr(t)
+
+
+def _call(fn, dev, *args):
+    """fn(*args, stream) on dev's current stream, with dev current."""
+    if torch.cuda.current_device() == dev.index:
+        fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+
+
+class Packed:
+    """A matrix [T, n] in 8 bits: `codes` uint8 [T, >= n rounded up to 16] and
+    `scales` uint8 [T, >= ceil(n / 32)], both with contiguous rows."""
+
+    __slots__ = ("codes", "scales", "n", "struct")
+
+    def __init__(self, codes, scales, n):
+        T = codes.shape[0]
+        for name, t, cols in (("codes", codes, _up(n, 16)), ("scales", scales, (n + 31) // 32)):
+            if t.dtype != torch.uint8 or t.dim() != 2:
+                raise TypeError(f"{name} must be a uint8 matrix")
+            if t.shape[0] != T or t.shape[1] < cols:
+                raise ValueError(f"{name} must be [{T}, >= {cols}], not {list(t.shape)}")
+            if t.stride(1) != 1 and t.shape[1] > 1:
+                raise ValueError(f"{name} must have contiguous rows")
+        if codes.device != scales.device:
+            raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
+        self.codes, self.scales, self.n = codes, scales, n
+        lc = codes.stride(0) if T > 1 else _up(n, 16)
+        ls = scales.stride(0) if T > 1 else (n + 31) // 32
+        self.struct = zl.zl_packed(codes.data_ptr(), scales.data_ptr(), lc, ls)
+
+    @classmethod
+    def empty(cls, T, n, device="cuda"):
+        return cls(torch.empty(T, _up(n, 16), dtype=torch.uint8, device=device),
+                   torch.empty(T, (n + 31) // 32, dtype=torch.uint8, device=device), n)
+
+    @property
+    def shape(self):
+        return (self.codes.shape[0], self.n)
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def nbytes(self):
+        return self.codes.numel() + self.scales.numel()
+
+
+def _packed(name, p, T, n):
+    if tuple(p.shape) != (T, n):
+        raise ValueError(f"{name} must be [{T}, {n}], not {list(p.shape)}")
+    return p.struct
+
+
+def pack(x, out=None):
+    """x in 8 bits."""
+    T, n = x.shape
+    ldx = _rows("x", x, T, n, _DT)
+    out = Packed.empty(T, n, x.device) if out is None else out
+    s = _packed("out", out, T, n)
+    _check_device(x.device, ("out", out))
+    _call(zl.zl_pack, x.device, T, n, x.data_ptr(), ldx, _DT[x.dtype], s)
+    return out
+
+
+def unpack(p, dtype=torch.bfloat16, out=None):
+    """The values of a Packed matrix."""
+    T, n = p.shape
+    out = torch.empty(T, n, dtype=dtype, device=p.device) if out is None else out
+    ld = _rows("out", out, T, n, _DT)
+    _check_device(p.device, ("out", out))
+    _call(zl.zl_unpack, p.device, T, n, p.struct, out.data_ptr(), ld, _DT[out.dtype])
+    return out
+
+
+def mlp_act(h, kind="swiglu", dtype=None, act=None, packed=None):
+    """silu(gate) * up of h = gate | up [T, 2 ff], or gelu(h), h [T, ff].
+    packed: a Packed of h's shape that receives h."""
+    T, nh = h.shape
+    k = _KIND[kind]
+    if k == zl.ZL_MLP_SWIGLU and nh % 2:
+        raise ValueError(f"h must be gate | up, not of {nh} columns")
+    ff = nh // 2 if k == zl.ZL_MLP_SWIGLU else nh
+    ldh = _rows("h", h, T, nh, _DT)
+    act = torch.empty(T, ff, dtype=dtype or h.dtype, device=h.device) if act is None else act
+    lda = _rows("act", act, T, ff, _DT)
+    ps = _NONE if packed is None else _packed("packed", packed, T, nh)
+    _check_device(h.device, ("act", act), ("packed", packed))
+    a = zl.zl_mlp_args(T, ff, k, _DT[h.dtype], _DT[act.dtype], h.data_ptr(), ldh, ps, act.data_ptr(), lda)
+    _call(zl.zl_mlp_act, h.device, a)
+    return act
+
+
+def mlp_act_bwd(h, dact, kind="swiglu", dtype=None, dh=None, act=None):
+    """Gradient with respect to h (a tensor of dact's type, or its Packed
+    copy).  act: a tensor that receives the activation, formed again."""
+    T, nh = h.shape
+    k = _KIND[kind]
+    if k == zl.ZL_MLP_SWIGLU and nh % 2:
+        raise ValueError(f"h must be gate | up, not of {nh} columns")
+    ff = nh // 2 if k == zl.ZL_MLP_SWIGLU else nh
+    dev = dact.device
+    ldda = _rows("dact", dact, T, ff, _DT)
+    dh = torch.empty(T, nh, dtype=dtype or dact.dtype, device=dev) if dh is None else dh
+    lddh = _rows("dh", dh, T, nh, _DT)
+    lda = 0 if act is None else _rows("act", act, T, ff, (dh.dtype,))
+    if isinstance(h, Packed):
+        hp, ldh, ps = None, 0, h.struct
+    else:
+        hp, ldh, ps = h.data_ptr(), _rows("h", h, T, nh, (dact.dtype,)), _NONE
+    _check_device(dev, ("h", h), ("dh", dh), ("act", act))
+    a = zl.zl_mlp_args(T, ff, k, _DT[dact.dtype], _DT[dh.dtype], hp, ldh, ps, _ptr(act), lda, dact.data_ptr(), ldda,
+                       dh.data_ptr(), lddh)
+    _call(zl.zl_mlp_act_backward, dev, a)
+    return dh
+
+
+NormGrads = namedtuple("NormGrads", "w_post b_post w_pre b_pre gate", defaults=(None,) * 5)
+NormGrads.__doc__ = "Gradients of block_norm's parameters (fp32; None = not wanted)."
+
+
+def _norm_common(d, T, dev, post, pre, gate, gate_rows, stats):
+    wb = [_vec(n, t, d) for n, t in zip(("w_post", "b_post", "w_pre", "b_pre"), (*(post or (None, None)),
+                                                                                *(pre or (None, None))))]
+    if gate is not None:
+        if gate_rows < 1:
+            raise ValueError("a gate needs gate_rows >= 1")
+        G = -(-T // gate_rows)
+        if gate.dtype != torch.float32 or tuple(gate.shape) != (G, d) or not gate.is_contiguous():
+            raise ValueError(f"gate must be a contiguous fp32 [{G}, {d}] tensor")
+    if stats.dtype != torch.float32 or tuple(stats.shape) != (T, 4) or not stats.is_contiguous():
+        raise ValueError(f"stats must be a contiguous fp32 [{T}, 4] tensor")
+    _check_device(dev, ("w_post", post and post[0]), ("b_post", post and post[1]), ("w_pre", pre and pre[0]),
+                  ("b_pre", pre and pre[1]), ("gate", gate), ("stats", stats))
+    return wb
+
+
+def block_norm(x, y, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5, layernorm=False, dtype=None,
+               xo=None, n=None, stats=None, y_packed=None, n_packed=None):
+    """xo = x + scale * gate * Norm(y), n = Norm(xo); returns (xo, n, stats).
+
+    x [T, d] fp32; post, pre: (weight, bias or None) of the norm of y and of
+    the norm of xo, or None (without post: y is None, xo is x itself; without
+    pre: n is None).  gate [ceil(T / gate_rows), d].  stats [T, 4] is what the
+    backward needs besides.  y_packed, n_packed: Packed [T, d] that receive y
+    and n.  n has `dtype` (default: y's, or bf16).  xo may be x."""
+    T, d = x.shape
+    dev = x.device
+    f32 = (torch.float32,)
+    ldx = _rows("x", x, T, d, f32)
+    stats = torch.empty(T, 4, device=dev) if stats is None else stats
+    wb = _norm_common(d, T, dev, post, pre, gate, gate_rows, stats)
+    if (y is None) != (post is None):
+        raise ValueError("y and post go together")
+    ldy = ldn = 0
+    ty, tn = zl.ZL_F32, zl.ZL_BF16
+    if y is not None:
+        ldy, ty = _rows("y", y, T, d, _DT), _DT[y.dtype]
+        xo = torch.empty_strided((T, d), (ldx, 1), dtype=torch.float32, device=dev) if xo is None else xo
+        if _rows("xo", xo, T, d, f32) != ldx:
+            raise ValueError("xo must have x's row stride")
+    elif xo is not None:
+        raise ValueError("xo is x where there is no y")
+    if pre is not None:
+        n = torch.empty(T, d, dtype=dtype or (torch.bfloat16 if y is None else y.dtype), device=dev) if n is None else n
+        ldn, tn = _rows("n", n, T, d, _DT), _DT[n.dtype]
+    elif n is not None:
+        raise ValueError("n needs pre")
+    _check_device(dev, ("y", y), ("xo", xo), ("n", n), ("y_packed", y_packed), ("n_packed", n_packed))
+    a = zl.zl_norm_args(T, d, int(layernorm), ty, tn, eps, scale, *wb, _ptr(gate), gate_rows, stats.data_ptr(),
+                        x.data_ptr(), _ptr(xo), ldx, _ptr(y), ldy, _ptr(n), ldn,
+                        _NONE if y_packed is None else _packed("y_packed", y_packed, T, d),
+                        _NONE if n_packed is None else _packed("n_packed", n_packed, T, d))
+    _call(zl.zl_block_norm, dev, a)
+    return (x if y is None else xo), n, stats
+
+
+def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5,
+                   layernorm=False, dtype=None, dx=None, dy=None, grads=None, grad_scale=1.0, accumulate=False,
+                   workspace=None):
+    """Backward of block_norm; returns (dx, dy).
+
+    dxo [T, d] fp32: gradient of xo besides that through n (None = 0); dn
+    [T, d]; y: block_norm's, or its Packed copy; xo, stats: block_norm's
+    outputs.  dn and y have one type.  dy has `dtype` (default: dn's or y's).
+    grads: NormGrads of fp32 tensors that receive (accumulate: are added)
+    grad_scale times the parameters' gradients.  dx may be dxo.  workspace:
+    fp32, zl.zl_block_norm_workspace elements, made here if None."""
+    src = dn if dn is not None else xo if xo is not None else dxo
+    if src is None:
+        raise ValueError("dxo, dn or xo must be there")
+    T, d = src.shape
+    dev = src.device
+    f32 = (torch.float32,)
+    wb = _norm_common(d, T, dev, post, pre, gate, gate_rows, stats)
+    if (y is None) != (post is None) or (dn is None) != (pre is None) or (pre is not None and xo is None):
+        raise ValueError("y and post, dn, xo and pre go together")
+    strided = [t for t in (dxo, dx, xo if pre is not None else None) if t is not None]
+    lds = {_rows("dxo, dx and xo", t, T, d, f32) for t in strided}
+    if len(lds) > 1:
+        raise ValueError("dxo, dx and xo must have one row stride")
+    ldx = lds.pop() if lds else d
+    if dx is None:
+        dx = torch.empty_strided((T, d), (ldx, 1), dtype=torch.float32, device=dev)
+    tin, ldn, ldy = None, 0, 0
+    if dn is not None:
+        ldn, tin = _rows("dn", dn, T, d, _DT), dn.dtype
+    yp, ys = None, _NONE
+    if isinstance(y, Packed):
+        ys = _packed("y", y, T, d)
+    elif y is not None:
+        ldy, yp = _rows("y", y, T, d, _DT if tin is None else (tin,)), y.data_ptr()
+        tin = y.dtype
+    tin = torch.float32 if tin is None else tin
+    if post is not None:
+        if dy is None:
+            dy = torch.empty_strided((T, d), (ldy or d, 1), dtype=dtype or tin, device=dev)
+        l = _rows("dy", dy, T, d, _DT)
+        if yp is not None and l != ldy:
+            raise ValueError("dy must have y's row stride")
+        ldy = l
+    elif dy is not None:
+        raise ValueError("dy needs post")
+    g = NormGrads() if grads is None else grads
+    gp = [_vec("grads." + k, t, d) for k, t in zip(g._fields[:4], g[:4])]
+    if g.gate is not None and (gate is None or g.gate.shape != gate.shape or g.gate.dtype != torch.float32 or
+                               not g.gate.is_contiguous()):
+        raise ValueError("grads.gate must be a contiguous fp32 tensor like gate")
+    if workspace is None:
+        workspace = torch.empty(zl.zl_block_norm_workspace(T, d, gate_rows if gate is not None else 0), device=dev)
+    elif workspace.dtype != torch.float32 or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous fp32 tensor")
+    _check_device(dev, ("dxo", dxo), ("y", y), ("xo", xo), ("dx", dx), ("dy", dy), ("workspace", workspace),
+                  *(("grads." + k, t) for k, t in zip(g._fields, g)))
+    a = zl.zl_norm_args(T, d, int(layernorm), _DT[tin], zl.ZL_F32 if dy is None else _DT[dy.dtype], eps, scale, *wb,
+                        _ptr(gate), gate_rows, stats.data_ptr(), None, _ptr(xo) if pre is not None else None, ldx, yp,
+                        ldy, None, ldn, ys, _NONE, _ptr(dxo), _ptr(dn), dx.data_ptr(), _ptr(dy), *gp, _ptr(g.gate),
+                        grad_scale, int(accumulate), _ptr(workspace), workspace.numel())
+    _call(zl.zl_block_norm_backward, dev, a)
+    return dx, dy
+
+
+def wgrad(dy, x, out=None, scale=1.0, accumulate=False, workspace=None):
+    """dw [n_out, n_in] fp32 = scale * dy^T x (added to `out` with
+    accumulate); dy [T, n_out], x a Packed [T, n_in].  workspace: fp32 scratch
+    that lets a small dw split the sum over T."""
+    T, M = dy.shape
+    N = x.n
+    lddy = _rows("dy", dy, T, M, _DT)
+    s = _packed("x", x, T, N)
+    if out is None:
+        out = (torch.zeros if accumulate else torch.empty)(M, N, device=dy.device)
+    ld = _rows("out", out, M, N, (torch.float32,))
+    if workspace is not None and (workspace.dtype != torch.float32 or not workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous fp32 tensor")
+    _check_device(dy.device, ("x", x), ("out", out), ("workspace", workspace))
+    _call(zl.zl_wgrad_packed, dy.device, T, M, N, dy.data_ptr(), lddy, _DT[dy.dtype], s, out.data_ptr(), ld, scale,
+          accumulate, _ptr(workspace), 0 if workspace is None else workspace.numel())
+    return out
+
+
+def rotary(x, pos, axis_of, n_heads, head_dim, theta, *, inverse=False, out=None):
+    """x [T, >= n_heads * head_dim] with the heads rotated by pos [axes, T]
+    (int32, contiguous); returns [T, n_heads * head_dim].  axis_of: bytes,
+    the axis of each frequency; 2 len(axis_of) columns of a head are rotated,
+    the others copied.  inverse: the gradient's way back.  out may be x."""
+    T, W = x.shape[0], n_heads * head_dim
+    if x.dim() != 2 or x.shape[1] < W:
+        raise ValueError(f"x must be [{T}, >= {W}], not {list(x.shape)}")
+    if x.dtype not in _DT or (x.stride(1) != 1 and W > 1):
+        raise TypeError("x must be fp32 or bf16 with contiguous rows")
+    if pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape[1] != T or not pos.is_contiguous():
+        raise TypeError(f"pos must be a contiguous int32 [axes, {T}] tensor")
+    out = torch.empty(T, W, dtype=x.dtype, device=x.device) if out is None else out
+    if out.dtype != x.dtype or out.dim() != 2 or out.shape[0] != T or out.shape[1] < W or out.stride(1) != 1:
+        raise ValueError(f"out must be [{T}, >= {W}] of x's type with contiguous rows")
+    _check_device(x.device, ("pos", pos), ("out", out))
+    ldx, ldo = (x.stride(0), out.stride(0)) if T > 1 else (W, W)
+    _call(zl.zl_rotary, x.device, T, n_heads, head_dim, 2 * len(axis_of), x.data_ptr(), ldx, out.data_ptr(), ldo,
+          _DT[x.dtype], pos.data_ptr(), pos.shape[0], axis_of, theta, inverse)
+    return out

@@ -1,4 +1,4 @@
-"""ctypes binding of libzl (include/zl.h, include/zl_inspect.h).
+"""ctypes binding of libzl (include/zl.h, zl_inspect.h, zl_runtime.h, zl_layer.h).
 
 Argument marshalling only: every function here forwards to the C call of the
 same name, raising ZlError on a negative status.  Pointers are plain ints
@@ -16,6 +16,7 @@ ZL_ARCH_LLAMA, ZL_ARCH_GPT2 = 0, 1
 ZL_F32, ZL_BF16 = 0, 1
 ZL_KL_REVERSE, ZL_KL_FORWARD = 0, 1
 ZL_ADAMW, ZL_SGD = 0, 1
+ZL_MLP_SWIGLU, ZL_MLP_GELU = 0, 1
 
 EXPORTED = [
     "zl_param_layout", "zl_workspace_size", "zl_chunk_create", "zl_chunk_destroy",
@@ -28,6 +29,8 @@ EXPORTED = [
     "zl_pipeline_sync", "zl_pipeline_progress", "zl_pipeline_checkpoint", "zl_pipeline_destroy",
     "zl_chunk_save", "zl_chunk_load", "zl_checkpoint_read_info",
     "zl_kernel_attention_bwd_noalloc",
+    "zl_pack", "zl_unpack", "zl_mlp_act", "zl_mlp_act_backward", "zl_block_norm",
+    "zl_block_norm_backward", "zl_block_norm_workspace", "zl_wgrad_packed", "zl_rotary",
 ]
 
 
@@ -84,6 +87,37 @@ class zl_profile_entry(ctypes.Structure):
                 ("bytes", ctypes.c_double)]
 
 
+class zl_packed(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("ld_codes", ctypes.c_int64), ("ld_scales", ctypes.c_int64)]
+
+
+class zl_mlp_args(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("ff", ctypes.c_int), ("kind", ctypes.c_int),
+                ("in_dtype", ctypes.c_int), ("out_dtype", ctypes.c_int), ("h", ctypes.c_void_p),
+                ("ldh", ctypes.c_int64), ("packed", zl_packed), ("a", ctypes.c_void_p),
+                ("lda", ctypes.c_int64), ("da", ctypes.c_void_p), ("ldda", ctypes.c_int64),
+                ("dh", ctypes.c_void_p), ("lddh", ctypes.c_int64)]
+
+
+class zl_norm_args(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("d", ctypes.c_int), ("layernorm", ctypes.c_int),
+                ("in_dtype", ctypes.c_int), ("out_dtype", ctypes.c_int), ("eps", ctypes.c_float),
+                ("scale", ctypes.c_float), ("w_post", ctypes.c_void_p),
+                ("b_post", ctypes.c_void_p), ("w_pre", ctypes.c_void_p),
+                ("b_pre", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("gate_rows", ctypes.c_int64), ("stats", ctypes.c_void_p),
+                ("x", ctypes.c_void_p), ("xo", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64), ("n", ctypes.c_void_p),
+                ("ldn", ctypes.c_int64), ("y_packed", zl_packed), ("n_packed", zl_packed),
+                ("dxo", ctypes.c_void_p), ("dn", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+                ("dy", ctypes.c_void_p), ("dw_post", ctypes.c_void_p),
+                ("db_post", ctypes.c_void_p), ("dw_pre", ctypes.c_void_p),
+                ("db_pre", ctypes.c_void_p), ("dgate", ctypes.c_void_p),
+                ("grad_scale", ctypes.c_float), ("accumulate", ctypes.c_int),
+                ("workspace", ctypes.c_void_p), ("workspace_elems", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -138,6 +172,17 @@ def load(path=None):
         "zl_chunk_save": [vp, ctypes.c_char_p, i64, i64, vp],
         "zl_chunk_load": [vp, ctypes.c_char_p, P(i64), P(i64), vp],
         "zl_checkpoint_read_info": [ctypes.c_char_p, P(zl_checkpoint_info)],
+        "zl_pack": [i64, c, vp, i64, c, P(zl_packed), vp],
+        "zl_unpack": [i64, c, P(zl_packed), vp, i64, c, vp],
+        "zl_mlp_act": [P(zl_mlp_args), vp],
+        "zl_mlp_act_backward": [P(zl_mlp_args), vp],
+        "zl_block_norm": [P(zl_norm_args), vp],
+        "zl_block_norm_backward": [P(zl_norm_args), vp],
+        "zl_block_norm_workspace": [i64, c, i64, P(sz)],
+        "zl_wgrad_packed": [i64, c, c, vp, i64, c, P(zl_packed), ctypes.c_float, c, vp, i64, vp, sz,
+                            vp],
+        "zl_rotary": [i64, c, c, c, vp, i64, vp, i64, c, vp, c, ctypes.c_char_p, ctypes.c_double, c,
+                      vp],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -367,6 +412,54 @@ def zl_checkpoint_read_info(path):
     _check(load().zl_checkpoint_read_info(os.fsencode(path), ctypes.byref(info)),
            "zl_checkpoint_read_info")
     return {n: getattr(info, n) for n, _ in zl_checkpoint_info._fields_}
+
+
+def zl_pack(T, n, x, ldx, dtype, out, stream=0):
+    _check(load().zl_pack(T, n, x, ldx, dtype, ctypes.byref(out), stream), "zl_pack")
+
+
+def zl_unpack(T, n, packed, x, ldx, dtype, stream=0):
+    _check(load().zl_unpack(T, n, ctypes.byref(packed), x, ldx, dtype, stream), "zl_unpack")
+
+
+def zl_mlp_act(args, stream=0):
+    _check(load().zl_mlp_act(ctypes.byref(args), stream), "zl_mlp_act")
+
+
+def zl_mlp_act_backward(args, stream=0):
+    _check(load().zl_mlp_act_backward(ctypes.byref(args), stream), "zl_mlp_act_backward")
+
+
+def zl_block_norm(args, stream=0):
+    _check(load().zl_block_norm(ctypes.byref(args), stream), "zl_block_norm")
+
+
+def zl_block_norm_backward(args, stream=0):
+    _check(load().zl_block_norm_backward(ctypes.byref(args), stream), "zl_block_norm_backward")
+
+
+def zl_block_norm_workspace(T, d, gate_rows=0):
+    """Floats of workspace of zl_block_norm_backward."""
+    n = ctypes.c_size_t()
+    _check(load().zl_block_norm_workspace(T, d, gate_rows, ctypes.byref(n)),
+           "zl_block_norm_workspace")
+    return n.value
+
+
+def zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, x, dw, lddw, scale=1.0, accumulate=0,
+                    workspace=None, workspace_elems=0, stream=0):
+    _check(load().zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, ctypes.byref(x), scale,
+                                  int(accumulate), dw, lddw, workspace, workspace_elems, stream),
+           "zl_wgrad_packed")
+
+
+def zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes, axis_of, theta,
+              inverse=0, stream=0):
+    """axis_of: bytes, one axis number per frequency (rot / 2 of them)."""
+    if rot > 0 and len(axis_of) < rot // 2:
+        raise ValueError(f"axis_of must hold rot / 2 = {rot // 2} axis numbers")
+    _check(load().zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes,
+                            bytes(axis_of), theta, int(inverse), stream), "zl_rotary")
 
 
 def zl_profile_end(h, max_entries=256):

@@ -1,0 +1,211 @@
+"""Refusals of the layer operators (include/zl_layer.h): every call here is
+turned down on the host, before anything is launched (no GPU)."""
+import ctypes
+
+import pytest
+
+from paper_2608_07974_amd import zl
+
+torch = pytest.importorskip("torch")
+from paper_2608_07974_amd import layer  # noqa: E402
+
+A = 1 << 20  # an address that is never used: 16-byte aligned
+INV, UNS, WS = zl.ZL_ERR_INVALID_ARG, zl.ZL_ERR_UNSUPPORTED, zl.ZL_ERR_WORKSPACE
+
+
+def _refused(status, fn, *args, **kw):
+    with pytest.raises(zl.ZlError) as ei:
+        fn(*args, **kw)
+    assert ei.value.status == status, ei.value
+    return str(ei.value)
+
+
+def _pk(n=64, codes=A, scales=A, ldc=None, lds=None):
+    return zl.zl_packed(codes, scales, n if ldc is None else ldc, -(-n // 32) if lds is None else lds)
+
+
+@pytest.mark.parametrize("kw", [dict(T=-1), dict(n=0), dict(n=60), dict(n=-8), dict(x=0), dict(x=A + 8), dict(ldx=56),
+                                dict(ldx=68), dict(dtype=2), dict(p=_pk(codes=0)), dict(p=_pk(scales=0)),
+                                dict(p=_pk(codes=A + 8)), dict(p=_pk(ldc=72)), dict(p=_pk(ldc=48)),
+                                dict(p=_pk(lds=1))])
+def test_pack_refuses(kw):
+    a = dict(T=4, n=64, x=A, ldx=64, dtype=zl.ZL_BF16, p=_pk())
+    a.update(kw)
+    _refused(INV, zl.zl_pack, a["T"], a["n"], a["x"], a["ldx"], a["dtype"], a["p"])
+    _refused(INV, zl.zl_unpack, a["T"], a["n"], a["p"], a["x"], a["ldx"], a["dtype"])
+
+
+def test_null_argument_structures():
+    lib = zl.load()
+    assert lib.zl_pack(4, 64, A, 64, zl.ZL_F32, None, None) == INV
+    assert lib.zl_unpack(4, 64, None, A, 64, zl.ZL_F32, None) == INV
+    for f in (lib.zl_mlp_act, lib.zl_mlp_act_backward, lib.zl_block_norm, lib.zl_block_norm_backward):
+        assert f(None, None) == INV
+    assert lib.zl_block_norm_workspace(4, 64, 0, None) == INV
+    assert lib.zl_wgrad_packed(4, 8, 8, A, 8, zl.ZL_F32, None, 1.0, 0, A, 8, None, 0, None) == INV
+
+
+def _mlp(back, **kw):
+    a = dict(T=4, ff=64, kind=zl.ZL_MLP_SWIGLU, in_dtype=zl.ZL_BF16, out_dtype=zl.ZL_BF16, h=A, ldh=128,
+             packed=zl.zl_packed(), a=A, lda=64)
+    if back:
+        a.update(da=A, ldda=64, dh=A, lddh=128)
+    a.update(kw)
+    return zl.zl_mlp_args(**a)
+
+
+@pytest.mark.parametrize("kw", [dict(T=-1), dict(ff=60), dict(ff=0), dict(kind=2), dict(in_dtype=2), dict(out_dtype=-1),
+                                dict(h=0), dict(h=A + 2), dict(ldh=120), dict(a=A + 8), dict(lda=56),
+                                dict(packed=_pk(64))])
+@pytest.mark.parametrize("back", [False, True])
+def test_mlp_refuses(back, kw):
+    _refused(INV, zl.zl_mlp_act_backward if back else zl.zl_mlp_act, _mlp(back, **kw))
+
+
+def test_mlp_refuses_more():
+    _refused(INV, zl.zl_mlp_act, _mlp(False, a=0))
+    for kw in (dict(da=0), dict(dh=0), dict(ldda=56), dict(lddh=64), dict(packed=_pk(128))):  # the last: h as well
+        _refused(INV, zl.zl_mlp_act_backward, _mlp(True, **kw))
+    for back in (False, True):  # 8-bit blocks that both halves would share
+        kw = dict(ff=40, ldh=80, packed=_pk(80), h=0 if back else A)
+        _refused(UNS, zl.zl_mlp_act_backward if back else zl.zl_mlp_act, _mlp(back, **kw))
+
+
+def _norm(back, **kw):
+    a = dict(T=4, d=64, layernorm=0, in_dtype=zl.ZL_BF16, out_dtype=zl.ZL_BF16, eps=1e-5, scale=1.0, w_post=A, w_pre=A,
+             gate=A, gate_rows=4, stats=A, xo=A, ldx=64, y=A, ldy=64, ldn=64)
+    if back:
+        a.update(dn=A, dx=A, dy=A, dw_post=A, dw_pre=A, dgate=A, grad_scale=1.0, workspace=A, workspace_elems=1 << 30)
+    else:
+        a.update(x=A, n=A)
+    a.update(kw)
+    return zl.zl_norm_args(**a)
+
+
+@pytest.mark.parametrize("kw", [dict(T=-1), dict(d=60), dict(d=0), dict(in_dtype=3), dict(out_dtype=3), dict(eps=0.0),
+                                dict(eps=float("nan")), dict(eps=float("inf")), dict(w_post=0, w_pre=0),
+                                dict(w_post=A + 4), dict(b_post=A), dict(b_pre=A), dict(gate_rows=0),
+                                dict(gate_rows=-3), dict(gate=A + 4), dict(w_post=0), dict(stats=0), dict(stats=A + 8),
+                                dict(xo=0), dict(ldx=60), dict(ldx=56), dict(y=0), dict(y=A + 2), dict(ldy=8),
+                                dict(ldn=8), dict(y_packed=_pk(32))])
+@pytest.mark.parametrize("back", [False, True])
+def test_block_norm_refuses(back, kw):
+    _refused(INV, zl.zl_block_norm_backward if back else zl.zl_block_norm, _norm(back, **kw))
+
+
+def test_block_norm_refuses_more():
+    for kw in (dict(x=0), dict(n=0), dict(n_packed=_pk(32)), dict(w_pre=0, n_packed=_pk())):
+        _refused(INV, zl.zl_block_norm, _norm(False, **kw))
+    for kw in (dict(dx=0), dict(dn=0), dict(dy=0), dict(db_post=A), dict(db_pre=A), dict(gate=0), dict(dgate=A + 4),
+               dict(w_pre=0), dict(dxo=A + 4), dict(y_packed=_pk())):
+        _refused(INV, zl.zl_block_norm_backward, _norm(True, **kw))
+    for back in (False, True):
+        kw = dict(d=8200, ldx=8200, ldy=8200, ldn=8200)
+        _refused(UNS, zl.zl_block_norm_backward if back else zl.zl_block_norm, _norm(back, **kw))
+    need = zl.zl_block_norm_workspace(4, 64, 4)
+    for kw in (dict(workspace=0), dict(workspace=A + 4), dict(workspace_elems=need - 1)):
+        _refused(WS, zl.zl_block_norm_backward, _norm(True, **kw))
+
+
+def test_block_norm_workspace_is_bounded():
+    """Five partial rows per block, of a number of blocks that does not grow
+    with the rows."""
+    for T in (0, 1, 5, 255, 256, 4096, 16384, 1000000):
+        for d in (8, 768, 4096, 8192):
+            for rows in (0, 1, 7, 64, 1000, T, 2 * T + 1):
+                blocks = zl.zl_block_norm_workspace(T, d, rows) // (5 * d)
+                assert min(T, 1) <= blocks <= min(2 * T, 2200), (T, d, rows)
+    for args in ((-1, 64, 0), (4, 60, 0), (4, 64, -1)):
+        _refused(INV, zl.zl_block_norm_workspace, *args)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=-1), INV), (dict(T=1 << 31), UNS), (dict(M=60), INV), (dict(N=0), INV), (dict(dy=0), INV), (dict(dy=A + 4), INV),
+    (dict(lddy=56), INV), (dict(dtype=5), INV), (dict(p=_pk(32)), INV), (dict(p=_pk(codes=A + 8)), INV), (dict(dw=0), INV),
+    (dict(dw=A + 4), INV), (dict(lddw=56), INV), (dict(ws=A + 4), INV)])
+def test_wgrad_refuses(kw, status):
+    a = dict(T=4, M=64, N=64, dy=A, lddy=64, dtype=zl.ZL_BF16, p=_pk(), dw=A, lddw=64, ws=0)
+    a.update(kw)
+    _refused(status, zl.zl_wgrad_packed, a["T"], a["M"], a["N"], a["dy"], a["lddy"], a["dtype"], a["p"], a["dw"], a["lddw"],
+             workspace=a["ws"], workspace_elems=1000)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=-1), INV), (dict(H=0), INV), (dict(hd=7), INV), (dict(hd=0), INV), (dict(hd=258, rot=16), UNS), (dict(rot=3), INV),
+    (dict(rot=0), INV), (dict(rot=18), INV), (dict(axes=bytes([0, 1, 2, 0, 1, 2, 3, 0])), INV), (dict(na=0), INV),
+    (dict(na=17), INV), (dict(theta=1.0), INV), (dict(theta=float("nan")), INV), (dict(theta=float("inf")), INV),
+    (dict(x=0), INV), (dict(out=0), INV), (dict(pos=0), INV), (dict(pos=A + 2), INV), (dict(x=A + 1), INV),
+    (dict(ldx=60), INV), (dict(ldo=63), INV), (dict(ldo=72), INV), (dict(dtype=9), INV), (dict(H=1 << 22, ldx=1 << 30), UNS)])
+def test_rotary_refuses(kw, status):
+    a = dict(T=4, H=4, hd=16, rot=16, x=A, ldx=64, out=A, ldo=64, dtype=zl.ZL_BF16, pos=A, na=3,
+             axes=bytes([0, 1, 2, 0, 1, 2, 0, 0]), theta=1e4)
+    a.update(kw)
+    if len(a["axes"]) < a["rot"] // 2:
+        a["axes"] = bytes(a["rot"] // 2)
+    _refused(status, zl.zl_rotary, a["T"], a["H"], a["hd"], a["rot"], a["x"], a["ldx"], a["out"], a["ldo"], a["dtype"],
+             a["pos"], a["na"], a["axes"], a["theta"])
+
+
+def test_rotary_needs_every_axis_number():
+    with pytest.raises(ValueError, match="axis numbers"):
+        zl.zl_rotary(4, 4, 16, 16, A, 64, A, 64, zl.ZL_BF16, A, 3, bytes(7), 1e4)
+    assert zl.load().zl_rotary(4, 4, 16, 16, A, 64, A, 64, zl.ZL_BF16, A, 3, None, 1e4, 0, None) == INV
+
+
+def test_structures_match_the_header():
+    """Sizes that the C compiler gives the argument structures."""
+    assert ctypes.sizeof(zl.zl_packed) == 32
+    assert ctypes.sizeof(zl.zl_mlp_args) == 8 + 16 + 16 + 32 + 3 * 16
+    assert ctypes.sizeof(zl.zl_norm_args) == 8 + 24 + 6 * 8 + 8 + 7 * 8 + 64 + 9 * 8 + 8 + 16
+
+
+def test_torch_layer_refuses_host_tensors_and_bad_shapes():
+    """The torch functions check what the library cannot see: placement,
+    shapes, types, overlapping rows."""
+    x = torch.zeros(4, 64)
+    with pytest.raises(ValueError, match="GPU"):
+        layer.pack(x, out=layer.Packed.empty(4, 64, "cpu"))
+    with pytest.raises(ValueError):
+        layer.pack(x, out=layer.Packed.empty(3, 64, "cpu"))
+    with pytest.raises(TypeError):
+        layer.pack(x.half())
+    with pytest.raises(ValueError, match="contiguous rows"):
+        layer.pack(torch.zeros(64, 4).t())
+    with pytest.raises(ValueError, match="overlap"):
+        layer.pack(torch.zeros(1, 64).expand(4, 64))
+    with pytest.raises(ValueError):  # the last code row would be read past its end
+        layer.Packed(torch.zeros(4, 72, dtype=torch.uint8), torch.zeros(4, 3, dtype=torch.uint8), 72)
+    with pytest.raises(TypeError):
+        layer.Packed(x, torch.zeros(4, 2, dtype=torch.uint8), 64)
+    with pytest.raises(ValueError):
+        layer.mlp_act(torch.zeros(4, 65))
+    with pytest.raises(KeyError):
+        layer.mlp_act(x, "relu")
+    with pytest.raises(ValueError):
+        layer.mlp_act_bwd(x, torch.zeros(4, 64))
+    with pytest.raises(TypeError):  # h and its gradient of two types
+        layer.mlp_act_bwd(x, torch.zeros(4, 32, dtype=torch.bfloat16))
+    w = torch.ones(64)
+    for kw in (dict(y=None), dict(post=None), dict(post=(torch.ones(63), None)), dict(gate=torch.ones(3, 64), gate_rows=2),
+               dict(gate=torch.ones(2, 64)), dict(stats=torch.zeros(4, 3)), dict(xo=torch.zeros(4, 72)[:, :64]),
+               dict(n=torch.zeros(4, 64), pre=None)):
+        a = dict(y=x, post=(w, None), pre=(w, None))
+        a.update(kw)
+        with pytest.raises(ValueError):
+            layer.block_norm(x, **a)
+    st = torch.zeros(4, 4)
+    for kw in (dict(dn=None), dict(y=None), dict(xo=None), dict(dy=torch.zeros(4, 72)[:, :64]),
+               dict(grads=layer.NormGrads(gate=torch.zeros(1, 64))), dict(grads=layer.NormGrads(w_pre=torch.zeros(63))),
+               dict(dxo=torch.zeros(4, 72)[:, :64])):
+        a = dict(dxo=x, dn=x, y=x, xo=x, stats=st, post=(w, None), pre=(w, None))
+        a.update(kw)
+        with pytest.raises(ValueError):
+            layer.block_norm_bwd(**a)
+    with pytest.raises(ValueError):
+        layer.wgrad(torch.zeros(3, 8), layer.Packed.empty(4, 64, "cpu"))
+    with pytest.raises(TypeError):
+        layer.rotary(x, torch.zeros(3, 4), bytes(8), 4, 16, 1e4)
+    with pytest.raises(TypeError):
+        layer.rotary(x, torch.zeros(3, 5, dtype=torch.int32), bytes(8), 4, 16, 1e4)
+    with pytest.raises(ValueError):
+        layer.rotary(x, torch.zeros(3, 4, dtype=torch.int32), bytes(8), 5, 16, 1e4)
