@@ -1,14 +1,17 @@
 // Weight gradient from a packed activation (include/zl_layer.h):
 //   dw[m, n] = sum_t dy[t, m] x[t, n],  x in 8 bits with a scale per 32 columns.
+//
+// bf16: the weight-gradient GEMM's tiles (gemm_tiles.h, both operands
+// MN-major): dy is copied to LDS by direct loads, x is loaded as codes into
+// registers (half the bytes), turned into bf16 there (exact) and stored to the
+// same LDS layout that the direct copies would leave.
 #include <string.h>
 
-#include "gemm_epilogue.h"
+#include "gemm_tiles.h"
 #include "layer.h"
 #include "packed.h"
 
 namespace zl {
-
-hipError_t launch_splitk_reduce(const float* part, int nz, int M, int N, const EpiArgs& e, hipStream_t s);
 
 // ------------------------------------------------------------ vector ALUs
 // 64 x 64 tiles, 16 tokens a step, 4 x 4 outputs per thread.  A block has
@@ -98,8 +101,225 @@ static hipError_t wgrad_valu(const WgradArgs& a, hipStream_t s) {
   return launch_splitk_reduce(a.part, (int)nz, a.M, a.N, grad_epi(a), s);
 }
 
+// ------------------------------------------------------------------- MFMA
+__device__ uint8_t llvm_amdgcn_raw_buffer_load_u8(i32x4_t rsrc, uint32_t voffset, uint32_t soffset, int aux)
+    __asm("llvm.amdgcn.raw.buffer.load.i8");
+
+// One thread's share of a k tile of x: 16 codes of one token and their scale
+// byte.  Tokens and columns outside the matrix read as zero codes.
+template <int BN, int BK, int NT>
+struct CodeTile {
+  static constexpr int CPR = BN / 16;  // 16-code chunks per token
+  static_assert(CPR * BK == NT, "one chunk per thread");
+  uint32_t coff, soff;  // byte offsets at k0 = 0, or DMA_OOB
+  uint32_t cstep, sstep;  // bytes per token
+  int k;
+  uint32_t lds;  // byte offset of the chunk's two 16-byte pieces in the bf16 tile
+
+  __device__ __forceinline__ void init(const zl_packed& x, int n0, int nvalid) {
+    k = threadIdx.x / CPR;
+    const int q = threadIdx.x % CPR;
+    const bool ok = q * 16 < nvalid;
+    cstep = (uint32_t)x.ld_codes;
+    sstep = (uint32_t)x.ld_scales;
+    coff = ok ? k * cstep + q * 16 : DMA_OOB;
+    soff = ok ? k * sstep + q / 2 : DMA_OOB;
+    // pieces 2 q and 2 q + 1 of LDS row k; the swizzle is even, so they stay together
+    lds = (uint32_t)(k * BN * 2 + ((2 * q) ^ xsk<32>(k)) * 16);
+  }
+  __device__ __forceinline__ void load(uint4& c, uint32_t& s, int k0, int kvalid, i32x4_t rc, i32x4_t rs) const {
+    const bool in = k0 + k < kvalid;
+    c = __builtin_bit_cast(uint4, buffer_load16(rc, in ? coff + (uint32_t)k0 * cstep : DMA_OOB));
+    s = llvm_amdgcn_raw_buffer_load_u8(rs, in ? soff + (uint32_t)k0 * sstep : DMA_OOB, 0, 0);
+  }
+  // 4 codes to bf16; a scale byte of 255 makes NaN of any code
+  __device__ static __forceinline__ uint2 widen(uint32_t w, uint32_t s) {
+    w = s == 255 ? 0x7f7f7f7fu : w;
+    const float f = __uint_as_float(s << 23);
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, true)));
+  }
+  __device__ __forceinline__ void store(const uint4& c, uint32_t s, unsigned char* tile) const {
+    const uint2 a = widen(c.x, s), b = widen(c.y, s), d = widen(c.z, s), e = widen(c.w, s);
+    *reinterpret_cast<uint4*>(tile + lds) = make_uint4(a.x, a.y, b.x, b.y);
+    *reinterpret_cast<uint4*>(tile + lds + 16) = make_uint4(d.x, d.y, e.x, e.y);
+  }
+};
+
+// NST LDS stages of BK tokens.  In the last slice of tile kt, behind the barrier
+// that releases its stage: x of tile kt + NST goes from registers into the
+// stage, the codes of tile kt + NST + D are loaded in their place, and dy of
+// tile kt + NST starts on its way.  Codes before dy: waiting for the oldest codes
+// then leaves the newest copy of dy in flight.
+template <int BM, int BN, int WM, int WN, int NST, int D>
+__global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, EpiArgs e, zl_packed x) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int BK = 32, MF = 32, NT = WM * WN * 64;
+  constexpr int TM = BM / WM, TN = BN / WN, FM = TM / MF, FN = TN / MF, NS = BK / Mma<MF>::KS, NMF = FM * FN;
+  constexpr uint32_t ABYTES = BM * BK * 2, STAGE = (BM + BN) * BK * 2;
+  using TA = DmaTile<BM, BK, NT, false, MF>;
+  constexpr int PER_TILE = TA::ITEMS + 2;
+  static_assert(NS == 2 && NMF >= 4 && NST >= 3 && D >= 2 && (NST - 2) * PER_TILE < 64, "schedule");
+
+  int tm, tn;
+  tile_coords(blockIdx.x, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wm = wave / WN, wn = wave % WN;
+  const int kbeg = blockIdx.z * g.ksplit, klen = min(g.K - kbeg, g.ksplit);
+  const i32x4_t ra = buffer_rsrc(static_cast<const bf16_t*>(g.A) + (int64_t)kbeg * g.lda + m0);
+  const i32x4_t rc = buffer_rsrc(static_cast<const uint8_t*>(x.codes) + kbeg * x.ld_codes + n0);
+  const i32x4_t rs = buffer_rsrc(static_cast<const uint8_t*>(x.scales) + kbeg * x.ld_scales + n0 / PBLK);
+  TA da;
+  da.init(wave, lane, g.lda, min(g.M - m0, BM));
+  CodeTile<BN, BK, NT> tb;
+  tb.init(x, n0, min(g.N - n0, BN));
+  FragTile<BM, BK, FM, false, MF> fa;
+  FragTile<BN, BK, FN, false, MF> fb;
+  fa.init(wm * TM, lane);
+  fb.init(wn * TN, lane);
+
+  f32x16_t acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(smem);
+  // whole rounds of D tiles (the register sets' indexes are compile-time):
+  // tiles past klen are zeros
+  const int nk = ((klen + BK - 1) / BK + D - 1) / D * D;
+#pragma unroll
+  for (int t = 0; t < NST; ++t) da.issue(lds0 + t * STAGE, wave, t * BK, klen, ra);
+  uint4 c[D];
+  uint32_t sc[D];
+  {
+    uint4 pc[NST];
+    uint32_t ps[NST];
+#pragma unroll
+    for (int t = 0; t < NST; ++t) tb.load(pc[t], ps[t], t * BK, klen, rc, rs);
+#pragma unroll
+    for (int t = 0; t < D; ++t) tb.load(c[t], sc[t], (NST + t) * BK, klen, rc, rs);
+#pragma unroll
+    for (int t = 0; t < NST; ++t) tb.store(pc[t], ps[t], smem + t * STAGE + ABYTES);
+  }
+  wait_vmcnt<2 * D>();  // every copy of dy was issued before the codes
+  __syncthreads();
+  bf16x8_t af[2][FM], bfr[2][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) af[0][i] = fa.read(reinterpret_cast<const bf16_t*>(smem), 0, i);
+#pragma unroll
+  for (int j = 0; j < FN; ++j) bfr[0][j] = fb.read(reinterpret_cast<const bf16_t*>(smem) + BM * BK, 0, j);
+  int rd = 0;
+  for (int kt0 = 0; kt0 < nk; kt0 += D) {
+#pragma unroll
+    for (int u = 0; u < D; ++u) {
+      const int kt = kt0 + u;
+      const int rn = rd + 1 == NST ? 0 : rd + 1;
+      const bf16_t* as = reinterpret_cast<const bf16_t*>(smem + rd * STAGE);
+      const bf16_t* an = reinterpret_cast<const bf16_t*>(smem + rn * STAGE);
+      uint2 w[4];
+#pragma unroll
+      for (int q = 0; q < NS; ++q) {
+        const int cb = q, nb = q ^ 1;
+        const bf16_t* src = q + 1 < NS ? as : an;
+        const int qs = q + 1 < NS ? q + 1 : 0;
+        if (q + 1 == NS) {
+          wait_vmcnt<(NST - 2) * PER_TILE>();  // this wave's share of dy of tile kt + 1
+          __syncthreads();                      // everyone's share and x; tile kt fully read
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < NMF; ++t) {
+          acc[t / FN][t % FN] = Mma<MF>::run(af[cb][t / FN], bfr[cb][t % FN], acc[t / FN][t % FN]);
+#pragma unroll
+          for (int r = 0; r < FM + FN; ++r) {
+            if (r * NMF / (FM + FN) != t) continue;
+            if (r < FM) af[nb][r] = fa.read(src, qs, r);
+            else bfr[nb][r - FM] = fb.read(src + BM * BK, qs, r - FM);
+          }
+          if (q + 1 == NS) {
+            unsigned char* st = smem + rd * STAGE + ABYTES + tb.lds;
+            if (t < 2) {
+              w[2 * t] = tb.widen(t == 0 ? c[u].x : c[u].z, sc[u]);
+              w[2 * t + 1] = tb.widen(t == 0 ? c[u].y : c[u].w, sc[u]);
+              *reinterpret_cast<uint4*>(st + 16 * t) = make_uint4(w[2 * t].x, w[2 * t].y, w[2 * t + 1].x, w[2 * t + 1].y);
+            }
+            if (t == 2) tb.load(c[u], sc[u], (kt + NST + D) * BK, klen, rc, rs);
+            if (t == 3) da.issue(lds0 + rd * STAGE, wave, (kt + NST) * BK, klen, ra);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      rd = rn;
+    }
+  }
+  dma_wait();  // zero-fill copies past the end must land before LDS is reused
+  __syncthreads();
+  store_tile<BM, BN, WM, WN, MF>(acc, smem, g, e, m0, n0, wave, lane);
+}
+
+template <int BM, int BN, int WM, int WN, int NST, int D>
+static hipError_t wgrad_mfma(const GemmDesc& g, const EpiArgs& e, const zl_packed& x, int nz, hipStream_t s) {
+  auto kern = wgrad_mfma_kernel<BM, BN, WM, WN, NST, D>;
+  const size_t main = (size_t)NST * (BM + BN) * 32 * sizeof(bf16_t), epi = (size_t)WM * WN * 32 * (BN / WN + 4) * sizeof(float);
+  const size_t lds = main > epi ? main : epi;
+  hipError_t err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (err != hipSuccess) return err;
+  const int nb = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
+  hipLaunchKernelGGL(kern, dim3(nb, 1, nz), dim3(WM * WN * 64), lds, s, g, e, x);
+  return hipGetLastError();
+}
+
+// One segment of tokens whose buffer offsets stay below 2^31.
+static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accumulate, hipStream_t s) {
+  GemmDesc g;
+  memset(&g, 0, sizeof(g));
+  g.M = a.M;
+  g.N = a.N;
+  g.K = T;
+  g.A = static_cast<const bf16_t*>(a.dy) + t0 * a.lddy;
+  g.lda = a.lddy;
+  zl_packed x = a.x;
+  x.codes = static_cast<uint8_t*>(x.codes) + t0 * x.ld_codes;
+  x.scales = static_cast<uint8_t*>(x.scales) + t0 * x.ld_scales;
+  EpiArgs e = grad_epi(a);
+  e.accumulate = accumulate;
+  const GemmPlan plan = plan_gemm({a.M, a.N, T, false, false, a.part != nullptr, a.part_elems, false, 0});
+  const int nz = split_k(T, plan.nz, 32, g.ksplit);
+  EpiArgs ep = e;
+  if (nz > 1) {
+    memset(&ep, 0, sizeof(ep));
+    ep.kind = EPI_STORE;
+    ep.out = a.part;
+    ep.ldo = a.N;
+    ep.out_dtype = F32;
+    ep.scale = 1.f;
+    ep.zstride = (int64_t)a.M * a.N;
+  }
+  hipError_t err = plan.large ? wgrad_mfma<256, 256, 4, 2, 3, 2>(g, ep, x, nz, s)
+                              : wgrad_mfma<128, 128, 2, 2, 3, 2>(g, ep, x, nz, s);
+  if (err != hipSuccess || nz == 1) return err;
+  return launch_splitk_reduce(a.part, nz, a.M, a.N, e, s);
+}
+
 hipError_t launch_wgrad_packed(const WgradArgs& a, int dtype, hipStream_t s) {
-  return dtype == BF16 ? wgrad_valu<true>(a, s) : wgrad_valu<false>(a, s);
+  if (dtype != BF16) return wgrad_valu<false>(a, s);
+  // tokens per launch: the largest offset from a tile's origin stays below 2^31
+  const int64_t row = 2 * a.lddy > a.x.ld_codes ? 2 * a.lddy : a.x.ld_codes;
+  const int64_t top = row > a.x.ld_scales ? row : a.x.ld_scales;
+  const int64_t most = (((int64_t)1 << 31) - 1024) / top - 1024;
+  if (a.T > 0 && a.T <= most) return wgrad_segment(a, 0, (int)a.T, a.accumulate != 0, s);
+  if (a.T == 0 || most < 4096) return wgrad_valu<true>(a, s);
+  const int64_t step = most / 32 * 32;
+  for (int64_t t = 0; t < a.T; t += step) {
+    const int64_t n = a.T - t < step ? a.T - t : step;
+    hipError_t err = wgrad_segment(a, t, (int)n, t > 0 || a.accumulate, s);
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 
 }  // namespace zl

@@ -440,7 +440,7 @@ def test_block_norm_empty_batch():
 @pytest.mark.parametrize("dt", [F32, BF])
 @pytest.mark.parametrize("T,M,N,pad", [(1, 8, 8, 0), (33, 72, 40, 16), (31, 256, 256, 0), (32, 264, 48, 0), (64, 128, 1000, 0),
                                        (1000, 264, 520, 16), (5000, 64, 64, 0), (4096, 136, 768, 0), (700, 520, 2056, 0),
-                                       (257, 2048, 264, 0), (1024, 768, 768, 0)])
+                                       (257, 2048, 264, 0), (1024, 768, 768, 0), (333, 4096, 3848, 0)])
 @pytest.mark.parametrize("ws", [0, 1 << 22])
 def test_wgrad(dt, T, M, N, pad, ws):
     layer = _L()
