@@ -105,20 +105,26 @@ static hipError_t wgrad_valu(const WgradArgs& a, hipStream_t s) {
 __device__ uint8_t llvm_amdgcn_raw_buffer_load_u8(i32x4_t rsrc, uint32_t voffset, uint32_t soffset, int aux)
     __asm("llvm.amdgcn.raw.buffer.load.i8");
 
+// A buffer that ends with column `cols` of row `rows` - 1 (esz bytes each, row
+// stride ld): offsets of later rows lie past it, and read as zero.
+__device__ __forceinline__ i32x4_t rows_rsrc(const void* p, int64_t ld, int rows, int cols, int esz) {
+  i32x4_t r = buffer_rsrc(p);
+  r[2] = (int32_t)((uint32_t)((rows - 1) * ld + cols) * (uint32_t)esz);
+  return r;
+}
+
 // One thread's share of a k tile of x: 16 codes of one token and their scale
-// byte.  Tokens and columns outside the matrix read as zero codes.
+// byte.  Columns outside the matrix have DMA_OOB, which no advance brings back.
 template <int BN, int BK, int NT>
 struct CodeTile {
   static constexpr int CPR = BN / 16;  // 16-code chunks per token
   static_assert(CPR * BK == NT, "one chunk per thread");
-  uint32_t coff, soff;  // byte offsets at k0 = 0, or DMA_OOB
+  uint32_t coff, soff;    // byte offsets at k0 = 0
   uint32_t cstep, sstep;  // bytes per token
-  int k;
-  uint32_t lds;  // byte offset of the chunk's two 16-byte pieces in the bf16 tile
+  uint32_t lds;           // byte offset of the chunk's two 16-byte pieces in the bf16 tile
 
-  __device__ __forceinline__ void init(const zl_packed& x, int n0, int nvalid) {
-    k = threadIdx.x / CPR;
-    const int q = threadIdx.x % CPR;
+  __device__ __forceinline__ void init(const zl_packed& x, int nvalid) {
+    const int k = threadIdx.x / CPR, q = threadIdx.x % CPR;
     const bool ok = q * 16 < nvalid;
     cstep = (uint32_t)x.ld_codes;
     sstep = (uint32_t)x.ld_scales;
@@ -127,10 +133,9 @@ struct CodeTile {
     // pieces 2 q and 2 q + 1 of LDS row k; the swizzle is even, so they stay together
     lds = (uint32_t)(k * BN * 2 + ((2 * q) ^ xsk<32>(k)) * 16);
   }
-  __device__ __forceinline__ void load(uint4& c, uint32_t& s, int k0, int kvalid, i32x4_t rc, i32x4_t rs) const {
-    const bool in = k0 + k < kvalid;
-    c = __builtin_bit_cast(uint4, buffer_load16(rc, in ? coff + (uint32_t)k0 * cstep : DMA_OOB));
-    s = llvm_amdgcn_raw_buffer_load_u8(rs, in ? soff + (uint32_t)k0 * sstep : DMA_OOB, 0, 0);
+  __device__ __forceinline__ void load(uint4& c, uint32_t& s, int k0, i32x4_t rc, i32x4_t rs) const {
+    c = __builtin_bit_cast(uint4, buffer_load16(rc, coff + (uint32_t)k0 * cstep));
+    s = llvm_amdgcn_raw_buffer_load_u8(rs, soff + (uint32_t)k0 * sstep, 0, 0);
   }
   // 4 codes to bf16; a scale byte of 255 makes NaN of any code
   __device__ static __forceinline__ uint2 widen(uint32_t w, uint32_t s) {
@@ -139,19 +144,23 @@ struct CodeTile {
     return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, false)),
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, true)));
   }
-  __device__ __forceinline__ void store(const uint4& c, uint32_t s, unsigned char* tile) const {
-    const uint2 a = widen(c.x, s), b = widen(c.y, s), d = widen(c.z, s), e = widen(c.w, s);
-    *reinterpret_cast<uint4*>(tile + lds) = make_uint4(a.x, a.y, b.x, b.y);
-    *reinterpret_cast<uint4*>(tile + lds + 16) = make_uint4(d.x, d.y, e.x, e.y);
+  // codes 8 h .. 8 h + 7 into the tile
+  __device__ __forceinline__ void store_half(const uint4& c, uint32_t s, unsigned char* tile, int h) const {
+    const uint2 a = widen(h ? c.z : c.x, s), b = widen(h ? c.w : c.y, s);
+    *reinterpret_cast<uint4*>(tile + lds + 16 * h) = make_uint4(a.x, a.y, b.x, b.y);
   }
 };
 
-// NST LDS stages of BK tokens.  In the last slice of tile kt, behind the barrier
-// that releases its stage: x of tile kt + NST goes from registers into the
-// stage, the codes of tile kt + NST + D are loaded in their place, and dy of
-// tile kt + NST starts on its way.  Codes before dy: waiting for the oldest codes
-// then leaves the newest copy of dy in flight.
-template <int BM, int BN, int WM, int WN, int NST, int D>
+// NST LDS stages of 32 tokens and as many register sets of codes.  In the last
+// slice of tile kt, behind the barrier that releases its stage: x of tile kt + NST
+// goes from its registers into the stage, the codes of tile kt + 2 NST are
+// loaded in their place, and dy of tile kt + NST starts on its way.  Codes before
+// dy: waiting for the oldest codes then leaves the newest copies of dy in flight.
+// The loop runs whole rounds of NST tiles, so that stages and register sets are
+// compile-time (16384 x 14336 x 4096: 1609 us, 1669 with a run-time stage); tiles
+// past the end are zeros by the buffers' ends, without a test per load (1519 us;
+// the bf16 GEMM of that size 1529, both at 1.26 - 1.27 PFLOP/s).
+template <int BM, int BN, int WM, int WN, int NST>
 __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, EpiArgs e, zl_packed x) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int BK = 32, MF = 32, NT = WM * WN * 64;
@@ -159,7 +168,7 @@ __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, Ep
   constexpr uint32_t ABYTES = BM * BK * 2, STAGE = (BM + BN) * BK * 2;
   using TA = DmaTile<BM, BK, NT, false, MF>;
   constexpr int PER_TILE = TA::ITEMS + 2;
-  static_assert(NS == 2 && NMF >= 4 && NST >= 3 && D >= 2 && (NST - 2) * PER_TILE < 64, "schedule");
+  static_assert(NS == 2 && NMF >= 4 && NST >= 3 && (NST - 2) * PER_TILE < 64, "schedule");
 
   int tm, tn;
   tile_coords(blockIdx.x, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN, tm, tn);
@@ -167,13 +176,21 @@ __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, Ep
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wm = wave / WN, wn = wave % WN;
   const int kbeg = blockIdx.z * g.ksplit, klen = min(g.K - kbeg, g.ksplit);
-  const i32x4_t ra = buffer_rsrc(static_cast<const bf16_t*>(g.A) + (int64_t)kbeg * g.lda + m0);
-  const i32x4_t rc = buffer_rsrc(static_cast<const uint8_t*>(x.codes) + kbeg * x.ld_codes + n0);
-  const i32x4_t rs = buffer_rsrc(static_cast<const uint8_t*>(x.scales) + kbeg * x.ld_scales + n0 / PBLK);
+  const int mv = min(g.M - m0, BM), nv = min(g.N - n0, BN);
+  const i32x4_t ra = rows_rsrc(static_cast<const bf16_t*>(g.A) + (int64_t)kbeg * g.lda + m0, g.lda, klen, mv, 2);
+  const i32x4_t rc = rows_rsrc(static_cast<const uint8_t*>(x.codes) + kbeg * x.ld_codes + n0, x.ld_codes, klen,
+                               (nv + 15) / 16 * 16, 1);
+  const i32x4_t rs = rows_rsrc(static_cast<const uint8_t*>(x.scales) + kbeg * x.ld_scales + n0 / PBLK, x.ld_scales, klen,
+                               (nv + PBLK - 1) / PBLK, 1);
   TA da;
-  da.init(wave, lane, g.lda, min(g.M - m0, BM));
+  da.init(wave, lane, g.lda, mv);
+  auto copy_dy = [&](uint32_t stage, int k0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < TA::ITEMS; ++j)
+      dma16(stage + (uint32_t)(wave * TA::ITEMS + j) * 1024u, da.off[j] + (uint32_t)k0 * da.kstride, ra);
+  };
   CodeTile<BN, BK, NT> tb;
-  tb.init(x, n0, min(g.N - n0, BN));
+  tb.init(x, nv);
   FragTile<BM, BK, FM, false, MF> fa;
   FragTile<BN, BK, FN, false, MF> fb;
   fa.init(wm * TM, lane);
@@ -188,39 +205,37 @@ __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, Ep
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(smem);
-  // whole rounds of D tiles (the register sets' indexes are compile-time):
-  // tiles past klen are zeros
-  const int nk = ((klen + BK - 1) / BK + D - 1) / D * D;
-#pragma unroll
-  for (int t = 0; t < NST; ++t) da.issue(lds0 + t * STAGE, wave, t * BK, klen, ra);
-  uint4 c[D];
-  uint32_t sc[D];
+  const int nk = (klen + BK - 1) / BK;
+  uint4 c[NST];
+  uint32_t sc[NST];
   {
     uint4 pc[NST];
     uint32_t ps[NST];
 #pragma unroll
-    for (int t = 0; t < NST; ++t) tb.load(pc[t], ps[t], t * BK, klen, rc, rs);
+    for (int t = 0; t < NST; ++t) tb.load(pc[t], ps[t], t * BK, rc, rs);
 #pragma unroll
-    for (int t = 0; t < D; ++t) tb.load(c[t], sc[t], (NST + t) * BK, klen, rc, rs);
+    for (int t = 0; t < NST; ++t) copy_dy(lds0 + t * STAGE, t * BK);
 #pragma unroll
-    for (int t = 0; t < NST; ++t) tb.store(pc[t], ps[t], smem + t * STAGE + ABYTES);
+    for (int t = 0; t < NST; ++t) tb.load(c[t], sc[t], (NST + t) * BK, rc, rs);
+#pragma unroll
+    for (int t = 0; t < NST; ++t) {
+      tb.store_half(pc[t], ps[t], smem + t * STAGE + ABYTES, 0);
+      tb.store_half(pc[t], ps[t], smem + t * STAGE + ABYTES, 1);
+    }
   }
-  wait_vmcnt<2 * D>();  // every copy of dy was issued before the codes
+  wait_vmcnt<2 * NST>();  // dy of the first NST tiles; the codes after it may be in flight
   __syncthreads();
   bf16x8_t af[2][FM], bfr[2][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i) af[0][i] = fa.read(reinterpret_cast<const bf16_t*>(smem), 0, i);
 #pragma unroll
   for (int j = 0; j < FN; ++j) bfr[0][j] = fb.read(reinterpret_cast<const bf16_t*>(smem) + BM * BK, 0, j);
-  int rd = 0;
-  for (int kt0 = 0; kt0 < nk; kt0 += D) {
+  for (int kt0 = 0; kt0 < nk; kt0 += NST) {
 #pragma unroll
-    for (int u = 0; u < D; ++u) {
+    for (int u = 0; u < NST; ++u) {
       const int kt = kt0 + u;
-      const int rn = rd + 1 == NST ? 0 : rd + 1;
-      const bf16_t* as = reinterpret_cast<const bf16_t*>(smem + rd * STAGE);
-      const bf16_t* an = reinterpret_cast<const bf16_t*>(smem + rn * STAGE);
-      uint2 w[4];
+      const bf16_t* as = reinterpret_cast<const bf16_t*>(smem + u * STAGE);
+      const bf16_t* an = reinterpret_cast<const bf16_t*>(smem + (u + 1 < NST ? u + 1 : 0) * STAGE);
 #pragma unroll
       for (int q = 0; q < NS; ++q) {
         const int cb = q, nb = q ^ 1;
@@ -241,19 +256,13 @@ __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, Ep
             else bfr[nb][r - FM] = fb.read(src + BM * BK, qs, r - FM);
           }
           if (q + 1 == NS) {
-            unsigned char* st = smem + rd * STAGE + ABYTES + tb.lds;
-            if (t < 2) {
-              w[2 * t] = tb.widen(t == 0 ? c[u].x : c[u].z, sc[u]);
-              w[2 * t + 1] = tb.widen(t == 0 ? c[u].y : c[u].w, sc[u]);
-              *reinterpret_cast<uint4*>(st + 16 * t) = make_uint4(w[2 * t].x, w[2 * t].y, w[2 * t + 1].x, w[2 * t + 1].y);
-            }
-            if (t == 2) tb.load(c[u], sc[u], (kt + NST + D) * BK, klen, rc, rs);
-            if (t == 3) da.issue(lds0 + rd * STAGE, wave, (kt + NST) * BK, klen, ra);
+            if (t < 2) tb.store_half(c[u], sc[u], smem + u * STAGE + ABYTES, t);
+            if (t == 2) tb.load(c[u], sc[u], (kt + 2 * NST) * BK, rc, rs);
+            if (t == 3) copy_dy(lds0 + u * STAGE, (kt + NST) * BK);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      rd = rn;
     }
   }
   dma_wait();  // zero-fill copies past the end must land before LDS is reused
@@ -261,9 +270,9 @@ __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, Ep
   store_tile<BM, BN, WM, WN, MF>(acc, smem, g, e, m0, n0, wave, lane);
 }
 
-template <int BM, int BN, int WM, int WN, int NST, int D>
+template <int BM, int BN, int WM, int WN, int NST>
 static hipError_t wgrad_mfma(const GemmDesc& g, const EpiArgs& e, const zl_packed& x, int nz, hipStream_t s) {
-  auto kern = wgrad_mfma_kernel<BM, BN, WM, WN, NST, D>;
+  auto kern = wgrad_mfma_kernel<BM, BN, WM, WN, NST>;
   const size_t main = (size_t)NST * (BM + BN) * 32 * sizeof(bf16_t), epi = (size_t)WM * WN * 32 * (BN / WN + 4) * sizeof(float);
   const size_t lds = main > epi ? main : epi;
   hipError_t err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -299,8 +308,10 @@ static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accu
     ep.scale = 1.f;
     ep.zstride = (int64_t)a.M * a.N;
   }
-  hipError_t err = plan.large ? wgrad_mfma<256, 256, 4, 2, 3, 2>(g, ep, x, nz, s)
-                              : wgrad_mfma<128, 128, 2, 2, 3, 2>(g, ep, x, nz, s);
+  // 4 stages for large tiles (3: 1526 us at 16384 x 14336 x 4096, 5: 1534), 3 for
+  // small ones, which share a CU (4096 x 2304 x 768: 32.8; 4 stages 33.5, 8 42.2)
+  hipError_t err = plan.large ? wgrad_mfma<256, 256, 4, 2, 4>(g, ep, x, nz, s)
+                              : wgrad_mfma<128, 128, 2, 2, 3>(g, ep, x, nz, s);
   if (err != hipSuccess || nz == 1) return err;
   return launch_splitk_reduce(a.part, nz, a.M, a.N, e, s);
 }
