@@ -31,6 +31,9 @@ def _ptr(t):
 
 
 def _check_device(dev, *named):
+    """Every tensor of (name, tensor or None) pairs is on the GPU dev.  (The
+    host's share of a small call is most of it: the checks of this file are
+    written for the case that passes.)"""
     if dev.type != "cuda":
         raise ValueError(f"tensors must be on a GPU, not {dev}")
     for name, t in named:
@@ -40,31 +43,44 @@ def _check_device(dev, *named):
 
 def _rows(name, t, T, n, dtypes):
     """Row stride of a [T, n] matrix with contiguous rows."""
+    if t.dtype in dtypes and t.shape == (T, n):
+        s0, s1 = t.stride()
+        if s1 == 1 and s0 >= n and T > 1:
+            return s0
+        if n > 1 and s1 != 1:
+            raise ValueError(f"{name} must have contiguous rows")
+        if T > 1:
+            raise ValueError(f"{name} must not overlap itself")
+        return _up(n, 8)
     if t.dtype not in dtypes:
         raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != n:
-        raise ValueError(f"{name} must be [{T}, {n}], not {list(t.shape)}")
-    if n > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must have contiguous rows")
-    ld = t.stride(0) if T > 1 else _up(n, 8)
-    if T > 1 and ld < n:
-        raise ValueError(f"{name} must not overlap itself")
-    return ld
+    raise ValueError(f"{name} must be [{T}, {n}], not {list(t.shape)}")
 
 
 def _vec(name, t, n):
-    if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous()):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 vector of {n}")
-    return _ptr(t)
+    return t.data_ptr()
+
+
+# torch's own accessor of the current stream's handle, without a Stream object
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_one_gpu = None  # whether this process sees one GPU only
 
 
 def _call(fn, dev, *args):
     """fn(*args, stream) on dev's current stream, with dev current."""
-    if torch.cuda.current_device() == dev.index:
-        fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    global _one_gpu
+    if _one_gpu is None:
+        _one_gpu = torch.cuda.device_count() == 1
+    if _one_gpu or torch.cuda.current_device() == dev.index:
+        fn(*args, _raw_stream(dev.index))
     else:
         with torch.cuda.device(dev):
-            fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            fn(*args, _raw_stream(dev.index))
 
 
 class Packed:
@@ -74,19 +90,23 @@ class Packed:
     __slots__ = ("codes", "scales", "n", "struct")
 
     def __init__(self, codes, scales, n):
-        T = codes.shape[0]
-        for name, t, cols in (("codes", codes, _up(n, 16)), ("scales", scales, (n + 31) // 32)):
-            if t.dtype != torch.uint8 or t.dim() != 2:
-                raise TypeError(f"{name} must be a uint8 matrix")
-            if t.shape[0] != T or t.shape[1] < cols:
-                raise ValueError(f"{name} must be [{T}, >= {cols}], not {list(t.shape)}")
-            if t.stride(1) != 1 and t.shape[1] > 1:
-                raise ValueError(f"{name} must have contiguous rows")
+        T, W = codes.shape if codes.dim() == 2 else (-1, -1)
+        c16, c32 = _up(n, 16), (n + 31) // 32
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or T < 0 or scales.dim() != 2:
+            raise TypeError("codes and scales must be uint8 matrices")
+        if W < c16 or scales.shape[0] != T or scales.shape[1] < c32:
+            raise ValueError(f"codes and scales must be [{T}, >= {c16}] and [{T}, >= {c32}], not {list(codes.shape)} and "
+                             f"{list(scales.shape)}")
+        (lc, c1), (ls, s1) = codes.stride(), scales.stride()
+        if (c1 != 1 and W > 1) or (s1 != 1 and scales.shape[1] > 1):
+            raise ValueError("codes and scales must have contiguous rows")
+        if T > 1 and (lc < c16 or ls < c32):
+            raise ValueError("codes and scales must not overlap themselves")
         if codes.device != scales.device:
             raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
         self.codes, self.scales, self.n = codes, scales, n
-        lc = codes.stride(0) if T > 1 else _up(n, 16)
-        ls = scales.stride(0) if T > 1 else (n + 31) // 32
+        if T <= 1:
+            lc, ls = c16, c32
         self.struct = zl.zl_packed(codes.data_ptr(), scales.data_ptr(), lc, ls)
 
     @classmethod
@@ -107,7 +127,7 @@ class Packed:
 
 
 def _packed(name, p, T, n):
-    if tuple(p.shape) != (T, n):
+    if p.n != n or p.codes.shape[0] != T:
         raise ValueError(f"{name} must be [{T}, {n}], not {list(p.shape)}")
     return p.struct
 
