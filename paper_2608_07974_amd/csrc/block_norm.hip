@@ -1,29 +1,33 @@
 // Norms around a block (include/zl_layer.h, zl_block_norm): the norm of a
 // block's output, its gate and residual scale, the addition to the residual
 // stream and the norm before the next block, in one pass over the rows, forward
-// and backward.  Bound by memory: forward 12 to 18 bytes a column with bf16
-// products, backward 17 to 19.
+// and backward.  Bound by memory: with bf16 products 12 bytes a column forward
+// (14 with both copies), 17 to 18 backward.
 #include "layer.h"
 #include "packed.h"
 
 namespace zl {
 
-// Sums over the NW waves of a row (nw at run time where NW is 0).  red: two
-// buffers used in turn, so one barrier per sum.
+// The sum of a wave's lanes, in every lane: within rows of 16 by DPP moves (lane
+// bits 0 and 1, then the mirrored lane of 8 and of 16), two exchanges beyond.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+}
 __device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  v = dpp_add<0x140>(dpp_add<0x141>(dpp_add<0x4E>(dpp_add<0xB1>(v))));
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
 }
 
 // ----------------------------------------------------------------- forward
 // NW waves per row, lane columns 8 (64 NW k + lane), k < G: the row stays in
 // registers between its sums (variance from centred values).
-template <int NW, int G, bool BI, bool BO>
+template <int NW, int G, bool BI, bool BO, bool NT>
 __global__ void __launch_bounds__(256) block_norm_fwd_kernel(zl_norm_args a) {
   __shared__ float red[2][4];
   const int lane = threadIdx.x % (64 * NW);
-  const int64_t r = (int64_t)blockIdx.x * (4 / NW) + threadIdx.x / (64 * NW);
+  const int64_t r = (int64_t)blockIdx.x * (4 / NW) + __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * NW));
   if (NW == 1 && r >= a.T) return;
   int par = 0;
   auto row_sum = [&](float v) __attribute__((always_inline)) {
@@ -68,8 +72,8 @@ __global__ void __launch_bounds__(256) block_norm_fwd_kernel(zl_norm_args a) {
     rx[k].zero();
     ry[k].zero();
     if (c < a.d) {
-      rx[k].load(a.x, r * a.ldx + c);
-      if (post) ry[k].load(a.y, r * a.ldy + c);
+      rx[k].load(a.x, r * a.ldx, c);
+      if (post) ry[k].load(a.y, r * a.ldy, c);
     }
   }
   float x[G][PW];
@@ -85,7 +89,7 @@ __global__ void __launch_bounds__(256) block_norm_fwd_kernel(zl_norm_args a) {
         const int c = (k * 64 * NW + lane) * PW;
         uint32_t sb;
         const uint2 code = pack8(y[k], sb);
-        if (c < a.d) store_packed(a.y_packed, r, c, code, sb);
+        if (c < a.d) store_packed<NT>(a.y_packed, r, c, code, sb);
       }
     }
     r0 = centre(y, m0);
@@ -96,22 +100,22 @@ __global__ void __launch_bounds__(256) block_norm_fwd_kernel(zl_norm_args a) {
       if (c >= a.d) continue;
       float w[PW], b[PW], g[PW];
       Raw8<false> t;
-      t.load(a.w_post, c);
+      t.load(a.w_post, 0, c);
       t.get(w);
       t.zero();
-      if (a.b_post) t.load(a.b_post, c);
+      if (a.b_post) t.load(a.b_post, 0, c);
       t.get(b);
 #pragma unroll
       for (int i = 0; i < PW; ++i) g[i] = a.scale;
       if (gate) {
-        t.load(gate, c);
+        t.load(gate, 0, c);
         t.get(g);
 #pragma unroll
         for (int i = 0; i < PW; ++i) g[i] *= a.scale;
       }
 #pragma unroll
       for (int i = 0; i < PW; ++i) x[k][i] += g[i] * (y[k][i] * r0 * w[i] + b[i]);
-      store8<false>(a.xo, r * a.ldx + c, x[k]);
+      store8<false>(a.xo, r * a.ldx, c, x[k]);
     }
   }
   if (a.w_pre) {
@@ -125,14 +129,14 @@ __global__ void __launch_bounds__(256) block_norm_fwd_kernel(zl_norm_args a) {
       if (c < a.d) {
         float w[PW], b[PW];
         Raw8<false> t;
-        t.load(a.w_pre, c);
+        t.load(a.w_pre, 0, c);
         t.get(w);
         t.zero();
-        if (a.b_pre) t.load(a.b_pre, c);
+        if (a.b_pre) t.load(a.b_pre, 0, c);
         t.get(b);
 #pragma unroll
         for (int i = 0; i < PW; ++i) o[i] = x[k][i] * r1 * w[i] + b[i];
-        store8<BO>(a.n, r * a.ldn + c, o);
+        store8<BO, NT>(a.n, r * a.ldn, c, o);
       }
       if (a.n_packed.codes) {
         if (BO)
@@ -144,23 +148,31 @@ __global__ void __launch_bounds__(256) block_norm_fwd_kernel(zl_norm_args a) {
           }
         uint32_t sb;
         const uint2 code = pack8(o, sb);
-        if (c < a.d) store_packed(a.n_packed, r, c, code, sb);
+        if (c < a.d) store_packed<NT>(a.n_packed, r, c, code, sb);
       }
     }
   }
   if (lane == 0) *reinterpret_cast<float4*>(a.stats + r * 4) = make_float4(m0, r0, m1, r1);
 }
 
+template <int NW, int G, bool NT>
+static void norm_fwd_types(const zl_norm_args& a, dim3 g, hipStream_t s) {
+  const dim3 b(256);
+  const bool bi = a.in_dtype == ZL_BF16, bo = a.out_dtype == ZL_BF16;
+  if (bi && bo) hipLaunchKernelGGL((block_norm_fwd_kernel<NW, G, true, true, NT>), g, b, 0, s, a);
+  else if (bi) hipLaunchKernelGGL((block_norm_fwd_kernel<NW, G, true, false, NT>), g, b, 0, s, a);
+  else if (bo) hipLaunchKernelGGL((block_norm_fwd_kernel<NW, G, false, true, NT>), g, b, 0, s, a);
+  else hipLaunchKernelGGL((block_norm_fwd_kernel<NW, G, false, false, NT>), g, b, 0, s, a);
+}
 template <int NW, int G>
 static hipError_t norm_fwd_go(const zl_norm_args& a, hipStream_t s) {
   const int64_t nb = (a.T + 4 / NW - 1) / (4 / NW);
   if (nb > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 g((unsigned)nb), b(256);
-  const bool bi = a.in_dtype == ZL_BF16, bo = a.out_dtype == ZL_BF16;
-  if (bi && bo) hipLaunchKernelGGL((block_norm_fwd_kernel<NW, G, true, true>), g, b, 0, s, a);
-  else if (bi) hipLaunchKernelGGL((block_norm_fwd_kernel<NW, G, true, false>), g, b, 0, s, a);
-  else if (bo) hipLaunchKernelGGL((block_norm_fwd_kernel<NW, G, false, true>), g, b, 0, s, a);
-  else hipLaunchKernelGGL((block_norm_fwd_kernel<NW, G, false, false>), g, b, 0, s, a);
+  // xo, n and the copies
+  const int64_t out = a.T * a.d * ((a.w_post ? 4 : 0) + (a.w_pre ? (a.out_dtype == ZL_BF16 ? 2 : 4) : 0) +
+                                   (a.y_packed.codes ? 1 : 0) + (a.n_packed.codes ? 1 : 0));
+  if (streaming(out, 0)) norm_fwd_types<NW, G, true>(a, dim3((unsigned)nb), s);
+  else norm_fwd_types<NW, G, false>(a, dim3((unsigned)nb), s);
   return hipGetLastError();
 }
 
@@ -179,197 +191,293 @@ hipError_t launch_block_norm(const zl_norm_args& a, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------- backward
-// A block per run of rows, 8 columns per thread; D = dL/dxo:
+// A block has slots of waves, each with rows of its own; a thread has G groups
+// of 8 columns.  Rows go round the slots of all blocks, so that what is read at
+// one time lies together (a run of rows per block, the runs a power of two apart:
+// 251 us at 16384 x 4096 where this took 237; 8192 x 2048: 72 and 67).  With D = dL/dxo:
 //   g = dn w_pre:  D = dxo + r1 (g - mean(g) - xh mean(g xh))   (mean(g): LayerNorm)
 //   dp = scale gate D, q = dp w_post:  dy = r0 (q - mean(q) - yh mean(q yh))
-// The parameters' sums over the block's rows stay in registers and go to
-// one partial row per block (no atomics); a second kernel adds those.
-// The next row is loaded while this one is reduced.  Rows of over 4096 columns
-// take 1024 threads, which leaves 128 registers each: LEAN reads the row when
-// it is due and the weights and the gate once per row (from the caches).
-// What the norm after the block sums needs the gate row only once for a run of
-// rows that share it: with S1 = sum D yh and S0 = sum D,
+// The parameters' sums over the block's rows stay in registers, meet across
+// slots in LDS and go to one partial row per block (no atomics); a second kernel
+// adds those.  What the norm after the block sums needs the gate row only once
+// for a run of rows that share it: with S1 = sum D yh and S0 = sum D,
 //   dgate = scale (w_post S1 + b_post S0),  dw_post = scale gate S1,  db_post = scale gate S0.
-// MULTI: a block has several gate rows (whole ones) and adds up the latter two.
+// MULTI: a slot has several gate rows (whole ones) and adds up the latter two.
+// The next row is loaded while this one is reduced; LEAN (registers short):
+// the row is read when it is due, weights and gate once per row (from the caches).
 template <bool BI, bool PK> struct RawY : Raw8<BI> {
-  __device__ __forceinline__ void fetch(const zl_norm_args& a, int64_t r, int c) { this->load(a.y, r * a.ldy + c); }
+  __device__ __forceinline__ void fetch(const zl_norm_args& a, int64_t r, uint32_t c) { this->load(a.y, r * a.ldy, c); }
 };
 template <bool BI> struct RawY<BI, true> : RawP {
-  __device__ __forceinline__ void fetch(const zl_norm_args& a, int64_t r, int c) { this->load(a.y_packed, r, c); }
+  __device__ __forceinline__ void fetch(const zl_norm_args& a, int64_t r, uint32_t c) { this->load(a.y_packed, r, c); }
 };
 
-template <int MAXT, bool LEAN, bool MULTI, bool LN, bool BI, bool PK>
-__global__ void __launch_bounds__(MAXT) block_norm_bwd_kernel(zl_norm_args a, NormPlan pl) {
-  __shared__ float red[2][2][MAXT / 64];
-  const int tid = threadIdx.x, c = tid * PW, nw = blockDim.x >> 6;
-  const bool ok = c < a.d, pre = a.w_pre != nullptr, post = a.w_post != nullptr;
-  int64_t r0, r1;
+template <int NT, int G, bool LEAN, bool MULTI, bool LN, bool BI, bool PK>
+__global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, NormPlan pl) {
+  constexpr int NW = NT / 64;
+  __shared__ float red[2][2][NW];
+  __shared__ float comb[G == 1 ? 3 * 64 * PW : 1];  // slots 1 ..: 3 of one wave or 1 of two
+  // LEAN and MULTI: the sums over gate rows, touched once per gate row, lie in LDS
+  constexpr bool SL = LEAN && MULTI;
+  __shared__ float sq[SL ? (LN ? 2 : 1) * G * PW * NT : 1];
+  // waves of a slot, this wave's slot and its place there
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = NW / pl.slots, slot = wave / nw, lane = threadIdx.x & 63;
+  const int tid = (wave - slot * nw) * 64 + lane, gs = nw * 64 * PW;  // columns of one group
+  const bool pre = a.w_pre != nullptr, post = a.w_post != nullptr;
+  uint32_t col[G];
+  bool ok[G];
+#pragma unroll
+  for (int k = 0; k < G; ++k) {
+    col[k] = k * gs + tid * PW;
+    ok[k] = (int)col[k] < a.d;
+  }
+  // this slot's first row, the end of what it shares, and the rows from a unit
+  // of `unit` rows (one gate row where MULTI) to this slot's next
+  const int64_t unit = MULTI ? a.gate_rows : 1;
+  int64_t r0, end, step;
   if (pl.group > 0) {
     const int64_t gi = blockIdx.x / pl.cpg, ci = blockIdx.x % pl.cpg;
-    r0 = gi * pl.group + ci * pl.rpb;
-    r1 = min(min(r0 + pl.rpb, (gi + 1) * pl.group), a.T);
+    r0 = gi * pl.group + ci * pl.slots + slot;
+    end = min((gi + 1) * pl.group, a.T);
+    step = pl.cpg * pl.slots;
   } else {
-    r0 = blockIdx.x * pl.rpb;
-    r1 = min(r0 + pl.rpb, a.T);
+    r0 = ((int64_t)blockIdx.x * pl.slots + slot) * unit;
+    end = a.T;
+    step = pl.nblk * pl.slots * unit;
   }
-  float wp[PW], wq[PW];  // w_pre, w_post
-  auto vec = [&](const float* p, float (&v)[PW]) __attribute__((always_inline)) {
+  auto vec = [&](const float* p, int k, float (&v)[PW]) __attribute__((always_inline)) {
     Raw8<false> t;
     t.zero();
-    if (ok && p) t.load(p, c);
+    if (ok[k] && p) t.load(p, 0, col[k]);
     t.get(v);
   };
-  if (!LEAN) {
-    vec(a.w_pre, wp);
-    vec(a.w_post, wq);
-  }
-  // gradient sums: the norm before the next block, S1 and S0, and MULTI's own
-  float swp[PW], sbp[PW], s1[PW], s0[PW], swq[PW], sbq[PW], gt[PW];
-#pragma unroll
-  for (int i = 0; i < PW; ++i) {
-    swp[i] = sbp[i] = s1[i] = s0[i] = swq[i] = sbq[i] = 0.f;
-    gt[i] = a.scale;
-  }
-  // scale * the gate row of r
+  float wp[G][PW], wq[G][PW], gt[G][PW];  // w_pre, w_post, scale * gate
+  // gradient sums: of the norm before the next block, S1 and S0, and MULTI's own
+  float swp[G][PW], sbp[G][PW], s1[G][PW], s0[G][PW], swq[G][PW], sbq[G][PW];
   auto load_gate = [&](int64_t r) __attribute__((always_inline)) {
-    vec(a.gate + r / a.gate_rows * a.d, gt);
 #pragma unroll
-    for (int i = 0; i < PW; ++i) gt[i] *= a.scale;
+    for (int k = 0; k < G; ++k) {
+      vec(a.gate + r / a.gate_rows * a.d, k, gt[k]);
+#pragma unroll
+      for (int i = 0; i < PW; ++i) gt[k][i] *= a.scale;
+    }
   };
-  if (!LEAN && !MULTI && a.gate && r0 < r1) load_gate(r0);
-  Raw8<false> nd, nx;
-  Raw8<BI> nn;
-  RawY<BI, PK> ny;
+#pragma unroll
+  for (int k = 0; k < G; ++k) {
+    if (!LEAN) {
+      vec(a.w_pre, k, wp[k]);
+      vec(a.w_post, k, wq[k]);
+    }
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+      swp[k][i] = sbp[k][i] = s1[k][i] = s0[k][i] = swq[k][i] = sbq[k][i] = 0.f;
+      gt[k][i] = a.scale;
+      if (SL) sq[(k * PW + i) * NT + threadIdx.x] = 0.f;
+      if (SL && LN) sq[((G + k) * PW + i) * NT + threadIdx.x] = 0.f;
+    }
+  }
+  if (!LEAN && !MULTI && a.gate && r0 < end) load_gate(r0);
+  Raw8<false> nd[G], nx[G];
+  Raw8<BI> nn[G];
+  RawY<BI, PK> ny[G];
   float4 nst;
   auto fetch = [&](int64_t r) __attribute__((always_inline)) {
-    nd.zero();
-    nx.zero();
-    nn.zero();
-    ny.zero();
     nst = *reinterpret_cast<const float4*>(a.stats + r * 4);
-    if (!ok) return;
-    if (a.dxo) nd.load(a.dxo, r * a.ldx + c);
-    if (pre) {
-      nx.load(a.xo, r * a.ldx + c);
-      nn.load(a.dn, r * a.ldn + c);
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+      if (!ok[k]) continue;
+      if (a.dxo) nd[k].load(a.dxo, r * a.ldx, col[k]);
+      if (pre) {
+        nx[k].load(a.xo, r * a.ldx, col[k]);
+        nn[k].load(a.dn, r * a.ldn, col[k]);
+      }
+      if (post) ny[k].fetch(a, r, col[k]);
     }
-    if (post) ny.fetch(a, r, c);
   };
+  nst = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < G; ++k) {
+    nd[k].zero();
+    nx[k].zero();
+    nn[k].zero();
+    ny[k].zero();
+  }
   int par = 0;
   auto sums = [&](float& u, float& v) __attribute__((always_inline)) {
     u = lanes_sum(u);
     if (LN) v = lanes_sum(v);
     if (nw == 1) return;
-    if ((tid & 63) == 0) {
-      red[par][0][tid >> 6] = u;
-      red[par][1][tid >> 6] = v;
+    if (lane == 0) {
+      red[par][0][wave] = u;
+      red[par][1][wave] = v;
     }
     __syncthreads();
-    u = v = 0.f;
-    for (int w = 0; w < nw; ++w) {
-      u += red[par][0][w];
-      v += red[par][1][w];
+    // lane l takes the sum of wave l % nw (nw is a power of two)
+    u = red[par][0][slot * nw + (lane & (nw - 1))];
+    v = LN ? red[par][1][slot * nw + (lane & (nw - 1))] : 0.f;
+    for (int o = 1; o < nw; o <<= 1) {
+      u += __shfl_xor(u, o, 64);
+      if (LN) v += __shfl_xor(v, o, 64);
     }
     par ^= 1;
   };
-  if (!LEAN && r0 < r1) fetch(r0);
-  int64_t left = 0;  // rows of the current gate row still to come in this block
-  for (int64_t r = r0; r < r1; ++r) {
-    if (LEAN) fetch(r);
-    float dv[PW], xv[PW], nv[PW], yv[PW];
-    nd.get(dv);
-    nx.get(xv);
-    nn.get(nv);
-    ny.get(yv);
+  if (!LEAN && r0 < end) fetch(r0);
+  int64_t r = r0, at_unit = 0;  // this round's row and its place in its unit
+  // every slot takes the same number of rounds (barriers); rows past the end count nothing
+  for (int64_t k0 = 0; k0 < pl.rows; ++k0) {
+    const bool in = r < end;
+    const bool last = MULTI ? at_unit + 1 == unit || r + 1 >= end : true;  // of its gate row
+    const int64_t next = MULTI && at_unit + 1 < unit ? r + 1 : r + step - (MULTI ? unit - 1 : 0);
+    if (LEAN && in) fetch(r);
+    Raw8<false> rd[G], rx[G];
+    Raw8<BI> rn[G];
+    RawY<BI, PK> ry[G];
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+      rd[k] = nd[k];
+      rx[k] = nx[k];
+      rn[k] = nn[k];
+      ry[k] = ny[k];
+    }
     const float4 st = nst;
-    if (!LEAN && r + 1 < r1) fetch(r + 1);
-    if (a.gate && (LEAN || (MULTI && left == 0))) load_gate(r);
-    if (MULTI && left == 0) left = min(a.gate_rows, r1 - r);
+    if (!LEAN && next < end) fetch(next);
+    if (in && a.gate && (LEAN || (MULTI && at_unit == 0))) load_gate(r);
+    float dv[G][PW];
+#pragma unroll
+    for (int k = 0; k < G; ++k) rd[k].get(dv[k]);
     if (pre) {
-      if (LEAN) vec(a.w_pre, wp);
-      float u = 0.f, v = 0.f, g[PW];
+      float u = 0.f, v = 0.f, g[G][PW], xv[G][PW];
 #pragma unroll
-      for (int i = 0; i < PW; ++i) {
-        xv[i] = (xv[i] - st.z) * st.w;
-        g[i] = nv[i] * wp[i];
-        u += g[i] * xv[i];
-        v += g[i];
-        swp[i] += nv[i] * xv[i];
-        if (LN) sbp[i] += nv[i];
+      for (int k = 0; k < G; ++k) {
+        float nv[PW];
+        if (LEAN) vec(a.w_pre, k, wp[k]);
+        rx[k].get(xv[k]);
+        rn[k].get(nv);
+#pragma unroll
+        for (int i = 0; i < PW; ++i) {
+          xv[k][i] = (xv[k][i] - st.z) * st.w;
+          g[k][i] = nv[i] * wp[k][i];
+          u += g[k][i] * xv[k][i];
+          v += g[k][i];
+          if (in) {
+            swp[k][i] += nv[i] * xv[k][i];
+            if (LN) sbp[k][i] += nv[i];
+          }
+        }
       }
       sums(u, v);
       u /= a.d;
       v = LN ? v / a.d : 0.f;
 #pragma unroll
-      for (int i = 0; i < PW; ++i) dv[i] += st.w * (g[i] - v - xv[i] * u);
+      for (int k = 0; k < G; ++k)
+#pragma unroll
+        for (int i = 0; i < PW; ++i) dv[k][i] += st.w * (g[k][i] - v - xv[k][i] * u);
     }
-    if (ok) store8<false>(a.dx, r * a.ldx + c, dv);
+#pragma unroll
+    for (int k = 0; k < G; ++k)
+      if (in && ok[k]) store8<false>(a.dx, r * a.ldx, col[k], dv[k]);
     if (post) {
-      if (LEAN) vec(a.w_post, wq);
-      float u = 0.f, v = 0.f, q[PW];
+      float u = 0.f, v = 0.f, q[G][PW], yv[G][PW];
 #pragma unroll
-      for (int i = 0; i < PW; ++i) {
-        yv[i] = (yv[i] - st.x) * st.y;
-        const float dp = gt[i] * dv[i];
-        q[i] = dp * wq[i];
-        u += q[i] * yv[i];
-        v += q[i];
-        s1[i] += dv[i] * yv[i];
-        if (LN) s0[i] += dv[i];
+      for (int k = 0; k < G; ++k) {
+        if (LEAN) vec(a.w_post, k, wq[k]);
+        ry[k].get(yv[k]);
+#pragma unroll
+        for (int i = 0; i < PW; ++i) {
+          yv[k][i] = (yv[k][i] - st.x) * st.y;
+          q[k][i] = gt[k][i] * dv[k][i] * wq[k][i];
+          u += q[k][i] * yv[k][i];
+          v += q[k][i];
+          if (in) {
+            s1[k][i] += dv[k][i] * yv[k][i];
+            if (LN) s0[k][i] += dv[k][i];
+          }
+        }
       }
       sums(u, v);
       u /= a.d;
       v = LN ? v / a.d : 0.f;
 #pragma unroll
-      for (int i = 0; i < PW; ++i) q[i] = st.y * (q[i] - v - yv[i] * u);
-      if (ok) {
-        if (a.out_dtype == ZL_BF16) store8<true>(a.dy, r * a.ldy + c, q);
-        else store8<false>(a.dy, r * a.ldy + c, q);
+      for (int k = 0; k < G; ++k) {
+#pragma unroll
+        for (int i = 0; i < PW; ++i) q[k][i] = st.y * (q[k][i] - v - yv[k][i] * u);
+        if (in && ok[k]) {
+          if (a.out_dtype == ZL_BF16) store8<true>(a.dy, r * a.ldy, col[k], q[k]);
+          else store8<false>(a.dy, r * a.ldy, col[k], q[k]);
+        }
       }
     }
-    if (MULTI && post && --left == 0) {  // all rows of this gate row were this block's
-      if (a.dgate && ok) {
-        const int64_t o = r / a.gate_rows * a.d + c;
-        float t[PW], w[PW], b[PW];
-        vec(a.accumulate ? a.dgate + (o - c) : nullptr, t);
-        vec(a.w_post, w);
-        vec(LN ? a.b_post : nullptr, b);
+    if (MULTI && in && last) {
+      const int64_t o = r / a.gate_rows * a.d;
 #pragma unroll
-        for (int i = 0; i < PW; ++i) t[i] += a.grad_scale * a.scale * (w[i] * s1[i] + b[i] * s0[i]);
-        store8<false>(a.dgate, o, t);
-      }
+      for (int k = 0; k < G; ++k) {
+        if (a.dgate && ok[k]) {
+          float t[PW], w[PW], b[PW];
+          vec(a.accumulate ? a.dgate + o : nullptr, k, t);
+          vec(a.w_post, k, w);
+          vec(LN ? a.b_post : nullptr, k, b);
 #pragma unroll
-      for (int i = 0; i < PW; ++i) {
-        swq[i] += gt[i] * s1[i];
-        if (LN) sbq[i] += gt[i] * s0[i];
-        s1[i] = s0[i] = 0.f;
+          for (int i = 0; i < PW; ++i) t[i] += a.grad_scale * a.scale * (w[i] * s1[k][i] + b[i] * s0[k][i]);
+          store8<false>(a.dgate, o, col[k], t);
+        }
+#pragma unroll
+        for (int i = 0; i < PW; ++i) {
+          if (SL) {
+            sq[(k * PW + i) * NT + threadIdx.x] += gt[k][i] * s1[k][i];
+            if (LN) sq[((G + k) * PW + i) * NT + threadIdx.x] += gt[k][i] * s0[k][i];
+          } else {
+            swq[k][i] += gt[k][i] * s1[k][i];
+            if (LN) sbq[k][i] += gt[k][i] * s0[k][i];
+          }
+          s1[k][i] = s0[k][i] = 0.f;
+        }
       }
     }
+    if (MULTI) at_unit = at_unit + 1 < unit ? at_unit + 1 : 0;
+    r = next;
   }
-  if (!ok) return;
-  float* part = a.workspace + blockIdx.x * (int64_t)a.d + c;
-  const int64_t step = pl.nblk * a.d;
-  if (a.dw_pre) store8<false>(part, 0, swp);
-  if (LN && a.db_pre) store8<false>(part, step, sbp);
-  if (!post) return;
-  if (!MULTI) {
-    if (LEAN && a.gate && r0 < r1) load_gate(r0);
-    if (a.dgate) {
-      float w[PW], b[PW], t[PW];
-      vec(a.w_post, w);
-      vec(LN ? a.b_post : nullptr, b);
+  // the slots' sums, then this block's partial row `which`
+  auto finish = [&](int which, int k, float (&v)[PW]) __attribute__((always_inline)) {
+    if (G == 1 && pl.slots > 1) {
+      __syncthreads();
+      if (slot > 0)
 #pragma unroll
-      for (int i = 0; i < PW; ++i) t[i] = a.scale * (w[i] * s1[i] + b[i] * s0[i]);
-      store8<false>(part, 4 * step, t);
+        for (int i = 0; i < PW; ++i) comb[((slot - 1) * PW + i) * nw * 64 + tid] = v[i];
+      __syncthreads();
+      if (slot > 0) return;
+      for (int t = 1; t < pl.slots; ++t)
+#pragma unroll
+        for (int i = 0; i < PW; ++i) v[i] += comb[((t - 1) * PW + i) * nw * 64 + tid];
     }
+    if (ok[k]) store8<false>(a.workspace, (which * pl.nblk + blockIdx.x) * a.d, col[k], v);
+  };
+  if (!MULTI && LEAN && a.gate && r0 < end) load_gate(r0);
+#pragma unroll
+  for (int k = 0; k < G; ++k) {
+    if (a.dw_pre) finish(0, k, swp[k]);
+    if (LN && a.db_pre) finish(1, k, sbp[k]);
+    if (!post) continue;
 #pragma unroll
     for (int i = 0; i < PW; ++i) {
-      swq[i] = gt[i] * s1[i];
-      sbq[i] = gt[i] * s0[i];
+      if (!MULTI) {
+        swq[k][i] = gt[k][i] * s1[k][i];
+        sbq[k][i] = gt[k][i] * s0[k][i];
+      } else if (SL) {
+        swq[k][i] = sq[(k * PW + i) * NT + threadIdx.x];
+        if (LN) sbq[k][i] = sq[((G + k) * PW + i) * NT + threadIdx.x];
+      }
+    }
+    if (a.dw_post) finish(2, k, swq[k]);
+    if (LN && a.db_post) finish(3, k, sbq[k]);
+    if (!MULTI && a.dgate) {
+      float w[PW], b[PW], t[PW];
+      vec(a.w_post, k, w);
+      vec(LN ? a.b_post : nullptr, k, b);
+#pragma unroll
+      for (int i = 0; i < PW; ++i) t[i] = a.scale * (w[i] * s1[k][i] + b[i] * s0[k][i]);
+      finish(4, k, t);
     }
   }
-  if (a.dw_post) store8<false>(part, 2 * step, swq);
-  if (LN && a.db_post) store8<false>(part, 3 * step, sbq);
 }
 
 // out = (accumulate ? out : 0) + scale * sum of partial rows, in a fixed order:
@@ -411,47 +519,49 @@ __global__ void __launch_bounds__(1024) block_norm_reduce_kernel(zl_norm_args a,
 }
 
 NormPlan norm_plan(int64_t T, int d, int64_t gate_rows) {
-  if (T <= 0) return {0, 0, 0, 0};
-  // four waves per SIMD, but not below 8 rows a block (partial rows cost what
-  // rows cost) until there are fewer blocks than CUs
-  const int waves = (d + 64 * PW - 1) / (64 * PW);
-  int64_t blocks = 256 * 16 / waves;
-  if (blocks > 1024) blocks = 1024;
+  if (T <= 0) return {0, 0, 0, 0, 1};
+  // rows of up to 512 columns: a wave each, four in a block, and so on
+  const int slots = d <= 64 * PW ? 4 : d <= 128 * PW ? 2 : 1;
+  // as many blocks as are resident, with 8 rows each at least (partial rows cost
+  // what two rows cost) until there are fewer blocks than CUs
+  int64_t blocks = 256 * (d <= 256 * PW ? 3 : d <= 512 * PW ? 2 : 1);
   if (blocks > T / 8) blocks = T / 8;
-  if (blocks < 256) blocks = T < 256 ? T : 256;
-  NormPlan p = {0, (T + blocks - 1) / blocks, 0, 0};
+  const int64_t most = (T + slots - 1) / slots;
+  if (blocks < 256) blocks = most < 256 ? most : 256;
+  NormPlan p = {0, (T + blocks * slots - 1) / (blocks * slots), 0, 0, slots};
   if (gate_rows > T) gate_rows = T;
-  if (gate_rows >= p.rpb) {
+  if (gate_rows >= p.rows * slots) {
     p.group = gate_rows;
-    p.cpg = (gate_rows + p.rpb - 1) / p.rpb;
-    p.rpb = (gate_rows + p.cpg - 1) / p.cpg;
+    p.cpg = (gate_rows + p.rows * slots - 1) / (p.rows * slots);
+    p.rows = (gate_rows + p.cpg * slots - 1) / (p.cpg * slots);
     p.nblk = (T + gate_rows - 1) / gate_rows * p.cpg;
   } else {
-    if (gate_rows > 0) p.rpb = p.rpb / gate_rows * gate_rows;
-    p.nblk = (T + p.rpb - 1) / p.rpb;
+    if (gate_rows > 0) p.rows = p.rows > gate_rows ? p.rows / gate_rows * gate_rows : gate_rows;
+    p.nblk = (T + p.rows * slots - 1) / (p.rows * slots);
   }
   return p;
 }
 
-template <int MAXT, bool LEAN, bool MULTI, bool LN>
-static void norm_bwd_types(const zl_norm_args& a, const NormPlan& pl, int threads, hipStream_t s) {
-  const dim3 g((unsigned)pl.nblk), b(threads);
+template <int NT, int G, bool LEAN, bool MULTI, bool LN>
+static void norm_bwd_types(const zl_norm_args& a, const NormPlan& pl, hipStream_t s) {
+  const dim3 g((unsigned)pl.nblk), b(NT);
   const bool bi = a.in_dtype == ZL_BF16, pk = a.w_post && a.y_packed.codes;
-  if (bi && pk) hipLaunchKernelGGL((block_norm_bwd_kernel<MAXT, LEAN, MULTI, LN, true, true>), g, b, 0, s, a, pl);
-  else if (bi) hipLaunchKernelGGL((block_norm_bwd_kernel<MAXT, LEAN, MULTI, LN, true, false>), g, b, 0, s, a, pl);
-  else if (pk) hipLaunchKernelGGL((block_norm_bwd_kernel<MAXT, LEAN, MULTI, LN, false, true>), g, b, 0, s, a, pl);
-  else hipLaunchKernelGGL((block_norm_bwd_kernel<MAXT, LEAN, MULTI, LN, false, false>), g, b, 0, s, a, pl);
+  constexpr bool L32 = LEAN || G == 2;  // fp32 dn and y: twice the registers of a row in flight
+  if (bi && pk) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MULTI, LN, true, true>), g, b, 0, s, a, pl);
+  else if (bi) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MULTI, LN, true, false>), g, b, 0, s, a, pl);
+  else if (pk) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MULTI, LN, false, true>), g, b, 0, s, a, pl);
+  else hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, L32, MULTI, LN, false, false>), g, b, 0, s, a, pl);
 }
 
-template <int MAXT, bool LEAN>
-static void norm_bwd_go(const zl_norm_args& a, const NormPlan& pl, int threads, hipStream_t s) {
+template <int NT, int G>
+static void norm_bwd_go(const zl_norm_args& a, const NormPlan& pl, hipStream_t s) {
   const bool multi = a.gate && a.w_post && pl.group == 0;
   if (a.layernorm) {
-    if (multi) norm_bwd_types<MAXT, LEAN, true, true>(a, pl, threads, s);
-    else norm_bwd_types<MAXT, LEAN, false, true>(a, pl, threads, s);
+    if (multi) norm_bwd_types<NT, G, G == 2, true, true>(a, pl, s);
+    else norm_bwd_types<NT, G, G == 2, false, true>(a, pl, s);
   } else {
-    if (multi) norm_bwd_types<MAXT, LEAN, true, false>(a, pl, threads, s);
-    else norm_bwd_types<MAXT, LEAN, false, false>(a, pl, threads, s);
+    if (multi) norm_bwd_types<NT, G, G == 2, true, false>(a, pl, s);
+    else norm_bwd_types<NT, G, false, false, false>(a, pl, s);
   }
 }
 
@@ -465,10 +575,12 @@ hipError_t launch_block_norm_bwd(const zl_norm_args& a, hipStream_t s) {
   }
   const NormPlan pl = norm_plan(a.T, a.d, a.gate ? a.gate_rows : 0);
   if (pl.nblk > 0x7fffffff) return hipErrorInvalidValue;
-  const int threads = (a.d + 64 * PW - 1) / (64 * PW) * 64;
-  if (threads <= 256) norm_bwd_go<256, false>(a, pl, threads, s);
-  else if (threads <= 512) norm_bwd_go<512, false>(a, pl, threads, s);
-  else norm_bwd_go<1024, true>(a, pl, threads, s);
+  // 8 columns a thread up to 4096 (16 on half the threads: 237 us at 16384 x 4096
+  // where this takes 223), 16 above (8 on 1024 threads, registers short: 150 us at
+  // 4096 x 8192 where this takes 134)
+  if (a.d <= 256 * PW) norm_bwd_go<256, 1>(a, pl, s);
+  else if (a.d <= 512 * PW) norm_bwd_go<512, 1>(a, pl, s);
+  else norm_bwd_go<512, 2>(a, pl, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const bool gate = a.dgate && pl.group > 0;

@@ -7,6 +7,10 @@
 
 namespace zl {
 
+// 0, 1 (stores) or 2 (loads too): which accesses of a call with so many bytes of
+// output and input stream past the caches.
+int streaming(int64_t out, int64_t in);
+
 hipError_t launch_pack(int64_t T, int n, const void* x, int64_t ldx, int dtype, const zl_packed& out,
                        hipStream_t s);
 hipError_t launch_unpack(int64_t T, int n, const zl_packed& in, void* x, int64_t ldx, int dtype,
@@ -15,11 +19,13 @@ hipError_t launch_unpack(int64_t T, int n, const zl_packed& in, void* x, int64_t
 hipError_t launch_mlp(const zl_mlp_args& a, bool backward, hipStream_t s);
 
 hipError_t launch_block_norm(const zl_norm_args& a, hipStream_t s);
-// How the backward's blocks take the rows: nblk blocks; group = 0: block i
-// has rows [i rpb, (i + 1) rpb), rpb a multiple of the gate's rows; group > 0:
-// every run of `group` rows (one gate row) has cpg blocks of rpb rows each.
+// How the backward's blocks take the rows: nblk blocks of `slots` slots; every
+// slot has up to `rows` rows, each slot in turn one of them.  group > 0: every
+// `group` rows (one gate row) have cpg blocks of their own; else, with a gate, a
+// turn is the rows of one gate row, and `rows` a multiple of them.
 struct NormPlan {
-  int64_t nblk, rpb, group, cpg;
+  int64_t nblk, rows, group, cpg;
+  int slots;
 };
 NormPlan norm_plan(int64_t T, int d, int64_t gate_rows);
 hipError_t launch_block_norm_bwd(const zl_norm_args& a, hipStream_t s);

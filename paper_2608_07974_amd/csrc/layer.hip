@@ -12,7 +12,9 @@ constexpr int LT = 256;  // threads per block
 
 // Columns to lanes, rows to blocks: a row takes 2^l2 lanes of 8 columns each
 // (whole 32-column blocks), ncx column chunks of them where it is longer; a
-// block has LT / 2^l2 rows at once, U times.
+// block has LT / 2^l2 rows at once, U times.  (Shorter chunks where many
+// lanes lie past the row measured slower: pack and unpack of 8192 x 1544 15.9 us,
+// in chunks of 256 columns 20.4.)
 struct RowGrid {
   int l2, ncx;
   int64_t T;
@@ -40,9 +42,17 @@ struct RowPos {
   __device__ __forceinline__ int64_t row(int u) const { return r0 + (int64_t)u * step; }
 };
 
+// How a call's accesses stream past the caches (NT of the kernels): 1, the stores,
+// where the outputs are larger than the L2s (32 MB) and so leave them before
+// the next kernel reads them; 2, the loads too, where the inputs are larger by far
+// than the Infinity Cache (256 MB).  SwiGLU 16384 x 14336 forward 337, 325, 306 us for
+// 0, 1, 2, backward 398, 380, 383; GELU 4096 x 3200 backward 22.5, 19.0, 20.7; pack
+// and unpack 4096 x 4096 (16 MB of codes) 17.7, 19.1, 20.1.
+int streaming(int64_t out, int64_t in) { return out <= (32 << 20) ? 0 : in <= (384 << 20) ? 1 : 2; }
+
 // ------------------------------------------------------------ pack, unpack
 // All loads of the U rows are in flight before the first is used.
-template <bool BF, int U>
+template <bool BF, int U, int NT>
 __global__ void __launch_bounds__(LT) pack_kernel(RowGrid g, int n, const void* __restrict__ x, int64_t ldx,
                                                   zl_packed out) {
   const RowPos p(g, U);
@@ -50,7 +60,7 @@ __global__ void __launch_bounds__(LT) pack_kernel(RowGrid g, int n, const void* 
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     raw[u].zero();
-    if (p.col < n && p.row(u) < g.T) raw[u].load(x, p.row(u) * ldx + p.col);
+    if (p.col < n && p.row(u) < g.T) raw[u].template load<(NT > 1)>(x, p.row(u) * ldx + p.col);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -58,11 +68,11 @@ __global__ void __launch_bounds__(LT) pack_kernel(RowGrid g, int n, const void* 
     uint32_t sb;
     raw[u].get(v);
     const uint2 c = pack8(v, sb);  // every lane of a block, also past the row's end
-    if (p.col < n && p.row(u) < g.T) store_packed(out, p.row(u), p.col, c, sb);
+    if (p.col < n && p.row(u) < g.T) store_packed<(NT > 0)>(out, p.row(u), p.col, c, sb);
   }
 }
 
-template <bool BF, int U>
+template <bool BF, int U, bool NT>
 __global__ void __launch_bounds__(LT) unpack_kernel(RowGrid g, int n, zl_packed in, void* __restrict__ x,
                                                     int64_t ldx) {
   const RowPos p(g, U);
@@ -78,7 +88,7 @@ __global__ void __launch_bounds__(LT) unpack_kernel(RowGrid g, int n, zl_packed 
     if (p.row(u) >= g.T) break;
     float v[PW];
     raw[u].get(v);
-    store8<BF>(x, p.row(u) * ldx + p.col, v);
+    store8<BF, NT>(x, p.row(u) * ldx + p.col, 0, v);
   }
 }
 
@@ -86,23 +96,29 @@ __global__ void __launch_bounds__(LT) unpack_kernel(RowGrid g, int n, zl_packed 
 // rows: latency counts), else U rows in flight.
 static bool few(const RowGrid& g) { return row_blocks(g, 1) <= 1024; }
 
-template <typename F1, typename FU>
-static hipError_t launch_rows(const RowGrid& g, int U, F1 one, FU many) {
+// f(blocks, U, NT) with compile-time U and NT: U rows per thread where there are
+// many, and streaming accesses only there.
+template <int N> using Int = std::integral_constant<int, N>;
+template <int U, typename F>
+static hipError_t launch_rows(const RowGrid& g, int nt, F&& f) {
   if (g.T <= 0) return hipSuccess;
-  const bool f = few(g);
-  const int64_t b = row_blocks(g, f ? 1 : U);
+  const bool one = few(g);
+  const int64_t b = row_blocks(g, one ? 1 : U);
   if (b > 0x7fffffff) return hipErrorInvalidValue;
-  if (f) one(dim3((unsigned)b));
-  else many(dim3((unsigned)b));
+  const dim3 grid((unsigned)b);
+  if (one) f(grid, Int<1>{}, Int<0>{});
+  else if (nt == 0) f(grid, Int<U>{}, Int<0>{});
+  else if (nt == 1) f(grid, Int<U>{}, Int<1>{});
+  else f(grid, Int<U>{}, Int<2>{});
   return hipGetLastError();
 }
 
 template <bool BF>
 static hipError_t pack_go(int64_t T, int n, const void* x, int64_t ldx, const zl_packed& out, hipStream_t s) {
   const RowGrid g = row_grid(T, n);
-  return launch_rows(g, 4,
-                     [&](dim3 b) { hipLaunchKernelGGL((pack_kernel<BF, 1>), b, dim3(LT), 0, s, g, n, x, ldx, out); },
-                     [&](dim3 b) { hipLaunchKernelGGL((pack_kernel<BF, 4>), b, dim3(LT), 0, s, g, n, x, ldx, out); });
+  return launch_rows<4>(g, streaming(T * n, T * n * (BF ? 2 : 4)), [&](dim3 b, auto u, auto nt) {
+    hipLaunchKernelGGL((pack_kernel<BF, u(), nt()>), b, dim3(LT), 0, s, g, n, x, ldx, out);
+  });
 }
 hipError_t launch_pack(int64_t T, int n, const void* x, int64_t ldx, int dtype, const zl_packed& out, hipStream_t s) {
   return dtype == BF16 ? pack_go<true>(T, n, x, ldx, out, s) : pack_go<false>(T, n, x, ldx, out, s);
@@ -111,9 +127,9 @@ hipError_t launch_pack(int64_t T, int n, const void* x, int64_t ldx, int dtype, 
 template <bool BF>
 static hipError_t unpack_go(int64_t T, int n, const zl_packed& in, void* x, int64_t ldx, hipStream_t s) {
   const RowGrid g = row_grid(T, n);
-  return launch_rows(g, 4,
-                     [&](dim3 b) { hipLaunchKernelGGL((unpack_kernel<BF, 1>), b, dim3(LT), 0, s, g, n, in, x, ldx); },
-                     [&](dim3 b) { hipLaunchKernelGGL((unpack_kernel<BF, 4>), b, dim3(LT), 0, s, g, n, in, x, ldx); });
+  return launch_rows<4>(g, streaming(T * n * (BF ? 2 : 4), 0), [&](dim3 b, auto u, auto nt) {
+    hipLaunchKernelGGL((unpack_kernel<BF, u(), (nt() > 0)>), b, dim3(LT), 0, s, g, n, in, x, ldx);
+  });
 }
 hipError_t launch_unpack(int64_t T, int n, const zl_packed& in, void* x, int64_t ldx, int dtype, hipStream_t s) {
   return dtype == BF16 ? unpack_go<true>(T, n, in, x, ldx, s) : unpack_go<false>(T, n, in, x, ldx, s);
@@ -123,7 +139,7 @@ hipError_t launch_unpack(int64_t T, int n, const zl_packed& in, void* x, int64_t
 __device__ __forceinline__ float sigmoid_f(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
 
 // SW: gate | up, lane columns col and ff + col; else GELU.  PK: also packs h.
-template <bool SW, bool PK, bool BI, bool BO, int U>
+template <bool SW, bool PK, bool BI, bool BO, int U, int NT>
 __global__ void __launch_bounds__(LT) mlp_fwd_kernel(RowGrid g, zl_mlp_args a) {
   const RowPos p(g, U);
   Raw8<BI> rg[U], ru[SW ? U : 1];
@@ -131,10 +147,10 @@ __global__ void __launch_bounds__(LT) mlp_fwd_kernel(RowGrid g, zl_mlp_args a) {
   for (int u = 0; u < U; ++u) {
     const bool ok = p.col < a.ff && p.row(u) < g.T;
     rg[u].zero();
-    if (ok) rg[u].load(a.h, p.row(u) * a.ldh + p.col);
+    if (ok) rg[u].template load<(NT > 1)>(a.h, p.row(u) * a.ldh + p.col);
     if constexpr (SW) {
       ru[u].zero();
-      if (ok) ru[u].load(a.h, p.row(u) * a.ldh + a.ff + p.col);
+      if (ok) ru[u].template load<(NT > 1)>(a.h, p.row(u) * a.ldh + a.ff + p.col);
     }
   }
 #pragma unroll
@@ -146,14 +162,14 @@ __global__ void __launch_bounds__(LT) mlp_fwd_kernel(RowGrid g, zl_mlp_args a) {
     if constexpr (SW) ru[u].get(y);
 #pragma unroll
     for (int k = 0; k < PW; ++k) o[k] = SW ? x[k] * sigmoid_f(x[k]) * y[k] : gelu_f(x[k]);
-    if (ok) store8<BO>(a.a, r * a.lda + p.col, o);
+    if (ok) store8<BO, (NT > 0)>(a.a, r * a.lda + p.col, 0, o);
     if constexpr (PK) {
       uint32_t sb;
       uint2 c = pack8(x, sb);
-      if (ok) store_packed(a.packed, r, p.col, c, sb);
+      if (ok) store_packed<(NT > 0)>(a.packed, r, p.col, c, sb);
       if constexpr (SW) {
         c = pack8(y, sb);
-        if (ok) store_packed(a.packed, r, a.ff + p.col, c, sb);
+        if (ok) store_packed<(NT > 0)>(a.packed, r, a.ff + p.col, c, sb);
       }
     }
   }
@@ -167,7 +183,7 @@ template <bool BI> struct RawH<BI, true> : RawP {
   __device__ __forceinline__ void fetch(const zl_mlp_args& a, int64_t r, int col) { this->load(a.packed, r, col); }
 };
 
-template <bool SW, bool PK, bool BI, bool BO, int U>
+template <bool SW, bool PK, bool BI, bool BO, int U, int NT>
 __global__ void __launch_bounds__(LT) mlp_bwd_kernel(RowGrid g, zl_mlp_args a) {
   const RowPos p(g, U);
   if (p.col >= a.ff) return;
@@ -201,7 +217,7 @@ __global__ void __launch_bounds__(LT) mlp_bwd_kernel(RowGrid g, zl_mlp_args a) {
         dg[k] = d[k] * y[k] * (s * (1.f + x[k] * (1.f - s)));
         du[k] = d[k] * silu;
       }
-      store8<BO>(a.dh, r * a.lddh + a.ff + p.col, du);
+      store8<BO, (NT > 0)>(a.dh, r * a.lddh + a.ff + p.col, 0, du);
     } else {
 #pragma unroll
       for (int k = 0; k < PW; ++k) {
@@ -209,21 +225,23 @@ __global__ void __launch_bounds__(LT) mlp_bwd_kernel(RowGrid g, zl_mlp_args a) {
         dg[k] = d[k] * gelu_grad_f(x[k]);
       }
     }
-    store8<BO>(a.dh, r * a.lddh + p.col, dg);
-    if (a.a) store8<BO>(a.a, r * a.lda + p.col, o);
+    store8<BO, (NT > 0)>(a.dh, r * a.lddh + p.col, 0, dg);
+    if (a.a) store8<BO, (NT > 0)>(a.a, r * a.lda + p.col, 0, o);
   }
 }
 
 template <bool SW, bool PK, bool BI, bool BO>
 static hipError_t mlp_go(const zl_mlp_args& a, bool backward, hipStream_t s) {
   const RowGrid g = row_grid(a.T, a.ff);
-  if (backward)
-    return launch_rows(g, 2,
-                       [&](dim3 b) { hipLaunchKernelGGL((mlp_bwd_kernel<SW, PK, BI, BO, 1>), b, dim3(LT), 0, s, g, a); },
-                       [&](dim3 b) { hipLaunchKernelGGL((mlp_bwd_kernel<SW, PK, BI, BO, 2>), b, dim3(LT), 0, s, g, a); });
-  return launch_rows(g, 2,
-                     [&](dim3 b) { hipLaunchKernelGGL((mlp_fwd_kernel<SW, PK, BI, BO, 1>), b, dim3(LT), 0, s, g, a); },
-                     [&](dim3 b) { hipLaunchKernelGGL((mlp_fwd_kernel<SW, PK, BI, BO, 2>), b, dim3(LT), 0, s, g, a); });
+  const int64_t n = a.T * a.ff, nh = (SW ? 2 : 1) * n;
+  const int64_t ei = BI ? 2 : 4, eo = BO ? 2 : 4;
+  if (backward)  // loads that stream gained nothing here
+    return launch_rows<2>(g, streaming(nh * eo + (a.a ? n * eo : 0), 0), [&](dim3 b, auto u, auto nt) {
+      hipLaunchKernelGGL((mlp_bwd_kernel<SW, PK, BI, BO, u(), (nt() > 0)>), b, dim3(LT), 0, s, g, a);
+    });
+  return launch_rows<2>(g, streaming(n * eo + (PK ? nh : 0), nh * ei), [&](dim3 b, auto u, auto nt) {
+    hipLaunchKernelGGL((mlp_fwd_kernel<SW, PK, BI, BO, u(), nt()>), b, dim3(LT), 0, s, g, a);
+  });
 }
 template <bool SW, bool PK>
 static hipError_t mlp_types(const zl_mlp_args& a, bool backward, hipStream_t s) {
@@ -254,14 +272,14 @@ __device__ __forceinline__ void load_cols(const void* p, int64_t i, float (&v)[V
     v[0] = BF ? bf16_to_f32(static_cast<const bf16_t*>(p)[i]) : static_cast<const float*>(p)[i];
   }
 }
-template <bool BF, int V>
+template <bool BF, int V, bool NT>
 __device__ __forceinline__ void store_cols(void* p, int64_t i, const float (&v)[V]) {
-  if constexpr (V == PW) store8<BF>(p, i, v);
+  if constexpr (V == PW) store8<BF, NT>(p, i, 0, v);
   else if (BF) static_cast<bf16_t*>(p)[i] = f32_to_bf16(v[0]);
   else static_cast<float*>(p)[i] = v[0];
 }
 
-template <bool BF, int V>
+template <bool BF, int V, bool NT>
 __global__ void __launch_bounds__(LT) rotary_kernel(RotaryArgs a, int tb, int hpb) {
   __shared__ __align__(16) float cs[LT], sn[LT];
   const int64_t t0 = (int64_t)blockIdx.x * tb;
@@ -292,8 +310,8 @@ __global__ void __launch_bounds__(LT) rotary_kernel(RotaryArgs a, int tb, int hp
       p[k] = x[k] * c - y[k] * s;
       r[k] = y[k] * c + x[k] * s;
     }
-    store_cols<BF, V>(a.out, oi, p);
-    store_cols<BF, V>(a.out, oi + a.half, r);
+    store_cols<BF, V, NT>(a.out, oi, p);
+    store_cols<BF, V, NT>(a.out, oi + a.half, r);
   }
   const int rest = a.hd - 2 * a.half;
   if (rest == 0 || (a.out == a.x && a.ldo == a.ldx)) return;
@@ -303,7 +321,7 @@ __global__ void __launch_bounds__(LT) rotary_kernel(RotaryArgs a, int tb, int hp
     const int64_t col = (int64_t)(h0 + h) * a.hd + 2 * a.half + (q - h * rper) * V;
     float x[V];
     load_cols<BF, V>(a.x, (t0 + t) * a.ldx + col, x);
-    store_cols<BF, V>(a.out, (t0 + t) * a.ldo + col, x);
+    store_cols<BF, V, NT>(a.out, (t0 + t) * a.ldo + col, x);
   }
 }
 
@@ -317,7 +335,11 @@ static hipError_t rotary_go(const RotaryArgs& a, hipStream_t s) {
   int by = 1;
   while (bx * by < 512 && by < a.heads && (int64_t)tb * (a.heads / (2 * by)) * (a.half / V) >= LT) by *= 2;
   const int hpb = (a.heads + by - 1) / by;
-  hipLaunchKernelGGL((rotary_kernel<BF, V>), dim3((unsigned)bx, (a.heads + hpb - 1) / hpb), dim3(LT), 0, s, a, tb, hpb);
+  const dim3 grid((unsigned)bx, (a.heads + hpb - 1) / hpb);
+  // whole lines: halves of 128 bytes and more, no columns left over
+  const bool nt = BF && V == PW && a.half >= 64 && a.hd == 2 * a.half && streaming(a.T * a.heads * a.hd * 2, 0) > 0;
+  if (nt) hipLaunchKernelGGL((rotary_kernel<BF, V, BF && V == PW>), grid, dim3(LT), 0, s, a, tb, hpb);
+  else hipLaunchKernelGGL((rotary_kernel<BF, V, false>), grid, dim3(LT), 0, s, a, tb, hpb);
   return hipGetLastError();
 }
 hipError_t launch_rotary(const RotaryArgs& a, int dtype, hipStream_t s) {

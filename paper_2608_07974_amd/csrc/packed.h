@@ -75,13 +75,29 @@ __device__ __forceinline__ void unpack8(const uint2 c, const uint32_t sb, float 
 }
 
 // 8 consecutive elements of an fp32 or bf16 row as they lie in memory (16-byte
-// aligned), and as numbers.
+// aligned), and as numbers.  Element i + c: where i is the same for all lanes,
+// the address is a scalar base and a 32-bit lane offset.
+template <typename T>
+__device__ __forceinline__ const T* at(const void* p, int64_t byte, uint32_t lane_byte) {
+  return reinterpret_cast<const T*>(static_cast<const char*>(p) + byte + lane_byte);
+}
+template <typename T>
+__device__ __forceinline__ T* at(void* p, int64_t byte, uint32_t lane_byte) {
+  return reinterpret_cast<T*>(static_cast<char*>(p) + byte + lane_byte);
+}
+// NT: streaming accesses.  An access of 16 (codes 8) bytes per lane writes whole
+// lines then; fp32 stores, 32 bytes per lane in two accesses, would not (rotary
+// of 16384 x 5120 fp32: 138 us, streaming 173) and never stream.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 template <bool BF> struct Raw8;
 template <> struct Raw8<true> {
   uint4 a;
   __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void load(const void* p, int64_t i) {
-    a = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(p) + i);
+  template <bool NT = false>
+  __device__ __forceinline__ void load(const void* p, int64_t i, uint32_t c = 0) {
+    const u32x4_t* q = at<u32x4_t>(p, i * 2, c * 2);
+    a = __builtin_bit_cast(uint4, NT ? __builtin_nontemporal_load(q) : *q);
   }
   __device__ __forceinline__ void get(float (&v)[PW]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
@@ -95,8 +111,9 @@ template <> struct Raw8<true> {
 template <> struct Raw8<false> {
   float4 a, b;
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void load(const void* p, int64_t i) {
-    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+  template <bool NT = false>
+  __device__ __forceinline__ void load(const void* p, int64_t i, uint32_t c = 0) {
+    const float4* q = at<float4>(p, i * 4, c * 4);
     a = q[0];
     b = q[1];
   }
@@ -106,13 +123,15 @@ template <> struct Raw8<false> {
   }
 };
 // Rounded to nearest even where the type is bf16.
-template <bool BF>
-__device__ __forceinline__ void store8(void* p, int64_t i, const float (&v)[PW]) {
+template <bool BF, bool NT = false>
+__device__ __forceinline__ void store8(void* p, int64_t i, uint32_t c, const float (&v)[PW]) {
   if constexpr (BF) {
-    *reinterpret_cast<uint4*>(static_cast<bf16_t*>(p) + i) =
-        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    const u32x4_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    u32x4_t* q = at<u32x4_t>(p, i * 2, c * 2);
+    if (NT) __builtin_nontemporal_store(w, q);
+    else *q = w;
   } else {
-    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
+    float4* q = at<float4>(p, i * 4, c * 4);
     q[0] = make_float4(v[0], v[1], v[2], v[3]);
     q[1] = make_float4(v[4], v[5], v[6], v[7]);
   }
@@ -123,16 +142,20 @@ struct RawP {
   uint2 c;
   uint32_t s;
   __device__ __forceinline__ void zero() { c = make_uint2(0, 0); s = 127; }
-  __device__ __forceinline__ void load(const zl_packed& p, int64_t r, int col) {
-    c = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.codes) + r * p.ld_codes + col);
-    s = static_cast<const uint8_t*>(p.scales)[r * p.ld_scales + col / PBLK];
+  __device__ __forceinline__ void load(const zl_packed& p, int64_t r, uint32_t col) {
+    c = *at<uint2>(static_cast<const void*>(p.codes), r * p.ld_codes, col);
+    s = *at<uint8_t>(static_cast<const void*>(p.scales), r * p.ld_scales, col / PBLK);
   }
   __device__ __forceinline__ void get(float (&v)[PW]) const { unpack8(c, s, v); }
 };
 // Stores the codes of a lane and, from the block's first lane, the scale.
-__device__ __forceinline__ void store_packed(const zl_packed& p, int64_t r, int col, uint2 c, uint32_t sb) {
-  *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.codes) + r * p.ld_codes + col) = c;
-  if ((col & (PBLK - 1)) == 0) static_cast<uint8_t*>(p.scales)[r * p.ld_scales + col / PBLK] = (uint8_t)sb;
+template <bool NT = false>
+__device__ __forceinline__ void store_packed(const zl_packed& p, int64_t r, uint32_t col, uint2 c, uint32_t sb) {
+  u32x2_t* q = at<u32x2_t>(p.codes, r * p.ld_codes, col);
+  const u32x2_t w = {c.x, c.y};
+  if (NT) __builtin_nontemporal_store(w, q);
+  else *q = w;
+  if ((col & (PBLK - 1)) == 0) *at<uint8_t>(p.scales, r * p.ld_scales, col / PBLK) = (uint8_t)sb;
 }
 
 }  // namespace zl
