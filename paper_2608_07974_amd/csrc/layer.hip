@@ -12,9 +12,11 @@ constexpr int LT = 256;  // threads per block
 
 // Columns to lanes, rows to blocks: a row takes 2^l2 lanes of 8 columns each
 // (whole 32-column blocks), ncx column chunks of them where it is longer; a
-// block has LT / 2^l2 rows at once, U times.  (Shorter chunks where many
-// lanes lie past the row measured slower: pack and unpack of 8192 x 1544 15.9 us,
-// in chunks of 256 columns 20.4.)
+// block has LT / 2^l2 rows at once, U times.  A row longer than a block's lanes
+// goes in chunks of 128 or 64 lanes where that leaves an eighth fewer lanes past
+// its end (pack and unpack of 8192 x 2056 bf16: 26.5 us in chunks of 256 lanes,
+// 22.5 so).  Groups of columns dealt out without regard to rows leave none, but
+// measured slower on long rows (SwiGLU backward 16384 x 14336: 401 us, 378 so).
 struct RowGrid {
   int l2, ncx;
   int64_t T;
@@ -23,6 +25,10 @@ static RowGrid row_grid(int64_t T, int n) {
   const int lanes = (n + PBLK - 1) / PBLK * (PBLK / PW);
   int l2 = 2;
   while ((1 << l2) < lanes && (1 << l2) < LT) ++l2;
+  auto padded = [&](int l) { return (lanes + (1 << l) - 1) >> l << l; };
+  if (lanes > LT)
+    for (int l = 7; l >= 6; --l)
+      if (padded(l) * 8 <= padded(l2) * 7) l2 = l;
   return {l2, (lanes + (1 << l2) - 1) >> l2, T};
 }
 static int64_t row_blocks(const RowGrid& g, int U) {

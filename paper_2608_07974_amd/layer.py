@@ -200,18 +200,19 @@ NormGrads.__doc__ = "Gradients of block_norm's parameters (fp32; None = not want
 
 
 def _norm_common(d, T, dev, post, pre, gate, gate_rows, stats):
-    wb = [_vec(n, t, d) for n, t in zip(("w_post", "b_post", "w_pre", "b_pre"), (*(post or (None, None)),
-                                                                                *(pre or (None, None))))]
+    """Pointers of the weights and biases, everything of them checked."""
+    w0, b0 = post or (None, None)
+    w1, b1 = pre or (None, None)
+    wb = _vec("w_post", w0, d), _vec("b_post", b0, d), _vec("w_pre", w1, d), _vec("b_pre", b1, d)
     if gate is not None:
         if gate_rows < 1:
             raise ValueError("a gate needs gate_rows >= 1")
         G = -(-T // gate_rows)
-        if gate.dtype != torch.float32 or tuple(gate.shape) != (G, d) or not gate.is_contiguous():
+        if gate.dtype != torch.float32 or gate.shape != (G, d) or not gate.is_contiguous():
             raise ValueError(f"gate must be a contiguous fp32 [{G}, {d}] tensor")
-    if stats.dtype != torch.float32 or tuple(stats.shape) != (T, 4) or not stats.is_contiguous():
+    if stats.dtype != torch.float32 or stats.shape != (T, 4) or not stats.is_contiguous():
         raise ValueError(f"stats must be a contiguous fp32 [{T}, 4] tensor")
-    _check_device(dev, ("w_post", post and post[0]), ("b_post", post and post[1]), ("w_pre", pre and pre[0]),
-                  ("b_pre", pre and pre[1]), ("gate", gate), ("stats", stats))
+    _check_device(dev, ("w_post", w0), ("b_post", b0), ("w_pre", w1), ("b_pre", b1), ("gate", gate), ("stats", stats))
     return wb
 
 
@@ -275,11 +276,15 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
     wb = _norm_common(d, T, dev, post, pre, gate, gate_rows, stats)
     if (y is None) != (post is None) or (dn is None) != (pre is None) or (pre is not None and xo is None):
         raise ValueError("y and post, dn, xo and pre go together")
-    strided = [t for t in (dxo, dx, xo if pre is not None else None) if t is not None]
-    lds = {_rows("dxo, dx and xo", t, T, d, f32) for t in strided}
-    if len(lds) > 1:
-        raise ValueError("dxo, dx and xo must have one row stride")
-    ldx = lds.pop() if lds else d
+    ldx = None
+    for t in (dxo, dx, xo if pre is not None else None):
+        if t is not None:
+            ld = _rows("dxo, dx and xo", t, T, d, f32)
+            if ldx is not None and ld != ldx:
+                raise ValueError("dxo, dx and xo must have one row stride")
+            ldx = ld
+    if ldx is None:
+        ldx = d
     if dx is None:
         dx = torch.empty_strided((T, d), (ldx, 1), dtype=torch.float32, device=dev)
     tin, ldn, ldy = None, 0, 0
@@ -302,7 +307,8 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
     elif dy is not None:
         raise ValueError("dy needs post")
     g = NormGrads() if grads is None else grads
-    gp = [_vec("grads." + k, t, d) for k, t in zip(g._fields[:4], g[:4])]
+    gp = (_vec("grads.w_post", g.w_post, d), _vec("grads.b_post", g.b_post, d), _vec("grads.w_pre", g.w_pre, d),
+          _vec("grads.b_pre", g.b_pre, d))
     if g.gate is not None and (gate is None or g.gate.shape != gate.shape or g.gate.dtype != torch.float32 or
                                not g.gate.is_contiguous()):
         raise ValueError("grads.gate must be a contiguous fp32 tensor like gate")
@@ -311,7 +317,8 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
     elif workspace.dtype != torch.float32 or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous fp32 tensor")
     _check_device(dev, ("dxo", dxo), ("y", y), ("xo", xo), ("dx", dx), ("dy", dy), ("workspace", workspace),
-                  *(("grads." + k, t) for k, t in zip(g._fields, g)))
+                  ("grads.w_post", g.w_post), ("grads.b_post", g.b_post), ("grads.w_pre", g.w_pre),
+                  ("grads.b_pre", g.b_pre), ("grads.gate", g.gate))
     a = zl.zl_norm_args(T, d, int(layernorm), _DT[tin], zl.ZL_F32 if dy is None else _DT[dy.dtype], eps, scale, *wb,
                         _ptr(gate), gate_rows, stats.data_ptr(), None, _ptr(xo) if pre is not None else None, ldx, yp,
                         ldy, None, ldn, ys, _NONE, _ptr(dxo), _ptr(dn), dx.data_ptr(), _ptr(dy), *gp, _ptr(g.gate),
