@@ -476,6 +476,76 @@ def test_wgrad_non_finite_stays_in_its_column():
         assert bad[:, 100].all() and bad[7].all() and bad.sum() == M + N - 1
 
 
+@pytest.mark.parametrize("dt", [F32, BF])
+def test_wgrad_takes_every_scale(dt):
+    """Scale bytes that packing never writes: 255 is NaN, the smallest and the
+    largest stand for what they say (values below the normal range may be
+    dropped, as the bf16 products do)."""
+    layer = _L()
+    T, M, N = 40, 136, 256
+    rng = _rng("scales")
+    codes = torch.from_numpy(rng.integers(0, 127, (T, N)).astype(np.uint8)).cuda()
+    scales = torch.full((T, N // 32), 127, dtype=torch.uint8, device="cuda")
+    scales[0, 0], scales[1, 1], scales[2, 2], scales[3, 3] = 255, 1, 0, 240
+    dy = np.abs(rng.standard_normal((T, M))) + 0.1
+    dyt = _dev(dy, dt)
+    got = _np(layer.wgrad(dyt, layer.Packed(codes, scales, N)))
+    a, b = _np(dyt), ol.values(codes.cpu().numpy(), scales.cpu().numpy())
+    assert np.isnan(got[:, :32]).all() and np.isfinite(got[:, 32:]).all()
+    ref, mag = a.T @ b[:, 32:], np.abs(a).T @ np.abs(b[:, 32:])
+    _near(got[:, 32:], ref, (T + 8) * U * mag)
+
+
+def test_wgrad_in_segments_of_tokens():
+    """Rows so far apart that 32-bit offsets do not reach the last: the sum
+    goes on in further launches (200000 apart) or through 64-bit addresses
+    (2^20 apart)."""
+    layer = _L()
+    rng = _rng("segments")
+    for T, ld, M, N, ws in ((5000, 200000, 264, 72, 0), (5000, 200000, 64, 64, 1 << 20), (1100, 1 << 20, 72, 40, 1 << 20)):
+        dy = torch.empty(T, ld, dtype=torch.bfloat16, device="cuda")[:, :M]
+        dy.copy_(torch.from_numpy(rng.standard_normal((T, M)).astype(np.float32)))
+        x = _acts(rng, T, N)
+        p = _packed(x)
+        a, b = _np(dy), ol.packed(x)
+        old = rng.standard_normal((M, N)).astype(np.float32)
+        w = torch.empty(ws, device="cuda") if ws else None
+        for acc in (False, True):
+            got = layer.wgrad(dy, p, out=_dev(old), scale=0.5, accumulate=acc, workspace=w)
+            _near(_np(got), acc * old + 0.5 * a.T @ b, (T + 16) * U * (np.abs(a).T @ np.abs(b) + np.abs(old)))
+        del dy, got
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Four rows 2^30 bytes and more apart through every other operator."""
+    layer = _L()
+    rng = _rng("far")
+    T, d, far = 4, 72, (1 << 29) + 8
+
+    def wide(a, dt=F32, ld=far):
+        t = torch.empty(T, ld, dtype=_dt(dt), device="cuda")[:, : a.shape[1]]
+        t.copy_(torch.from_numpy(np.asarray(a, np.float32)))
+        return t
+
+    x, y = _acts(rng, T, d), rng.standard_normal((T, d))
+    xw, yw = wide(x), wide(y, BF)
+    p = layer.Packed(torch.empty(T, 1 << 30, dtype=torch.uint8, device="cuda"), torch.empty(T, 1 << 30, dtype=torch.uint8, device="cuda"), d)
+    layer.pack(xw, out=p)
+    _same_codes(_bytes(p, T, d), ol.pack(_np(xw)))
+    back = layer.unpack(p, out=wide(0 * x))
+    assert np.array_equal(_np(back), ol.packed(_np(xw)))
+    assert torch.equal(layer.mlp_act(xw, "gelu", act=back), layer.mlp_act(xw.contiguous(), "gelu"))
+    assert torch.equal(layer.mlp_act_bwd(xw, xw, "gelu", dh=back), layer.mlp_act_bwd(xw.contiguous(), xw.contiguous(), "gelu"))
+    w = (_vec(1 + 0.1 * rng.standard_normal(d)), None)
+    near = layer.block_norm(xw.contiguous(), yw.contiguous(), w, w)
+    got = layer.block_norm(xw, yw, w, w, n=wide(y, BF))
+    assert all(torch.equal(a, b) for a, b in zip(got, near))
+    args = lambda f: (f(xw), f(yw), f(yw), f(got[0]), near[2], w, w)  # noqa: E731
+    assert all(torch.equal(a, b) for a, b in zip(layer.block_norm_bwd(*args(lambda t: t)), layer.block_norm_bwd(*args(lambda t: t.contiguous()))))
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")[None]
+    assert torch.equal(layer.rotary(xw, pos, bytes(12), 3, 24, 1e4, out=back), layer.rotary(xw.contiguous(), pos, bytes(12), 3, 24, 1e4))
+
+
 # ------------------------------------------------------------------- rotary
 @pytest.mark.parametrize("dt", [F32, BF])
 @pytest.mark.parametrize("T,H,hd,rot,axes,pad", [
