@@ -13,61 +13,87 @@
 
 namespace zl {
 
-// ------------------------------------------------------------ vector ALUs
-// 64 x 64 tiles, 16 tokens a step, 4 x 4 outputs per thread.  A block has
-// tokens [z per, (z + 1) per); with splits it writes fp32 partials.
-constexpr int VT = 64, VK = 16;
-
-template <bool BF>
-__global__ void __launch_bounds__(256) wgrad_valu_kernel(WgradArgs a, int64_t per, bool split) {
-  __shared__ __align__(16) float As[VK][VT], Bs[VK][VT];
-  const int m0 = blockIdx.y * VT, n0 = blockIdx.x * VT;
+// --------------------------------------------------------------- fp32 MFMA
+// BT x BT tiles of four waves, v_mfma_f32_32x32x2_f32 on fp32 tiles of 2048 / BT
+// tokens in LDS; the next tile is loaded and the one after it widened while
+// this one is multiplied (one barrier per tile).  64-bit addresses: also what
+// bf16 dy takes whose rows lie too far apart for buffer offsets.  A block has
+// tokens [z per, (z + 1) per); with splits it writes fp32 partials.  Registers for
+// three blocks a CU: 256 x 4096 x 8192 154 us (two: 173; 64 x 64 tiles on the vector
+// ALUs: 224).
+template <bool BF, int BT>
+__global__ void __launch_bounds__(256, 3) wgrad_f32_kernel(WgradArgs a, int64_t per, bool split) {
+  constexpr int VK = 2048 / BT, CH = BT / PW, F = BT / 64;  // 32 x 32 blocks per wave and side
+  __shared__ __align__(16) float As[2][VK][BT], Bs[2][VK][BT];
+  const int m0 = blockIdx.y * BT, n0 = blockIdx.x * BT;
   const int64_t t0 = blockIdx.z * per, t1 = min(t0 + per, a.T);
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  float acc[4][4] = {};
-  // this thread's 8 columns of one of the 16 tokens: threads 0 - 127 of dy, the others of x
-  const int lt = (tid & 127) >> 3, lc = (tid & 7) * PW;
-  for (int64_t t = t0; t < t1; t += VK) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // this thread's 8 columns of one token of the tile, of dy and of x
+  const int lt = tid / CH, lc = (tid % CH) * PW;
+  const int lr = lane & 31, lk = lane >> 5, wm = (wave >> 1) * 32 * F, wn = (wave & 1) * 32 * F;
+  f32x16_t acc[F][F];
+#pragma unroll
+  for (int i = 0; i < F; ++i)
+#pragma unroll
+    for (int j = 0; j < F; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  Raw8<BF> ra;
+  RawP rb;
+  auto load = [&](int64_t t) __attribute__((always_inline)) {
+    ra.zero();
+    rb.zero();
+    if (t + lt < t1 && m0 + lc < a.M) ra.load(a.dy, (t + lt) * a.lddy + m0 + lc);
+    if (t + lt < t1 && n0 + lc < a.N) rb.load(a.x, t + lt, n0 + lc);
+  };
+  auto put = [&](int buf) __attribute__((always_inline)) {
     float v[PW];
-    const bool ok = t + lt < t1 && (tid < 128 ? m0 + lc < a.M : n0 + lc < a.N);
-    if (tid < 128) {
-      Raw8<BF> r;
-      r.zero();
-      if (ok) r.load(a.dy, (t + lt) * a.lddy + m0 + lc);
-      r.get(v);
-    } else {
-      RawP r;
-      r.zero();
-      if (ok) r.load(a.x, t + lt, n0 + lc);
-      r.get(v);
+    ra.get(v);
+    *reinterpret_cast<float4*>(&As[buf][lt][lc]) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(&As[buf][lt][lc + 4]) = make_float4(v[4], v[5], v[6], v[7]);
+    rb.get(v);
+    *reinterpret_cast<float4*>(&Bs[buf][lt][lc]) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(&Bs[buf][lt][lc + 4]) = make_float4(v[4], v[5], v[6], v[7]);
+  };
+  load(t0);
+  put(0);
+  load(t0 + VK);
+  __syncthreads();
+  int buf = 0;
+  for (int64_t t = t0; t < t1; t += VK) {
+    put(buf ^ 1);  // the tile after this one
+    load(t + 2 * VK);
+#pragma unroll
+    for (int k = 0; k < VK; k += 2) {
+      float x[F], y[F];
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        x[i] = As[buf][k + lk][wm + 32 * i + lr];
+        y[i] = Bs[buf][k + lk][wn + 32 * i + lr];
+      }
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[j], acc[i][j], 0, 0, 0);
     }
     __syncthreads();
-    float* d = tid < 128 ? &As[lt][lc] : &Bs[lt][lc];
-#pragma unroll
-    for (int i = 0; i < PW; ++i) d[i] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < VK; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(&As[k][ty * 4]);
-      const float4 y = *reinterpret_cast<const float4*>(&Bs[k][tx * 4]);
-      const float xa[4] = {x.x, x.y, x.z, x.w}, ya[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += xa[i] * ya[j];
-    }
+    buf ^= 1;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + ty * 4 + i, n = n0 + tx * 4;
-    if (m >= a.M || n >= a.N) continue;
-    float* o = split ? a.part + ((int64_t)blockIdx.z * a.M + m) * a.N + n : a.dw + (int64_t)m * a.lddw + n;
+  for (int i = 0; i < F; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (split) o[j] = acc[i][j];
-      else o[j] = (a.accumulate ? o[j] : 0.f) + a.scale * acc[i][j];
-    }
-  }
+    for (int j = 0; j < F; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int m = m0 + wm + 32 * i + Mma<32>::row(lane, r), n = n0 + wn + 32 * j + lr;
+        if (m >= a.M || n >= a.N) continue;
+        if (split) {
+          a.part[((int64_t)blockIdx.z * a.M + m) * a.N + n] = acc[i][j][r];
+        } else {
+          float* o = a.dw + (int64_t)m * a.lddw + n;
+          *o = (a.accumulate ? *o : 0.f) + a.scale * acc[i][j][r];
+        }
+      }
 }
 
 static EpiArgs grad_epi(const WgradArgs& a) {
@@ -82,12 +108,14 @@ static EpiArgs grad_epi(const WgradArgs& a) {
   return e;
 }
 
-template <bool BF>
-static hipError_t wgrad_valu(const WgradArgs& a, hipStream_t s) {
-  const int nx = (a.N + VT - 1) / VT, ny = (a.M + VT - 1) / VT;
+template <bool BF, int BT>
+static hipError_t wgrad_f32_go(const WgradArgs& a, hipStream_t s) {
+  constexpr int VK = 2048 / BT;
+  const int64_t nx = (a.N + BT - 1) / BT, ny = (a.M + BT - 1) / BT;
   if (ny > 65535) return hipErrorInvalidValue;
-  // splits of at least 256 tokens until there are four blocks per CU
-  int64_t nz = 1024 / ((int64_t)nx * ny);
+  // splits of at least 256 tokens until there are two blocks per CU, four of the
+  // small ones (4096 x 1024 x 2048: 158 us, with two 166)
+  int64_t nz = (BT == 128 ? 512 : 1024) / (nx * ny);
   if (nz > a.T / 256) nz = a.T / 256;
   const int64_t room = a.part ? (int64_t)(a.part_elems / ((size_t)a.M * a.N)) : 0;
   if (nz > room) nz = room;
@@ -95,10 +123,17 @@ static hipError_t wgrad_valu(const WgradArgs& a, hipStream_t s) {
   int64_t per = (a.T + nz - 1) / nz;
   per = (per + VK - 1) / VK * VK;
   nz = a.T > 0 ? (a.T + per - 1) / per : 1;
-  hipLaunchKernelGGL((wgrad_valu_kernel<BF>), dim3(nx, ny, (unsigned)nz), dim3(256), 0, s, a, per, nz > 1);
+  hipLaunchKernelGGL((wgrad_f32_kernel<BF, BT>), dim3((unsigned)nx, (unsigned)ny, (unsigned)nz), dim3(256), 0, s, a, per, nz > 1);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || nz == 1) return e;
   return launch_splitk_reduce(a.part, (int)nz, a.M, a.N, grad_epi(a), s);
+}
+template <bool BF>
+static hipError_t wgrad_f32(const WgradArgs& a, hipStream_t s) {
+  // large tiles where they fill the chip without splits (1024 x 2048 x 4096: 150 us;
+  // 30 x 1000 x 2000, 128 of them, 13.0 where small ones take 6.7)
+  const int64_t large = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
+  return large >= 256 ? wgrad_f32_go<BF, 128>(a, s) : wgrad_f32_go<BF, 64>(a, s);
 }
 
 // ------------------------------------------------------------------- MFMA
@@ -317,13 +352,13 @@ static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accu
 }
 
 hipError_t launch_wgrad_packed(const WgradArgs& a, int dtype, hipStream_t s) {
-  if (dtype != BF16) return wgrad_valu<false>(a, s);
+  if (dtype != BF16) return wgrad_f32<false>(a, s);
   // tokens per launch: the largest offset from a tile's origin stays below 2^31
   const int64_t row = 2 * a.lddy > a.x.ld_codes ? 2 * a.lddy : a.x.ld_codes;
   const int64_t top = row > a.x.ld_scales ? row : a.x.ld_scales;
   const int64_t most = (((int64_t)1 << 31) - 1024) / top - 1024;
   if (a.T > 0 && a.T <= most) return wgrad_segment(a, 0, (int)a.T, a.accumulate != 0, s);
-  if (a.T == 0 || most < 4096) return wgrad_valu<true>(a, s);
+  if (a.T == 0 || most < 4096) return wgrad_f32<true>(a, s);
   const int64_t step = most / 32 * 32;
   for (int64_t t = 0; t < a.T; t += step) {
     const int64_t n = a.T - t < step ? a.T - t : step;
