@@ -9,7 +9,8 @@ Tensors are 2-D [T, columns], rows contiguous (any row stride that is a
 multiple of 8), bf16 or fp32, all on one GPU; work goes to that GPU's current
 stream.  Shapes, types and placement are checked here (the kernels take them
 on trust), the rest by the library, which raises zl.ZlError.  Output tensors
-may be given (and are returned); else they are made.
+may be given (and are returned); else they are made.  autograd does not see
+these calls: a layer calls the backward functions itself.
 """
 from collections import namedtuple
 
@@ -87,7 +88,7 @@ class Packed:
     """A matrix [T, n] in 8 bits: `codes` uint8 [T, >= n rounded up to 16] and
     `scales` uint8 [T, >= ceil(n / 32)], both with contiguous rows."""
 
-    __slots__ = ("codes", "scales", "n", "struct")
+    __slots__ = ("codes", "scales", "n")
 
     def __init__(self, codes, scales, n):
         T, W = codes.shape if codes.dim() == 2 else (-1, -1)
@@ -105,9 +106,13 @@ class Packed:
         if codes.device != scales.device:
             raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
         self.codes, self.scales, self.n = codes, scales, n
-        if T <= 1:
-            lc, ls = c16, c32
-        self.struct = zl.zl_packed(codes.data_ptr(), scales.data_ptr(), lc, ls)
+
+    def struct(self):
+        """The matrix as the library takes it."""
+        c, s = self.codes, self.scales
+        if c.shape[0] > 1:
+            return zl.zl_packed(c.data_ptr(), s.data_ptr(), c.stride(0), s.stride(0))
+        return zl.zl_packed(c.data_ptr(), s.data_ptr(), _up(self.n, 16), (self.n + 31) // 32)
 
     @classmethod
     def empty(cls, T, n, device="cuda"):
@@ -129,7 +134,7 @@ class Packed:
 def _packed(name, p, T, n):
     if p.n != n or p.codes.shape[0] != T:
         raise ValueError(f"{name} must be [{T}, {n}], not {list(p.shape)}")
-    return p.struct
+    return p.struct()
 
 
 def pack(x, out=None):
@@ -149,7 +154,7 @@ def unpack(p, dtype=torch.bfloat16, out=None):
     out = torch.empty(T, n, dtype=dtype, device=p.device) if out is None else out
     ld = _rows("out", out, T, n, _DT)
     _check_device(p.device, ("out", out))
-    _call(zl.zl_unpack, p.device, T, n, p.struct, out.data_ptr(), ld, _DT[out.dtype])
+    _call(zl.zl_unpack, p.device, T, n, p.struct(), out.data_ptr(), ld, _DT[out.dtype])
     return out
 
 
@@ -185,7 +190,7 @@ def mlp_act_bwd(h, dact, kind="swiglu", dtype=None, dh=None, act=None):
     lddh = _rows("dh", dh, T, nh, _DT)
     lda = 0 if act is None else _rows("act", act, T, ff, (dh.dtype,))
     if isinstance(h, Packed):
-        hp, ldh, ps = None, 0, h.struct
+        hp, ldh, ps = None, 0, h.struct()
     else:
         hp, ldh, ps = h.data_ptr(), _rows("h", h, T, nh, (dact.dtype,)), _NONE
     _check_device(dev, ("h", h), ("dh", dh), ("act", act))
