@@ -20,7 +20,8 @@ from . import zl
 
 _DT = {torch.float32: zl.ZL_F32, torch.bfloat16: zl.ZL_BF16}
 _KIND = {"swiglu": zl.ZL_MLP_SWIGLU, "gelu": zl.ZL_MLP_GELU}
-_NONE = zl.zl_packed(None, None, 0, 0)
+_NONE = (0, 0, 0, 0)  # no packed matrix
+_F32 = (torch.float32,)
 
 
 def _up(n, m):
@@ -28,18 +29,18 @@ def _up(n, m):
 
 
 def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
 
 
-def _check_device(dev, *named):
-    """Every tensor of (name, tensor or None) pairs is on the GPU dev.  (The
-    host's share of a small call is most of it: the checks of this file are
-    written for the case that passes.)"""
+# The host's share of a small call is most of it: the checks of this file are
+# written for the case that passes.
+def _check_device(dev, names, *tensors):
+    """Every tensor (or None) is on the GPU dev; names: theirs, in one text."""
     if dev.type != "cuda":
         raise ValueError(f"tensors must be on a GPU, not {dev}")
-    for name, t in named:
+    for i, t in enumerate(tensors):
         if t is not None and t.device != dev:
-            raise ValueError(f"{name} must be on {dev}, not {t.device}")
+            raise ValueError(f"{names.split()[i]} must be on {dev}, not {t.device}")
 
 
 def _rows(name, t, T, n, dtypes):
@@ -60,7 +61,7 @@ def _rows(name, t, T, n, dtypes):
 
 def _vec(name, t, n):
     if t is None:
-        return None
+        return 0
     if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 vector of {n}")
     return t.data_ptr()
@@ -88,31 +89,30 @@ class Packed:
     """A matrix [T, n] in 8 bits: `codes` uint8 [T, >= n rounded up to 16] and
     `scales` uint8 [T, >= ceil(n / 32)], both with contiguous rows."""
 
-    __slots__ = ("codes", "scales", "n")
+    __slots__ = ("codes", "scales", "n", "_ld")
 
     def __init__(self, codes, scales, n):
-        T, W = codes.shape if codes.dim() == 2 else (-1, -1)
-        c16, c32 = _up(n, 16), (n + 31) // 32
-        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or T < 0 or scales.dim() != 2:
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2:
             raise TypeError("codes and scales must be uint8 matrices")
-        if W < c16 or scales.shape[0] != T or scales.shape[1] < c32:
-            raise ValueError(f"codes and scales must be [{T}, >= {c16}] and [{T}, >= {c32}], not {list(codes.shape)} and "
-                             f"{list(scales.shape)}")
-        (lc, c1), (ls, s1) = codes.stride(), scales.stride()
-        if (c1 != 1 and W > 1) or (s1 != 1 and scales.shape[1] > 1):
-            raise ValueError("codes and scales must have contiguous rows")
-        if T > 1 and (lc < c16 or ls < c32):
-            raise ValueError("codes and scales must not overlap themselves")
+        (T, W), (Ts, Ws), c16, c32 = codes.shape, scales.shape, _up(n, 16), (n + 31) // 32
+        if W < c16 or Ts != T or Ws < c32:
+            raise ValueError(f"codes and scales must be [{T}, >= {c16}] and [{T}, >= {c32}], not [{T}, {W}] and [{Ts}, {Ws}]")
+        if codes.is_contiguous() and scales.is_contiguous():
+            self._ld = (W, Ws) if T > 1 else (c16, c32)
+        else:
+            (lc, c1), (ls, s1) = codes.stride(), scales.stride()
+            if (c1 != 1 and W > 1) or (s1 != 1 and Ws > 1):
+                raise ValueError("codes and scales must have contiguous rows")
+            if T > 1 and (lc < c16 or ls < c32):
+                raise ValueError("codes and scales must not overlap themselves")
+            self._ld = (lc, ls) if T > 1 else (c16, c32)
         if codes.device != scales.device:
             raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
         self.codes, self.scales, self.n = codes, scales, n
 
-    def struct(self):
-        """The matrix as the library takes it."""
-        c, s = self.codes, self.scales
-        if c.shape[0] > 1:
-            return zl.zl_packed(c.data_ptr(), s.data_ptr(), c.stride(0), s.stride(0))
-        return zl.zl_packed(c.data_ptr(), s.data_ptr(), _up(self.n, 16), (self.n + 31) // 32)
+    def fields(self):
+        """The matrix as the library takes it: pointers and row strides."""
+        return (self.codes.data_ptr(), self.scales.data_ptr()) + self._ld
 
     @classmethod
     def empty(cls, T, n, device="cuda"):
@@ -132,47 +132,59 @@ class Packed:
 
 
 def _packed(name, p, T, n):
+    if p is None:
+        return _NONE
     if p.n != n or p.codes.shape[0] != T:
         raise ValueError(f"{name} must be [{T}, {n}], not {list(p.shape)}")
-    return p.struct()
+    return p.fields()
 
 
 def pack(x, out=None):
     """x in 8 bits."""
     T, n = x.shape
+    dev = x.device
     ldx = _rows("x", x, T, n, _DT)
-    out = Packed.empty(T, n, x.device) if out is None else out
-    s = _packed("out", out, T, n)
-    _check_device(x.device, ("out", out))
-    _call(zl.zl_pack, x.device, T, n, x.data_ptr(), ldx, _DT[x.dtype], s)
+    out = Packed.empty(T, n, dev) if out is None else out
+    p = zl.pack_packed(*_packed("out", out, T, n))
+    _check_device(dev, "out", out)
+    _call(zl.zl_pack, dev, T, n, x.data_ptr(), ldx, _DT[x.dtype], p)
     return out
 
 
 def unpack(p, dtype=torch.bfloat16, out=None):
     """The values of a Packed matrix."""
     T, n = p.shape
-    out = torch.empty(T, n, dtype=dtype, device=p.device) if out is None else out
+    dev = p.device
+    out = torch.empty(T, n, dtype=dtype, device=dev) if out is None else out
     ld = _rows("out", out, T, n, _DT)
-    _check_device(p.device, ("out", out))
-    _call(zl.zl_unpack, p.device, T, n, p.struct(), out.data_ptr(), ld, _DT[out.dtype])
+    _check_device(dev, "out", out)
+    _call(zl.zl_unpack, dev, T, n, zl.pack_packed(*p.fields()), out.data_ptr(), ld, _DT[out.dtype])
     return out
+
+
+def _ff(h, kind):
+    """kind's number and the activation's width."""
+    k, nh = _KIND[kind], h.shape[1]
+    if k == zl.ZL_MLP_GELU:
+        return k, nh
+    if nh % 2:
+        raise ValueError(f"h must be gate | up, not of {nh} columns")
+    return k, nh // 2
 
 
 def mlp_act(h, kind="swiglu", dtype=None, act=None, packed=None):
     """silu(gate) * up of h = gate | up [T, 2 ff], or gelu(h), h [T, ff].
     packed: a Packed of h's shape that receives h."""
     T, nh = h.shape
-    k = _KIND[kind]
-    if k == zl.ZL_MLP_SWIGLU and nh % 2:
-        raise ValueError(f"h must be gate | up, not of {nh} columns")
-    ff = nh // 2 if k == zl.ZL_MLP_SWIGLU else nh
+    k, ff = _ff(h, kind)
+    dev = h.device
     ldh = _rows("h", h, T, nh, _DT)
-    act = torch.empty(T, ff, dtype=dtype or h.dtype, device=h.device) if act is None else act
+    act = torch.empty(T, ff, dtype=dtype or h.dtype, device=dev) if act is None else act
     lda = _rows("act", act, T, ff, _DT)
-    ps = _NONE if packed is None else _packed("packed", packed, T, nh)
-    _check_device(h.device, ("act", act), ("packed", packed))
-    a = zl.zl_mlp_args(T, ff, k, _DT[h.dtype], _DT[act.dtype], h.data_ptr(), ldh, ps, act.data_ptr(), lda)
-    _call(zl.zl_mlp_act, h.device, a)
+    ps = _packed("packed", packed, T, nh)
+    _check_device(dev, "act packed", act, packed)
+    _call(zl.zl_mlp_act, dev, zl.pack_mlp_args(T, ff, k, _DT[h.dtype], _DT[act.dtype], h.data_ptr(), ldh, *ps,
+                                               act.data_ptr(), lda, 0, 0, 0, 0))
     return act
 
 
@@ -180,45 +192,45 @@ def mlp_act_bwd(h, dact, kind="swiglu", dtype=None, dh=None, act=None):
     """Gradient with respect to h (a tensor of dact's type, or its Packed
     copy).  act: a tensor that receives the activation, formed again."""
     T, nh = h.shape
-    k = _KIND[kind]
-    if k == zl.ZL_MLP_SWIGLU and nh % 2:
-        raise ValueError(f"h must be gate | up, not of {nh} columns")
-    ff = nh // 2 if k == zl.ZL_MLP_SWIGLU else nh
+    k, ff = _ff(h, kind)
     dev = dact.device
     ldda = _rows("dact", dact, T, ff, _DT)
     dh = torch.empty(T, nh, dtype=dtype or dact.dtype, device=dev) if dh is None else dh
     lddh = _rows("dh", dh, T, nh, _DT)
     lda = 0 if act is None else _rows("act", act, T, ff, (dh.dtype,))
     if isinstance(h, Packed):
-        hp, ldh, ps = None, 0, h.struct()
+        hp, ldh, ps = 0, 0, h.fields()
     else:
         hp, ldh, ps = h.data_ptr(), _rows("h", h, T, nh, (dact.dtype,)), _NONE
-    _check_device(dev, ("h", h), ("dh", dh), ("act", act))
-    a = zl.zl_mlp_args(T, ff, k, _DT[dact.dtype], _DT[dh.dtype], hp, ldh, ps, _ptr(act), lda, dact.data_ptr(), ldda,
-                       dh.data_ptr(), lddh)
-    _call(zl.zl_mlp_act_backward, dev, a)
+    _check_device(dev, "h dh act", h, dh, act)
+    _call(zl.zl_mlp_act_backward, dev,
+          zl.pack_mlp_args(T, ff, k, _DT[dact.dtype], _DT[dh.dtype], hp, ldh, *ps, _ptr(act), lda, dact.data_ptr(), ldda,
+                           dh.data_ptr(), lddh))
     return dh
 
 
 NormGrads = namedtuple("NormGrads", "w_post b_post w_pre b_pre gate", defaults=(None,) * 5)
 NormGrads.__doc__ = "Gradients of block_norm's parameters (fp32; None = not wanted)."
+_NO_WB = (None, None)
 
 
 def _norm_common(d, T, dev, post, pre, gate, gate_rows, stats):
-    """Pointers of the weights and biases, everything of them checked."""
-    w0, b0 = post or (None, None)
-    w1, b1 = pre or (None, None)
-    wb = _vec("w_post", w0, d), _vec("b_post", b0, d), _vec("w_pre", w1, d), _vec("b_pre", b1, d)
+    """Pointers of the weights, biases, the gate, its rows and the statistics,
+    everything of them checked."""
+    (w0, b0), (w1, b1) = post or _NO_WB, pre or _NO_WB
+    gp = 0
     if gate is not None:
         if gate_rows < 1:
             raise ValueError("a gate needs gate_rows >= 1")
         G = -(-T // gate_rows)
         if gate.dtype != torch.float32 or gate.shape != (G, d) or not gate.is_contiguous():
             raise ValueError(f"gate must be a contiguous fp32 [{G}, {d}] tensor")
+        gp = gate.data_ptr()
     if stats.dtype != torch.float32 or stats.shape != (T, 4) or not stats.is_contiguous():
         raise ValueError(f"stats must be a contiguous fp32 [{T}, 4] tensor")
-    _check_device(dev, ("w_post", w0), ("b_post", b0), ("w_pre", w1), ("b_pre", b1), ("gate", gate), ("stats", stats))
-    return wb
+    _check_device(dev, "w_post b_post w_pre b_pre gate stats", w0, b0, w1, b1, gate, stats)
+    return (_vec("w_post", w0, d), _vec("b_post", b0, d), _vec("w_pre", w1, d), _vec("b_pre", b1, d), gp, gate_rows,
+            stats.data_ptr())
 
 
 def block_norm(x, y, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5, layernorm=False, dtype=None,
@@ -232,10 +244,9 @@ def block_norm(x, y, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5, 
     and n.  n has `dtype` (default: y's, or bf16).  xo may be x."""
     T, d = x.shape
     dev = x.device
-    f32 = (torch.float32,)
-    ldx = _rows("x", x, T, d, f32)
+    ldx = _rows("x", x, T, d, _F32)
     stats = torch.empty(T, 4, device=dev) if stats is None else stats
-    wb = _norm_common(d, T, dev, post, pre, gate, gate_rows, stats)
+    params = _norm_common(d, T, dev, post, pre, gate, gate_rows, stats)
     if (y is None) != (post is None):
         raise ValueError("y and post go together")
     ldy = ldn = 0
@@ -243,7 +254,7 @@ def block_norm(x, y, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5, 
     if y is not None:
         ldy, ty = _rows("y", y, T, d, _DT), _DT[y.dtype]
         xo = torch.empty_strided((T, d), (ldx, 1), dtype=torch.float32, device=dev) if xo is None else xo
-        if _rows("xo", xo, T, d, f32) != ldx:
+        if _rows("xo", xo, T, d, _F32) != ldx:
             raise ValueError("xo must have x's row stride")
     elif xo is not None:
         raise ValueError("xo is x where there is no y")
@@ -252,12 +263,11 @@ def block_norm(x, y, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5, 
         ldn, tn = _rows("n", n, T, d, _DT), _DT[n.dtype]
     elif n is not None:
         raise ValueError("n needs pre")
-    _check_device(dev, ("y", y), ("xo", xo), ("n", n), ("y_packed", y_packed), ("n_packed", n_packed))
-    a = zl.zl_norm_args(T, d, int(layernorm), ty, tn, eps, scale, *wb, _ptr(gate), gate_rows, stats.data_ptr(),
-                        x.data_ptr(), _ptr(xo), ldx, _ptr(y), ldy, _ptr(n), ldn,
-                        _NONE if y_packed is None else _packed("y_packed", y_packed, T, d),
-                        _NONE if n_packed is None else _packed("n_packed", n_packed, T, d))
-    _call(zl.zl_block_norm, dev, a)
+    _check_device(dev, "y xo n y_packed n_packed", y, xo, n, y_packed, n_packed)
+    _call(zl.zl_block_norm, dev,
+          zl.pack_norm_args(T, d, int(layernorm), ty, tn, eps, scale, *params, x.data_ptr(), _ptr(xo), ldx, _ptr(y), ldy,
+                            _ptr(n), ldn, *_packed("y_packed", y_packed, T, d), *_packed("n_packed", n_packed, T, d),
+                            0, 0, 0, 0, 0, 0, 0, 0, 0, 0.0, 0, 0, 0))
     return (x if y is None else xo), n, stats
 
 
@@ -277,14 +287,15 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
         raise ValueError("dxo, dn or xo must be there")
     T, d = src.shape
     dev = src.device
-    f32 = (torch.float32,)
-    wb = _norm_common(d, T, dev, post, pre, gate, gate_rows, stats)
+    params = _norm_common(d, T, dev, post, pre, gate, gate_rows, stats)
     if (y is None) != (post is None) or (dn is None) != (pre is None) or (pre is not None and xo is None):
         raise ValueError("y and post, dn, xo and pre go together")
+    if pre is None:
+        xo = None
     ldx = None
-    for t in (dxo, dx, xo if pre is not None else None):
+    for t in (dxo, dx, xo):
         if t is not None:
-            ld = _rows("dxo, dx and xo", t, T, d, f32)
+            ld = _rows("dxo, dx and xo", t, T, d, _F32)
             if ldx is not None and ld != ldx:
                 raise ValueError("dxo, dx and xo must have one row stride")
             ldx = ld
@@ -292,10 +303,9 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
         ldx = d
     if dx is None:
         dx = torch.empty_strided((T, d), (ldx, 1), dtype=torch.float32, device=dev)
-    tin, ldn, ldy = None, 0, 0
+    tin, ldn, ldy, yp, ys = None, 0, 0, 0, _NONE
     if dn is not None:
         ldn, tin = _rows("dn", dn, T, d, _DT), dn.dtype
-    yp, ys = None, _NONE
     if isinstance(y, Packed):
         ys = _packed("y", y, T, d)
     elif y is not None:
@@ -305,30 +315,28 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
     if post is not None:
         if dy is None:
             dy = torch.empty_strided((T, d), (ldy or d, 1), dtype=dtype or tin, device=dev)
-        l = _rows("dy", dy, T, d, _DT)
-        if yp is not None and l != ldy:
+        ld = _rows("dy", dy, T, d, _DT)
+        if yp and ld != ldy:
             raise ValueError("dy must have y's row stride")
-        ldy = l
+        ldy = ld
     elif dy is not None:
         raise ValueError("dy needs post")
-    g = NormGrads() if grads is None else grads
-    gp = (_vec("grads.w_post", g.w_post, d), _vec("grads.b_post", g.b_post, d), _vec("grads.w_pre", g.w_pre, d),
-          _vec("grads.b_pre", g.b_pre, d))
-    if g.gate is not None and (gate is None or g.gate.shape != gate.shape or g.gate.dtype != torch.float32 or
-                               not g.gate.is_contiguous()):
+    gw, gb, gv, gc, gg = grads or NormGrads()
+    if gg is not None and (gate is None or gg.shape != gate.shape or gg.dtype != torch.float32 or
+                           not gg.is_contiguous()):
         raise ValueError("grads.gate must be a contiguous fp32 tensor like gate")
     if workspace is None:
         workspace = torch.empty(zl.zl_block_norm_workspace(T, d, gate_rows if gate is not None else 0), device=dev)
     elif workspace.dtype != torch.float32 or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous fp32 tensor")
-    _check_device(dev, ("dxo", dxo), ("y", y), ("xo", xo), ("dx", dx), ("dy", dy), ("workspace", workspace),
-                  ("grads.w_post", g.w_post), ("grads.b_post", g.b_post), ("grads.w_pre", g.w_pre),
-                  ("grads.b_pre", g.b_pre), ("grads.gate", g.gate))
-    a = zl.zl_norm_args(T, d, int(layernorm), _DT[tin], zl.ZL_F32 if dy is None else _DT[dy.dtype], eps, scale, *wb,
-                        _ptr(gate), gate_rows, stats.data_ptr(), None, _ptr(xo) if pre is not None else None, ldx, yp,
-                        ldy, None, ldn, ys, _NONE, _ptr(dxo), _ptr(dn), dx.data_ptr(), _ptr(dy), *gp, _ptr(g.gate),
-                        grad_scale, int(accumulate), _ptr(workspace), workspace.numel())
-    _call(zl.zl_block_norm_backward, dev, a)
+    _check_device(dev, "dxo y xo dx dy workspace w_post b_post w_pre b_pre gate", dxo, y, xo, dx, dy, workspace, gw, gb,
+                  gv, gc, gg)
+    _call(zl.zl_block_norm_backward, dev,
+          zl.pack_norm_args(T, d, int(layernorm), _DT[tin], zl.ZL_F32 if dy is None else _DT[dy.dtype], eps, scale,
+                            *params, 0, _ptr(xo), ldx, yp, ldy, 0, ldn, *ys, *_NONE, _ptr(dxo), _ptr(dn), dx.data_ptr(),
+                            _ptr(dy), _vec("grads.w_post", gw, d), _vec("grads.b_post", gb, d),
+                            _vec("grads.w_pre", gv, d), _vec("grads.b_pre", gc, d), _ptr(gg), grad_scale,
+                            int(accumulate), workspace.data_ptr(), workspace.numel()))
     return dx, dy
 
 
@@ -337,17 +345,17 @@ def wgrad(dy, x, out=None, scale=1.0, accumulate=False, workspace=None):
     accumulate); dy [T, n_out], x a Packed [T, n_in].  workspace: fp32 scratch
     that lets a small dw split the sum over T."""
     T, M = dy.shape
-    N = x.n
+    N, dev = x.n, dy.device
     lddy = _rows("dy", dy, T, M, _DT)
-    s = _packed("x", x, T, N)
+    p = zl.pack_packed(*_packed("x", x, T, N))
     if out is None:
-        out = (torch.zeros if accumulate else torch.empty)(M, N, device=dy.device)
-    ld = _rows("out", out, M, N, (torch.float32,))
+        out = (torch.zeros if accumulate else torch.empty)(M, N, device=dev)
+    ld = _rows("out", out, M, N, _F32)
     if workspace is not None and (workspace.dtype != torch.float32 or not workspace.is_contiguous()):
         raise TypeError("workspace must be a contiguous fp32 tensor")
-    _check_device(dy.device, ("x", x), ("out", out), ("workspace", workspace))
-    _call(zl.zl_wgrad_packed, dy.device, T, M, N, dy.data_ptr(), lddy, _DT[dy.dtype], s, out.data_ptr(), ld, scale,
-          accumulate, _ptr(workspace), 0 if workspace is None else workspace.numel())
+    _check_device(dev, "x out workspace", x, out, workspace)
+    _call(zl.zl_wgrad_packed, dev, T, M, N, dy.data_ptr(), lddy, _DT[dy.dtype], p, out.data_ptr(), ld, scale, accumulate,
+          _ptr(workspace), 0 if workspace is None else workspace.numel())
     return out
 
 
@@ -357,17 +365,19 @@ def rotary(x, pos, axis_of, n_heads, head_dim, theta, *, inverse=False, out=None
     the axis of each frequency; 2 len(axis_of) columns of a head are rotated,
     the others copied.  inverse: the gradient's way back.  out may be x."""
     T, W = x.shape[0], n_heads * head_dim
+    dev = x.device
     if x.dim() != 2 or x.shape[1] < W:
         raise ValueError(f"x must be [{T}, >= {W}], not {list(x.shape)}")
-    if x.dtype not in _DT or (x.stride(1) != 1 and W > 1):
+    ldx, s1 = x.stride()
+    if x.dtype not in _DT or (s1 != 1 and W > 1):
         raise TypeError("x must be fp32 or bf16 with contiguous rows")
     if pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape[1] != T or not pos.is_contiguous():
         raise TypeError(f"pos must be a contiguous int32 [axes, {T}] tensor")
-    out = torch.empty(T, W, dtype=x.dtype, device=x.device) if out is None else out
+    out = torch.empty(T, W, dtype=x.dtype, device=dev) if out is None else out
     if out.dtype != x.dtype or out.dim() != 2 or out.shape[0] != T or out.shape[1] < W or out.stride(1) != 1:
         raise ValueError(f"out must be [{T}, >= {W}] of x's type with contiguous rows")
-    _check_device(x.device, ("pos", pos), ("out", out))
-    ldx, ldo = (x.stride(0), out.stride(0)) if T > 1 else (W, W)
-    _call(zl.zl_rotary, x.device, T, n_heads, head_dim, 2 * len(axis_of), x.data_ptr(), ldx, out.data_ptr(), ldo,
-          _DT[x.dtype], pos.data_ptr(), pos.shape[0], axis_of, theta, inverse)
+    _check_device(dev, "pos out", pos, out)
+    ldx, ldo = (ldx, out.stride(0)) if T > 1 else (W, W)
+    _call(zl.zl_rotary, dev, T, n_heads, head_dim, 2 * len(axis_of), x.data_ptr(), ldx, out.data_ptr(), ldo, _DT[x.dtype],
+          pos.data_ptr(), pos.shape[0], axis_of, theta, inverse)
     return out

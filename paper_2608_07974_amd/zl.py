@@ -6,6 +6,7 @@ same name, raising ZlError on a negative status.  Pointers are plain ints
 """
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_lib", "libzl.so")
@@ -118,6 +119,18 @@ class zl_norm_args(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_elems", ctypes.c_size_t)]
 
 
+# The same argument structures as bytes, made in one step (a ctypes structure of 40
+# fields takes three times the launch): functions below take either.
+pack_packed = struct.Struct("@PPqq").pack
+pack_mlp_args = struct.Struct("@qiiiiPq" "PPqq" "PqPqPq").pack
+pack_norm_args = struct.Struct("@qiiiiffPPPPPqPPPqPqPq" "PPqq" "PPqq" "PPPPPPPPPfiPN").pack
+
+
+def _ref(args):
+    """A structure argument as a pointer: bytes of its layout, or a ctypes structure."""
+    return args if type(args) is bytes else ctypes.byref(args)
+
+
 _lib = None
 
 
@@ -172,14 +185,14 @@ def load(path=None):
         "zl_chunk_save": [vp, ctypes.c_char_p, i64, i64, vp],
         "zl_chunk_load": [vp, ctypes.c_char_p, P(i64), P(i64), vp],
         "zl_checkpoint_read_info": [ctypes.c_char_p, P(zl_checkpoint_info)],
-        "zl_pack": [i64, c, vp, i64, c, P(zl_packed), vp],
-        "zl_unpack": [i64, c, P(zl_packed), vp, i64, c, vp],
-        "zl_mlp_act": [P(zl_mlp_args), vp],
-        "zl_mlp_act_backward": [P(zl_mlp_args), vp],
-        "zl_block_norm": [P(zl_norm_args), vp],
-        "zl_block_norm_backward": [P(zl_norm_args), vp],
+        "zl_pack": [i64, c, vp, i64, c, vp, vp],
+        "zl_unpack": [i64, c, vp, vp, i64, c, vp],
+        "zl_mlp_act": [vp, vp],
+        "zl_mlp_act_backward": [vp, vp],
+        "zl_block_norm": [vp, vp],
+        "zl_block_norm_backward": [vp, vp],
         "zl_block_norm_workspace": [i64, c, i64, P(sz)],
-        "zl_wgrad_packed": [i64, c, c, vp, i64, c, P(zl_packed), ctypes.c_float, c, vp, i64, vp, sz,
+        "zl_wgrad_packed": [i64, c, c, vp, i64, c, vp, ctypes.c_float, c, vp, i64, vp, sz,
                             vp],
         "zl_rotary": [i64, c, c, c, vp, i64, vp, i64, c, vp, c, ctypes.c_char_p, ctypes.c_double, c,
                       vp],
@@ -415,27 +428,27 @@ def zl_checkpoint_read_info(path):
 
 
 def zl_pack(T, n, x, ldx, dtype, out, stream=0):
-    _check(load().zl_pack(T, n, x, ldx, dtype, ctypes.byref(out), stream), "zl_pack")
+    _check(load().zl_pack(T, n, x, ldx, dtype, _ref(out), stream), "zl_pack")
 
 
 def zl_unpack(T, n, packed, x, ldx, dtype, stream=0):
-    _check(load().zl_unpack(T, n, ctypes.byref(packed), x, ldx, dtype, stream), "zl_unpack")
+    _check(load().zl_unpack(T, n, _ref(packed), x, ldx, dtype, stream), "zl_unpack")
 
 
 def zl_mlp_act(args, stream=0):
-    _check(load().zl_mlp_act(ctypes.byref(args), stream), "zl_mlp_act")
+    _check(load().zl_mlp_act(_ref(args), stream), "zl_mlp_act")
 
 
 def zl_mlp_act_backward(args, stream=0):
-    _check(load().zl_mlp_act_backward(ctypes.byref(args), stream), "zl_mlp_act_backward")
+    _check(load().zl_mlp_act_backward(_ref(args), stream), "zl_mlp_act_backward")
 
 
 def zl_block_norm(args, stream=0):
-    _check(load().zl_block_norm(ctypes.byref(args), stream), "zl_block_norm")
+    _check(load().zl_block_norm(_ref(args), stream), "zl_block_norm")
 
 
 def zl_block_norm_backward(args, stream=0):
-    _check(load().zl_block_norm_backward(ctypes.byref(args), stream), "zl_block_norm_backward")
+    _check(load().zl_block_norm_backward(_ref(args), stream), "zl_block_norm_backward")
 
 
 def zl_block_norm_workspace(T, d, gate_rows=0):
@@ -448,7 +461,7 @@ def zl_block_norm_workspace(T, d, gate_rows=0):
 
 def zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, x, dw, lddw, scale=1.0, accumulate=0,
                     workspace=None, workspace_elems=0, stream=0):
-    _check(load().zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, ctypes.byref(x), scale,
+    _check(load().zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, _ref(x), scale,
                                   int(accumulate), dw, lddw, workspace, workspace_elems, stream),
            "zl_wgrad_packed")
 
@@ -459,7 +472,8 @@ def zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes, a
     if rot > 0 and len(axis_of) < rot // 2:
         raise ValueError(f"axis_of must hold rot / 2 = {rot // 2} axis numbers")
     _check(load().zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes,
-                            bytes(axis_of), theta, int(inverse), stream), "zl_rotary")
+                            axis_of if type(axis_of) is bytes else bytes(axis_of), theta, int(inverse),
+                            stream), "zl_rotary")
 
 
 def zl_profile_end(h, max_entries=256):

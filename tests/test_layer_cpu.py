@@ -159,12 +159,44 @@ def test_structures_match_the_header():
     assert ctypes.sizeof(zl.zl_norm_args) == 8 + 24 + 6 * 8 + 8 + 7 * 8 + 64 + 9 * 8 + 8 + 16
 
 
+def test_packed_bytes_are_the_structures():
+    """The one-step byte forms of the argument structures hold the same bytes as
+    the structures filled field by field."""
+    def values(cls, at):
+        out = []
+        for _, ty in cls._fields_:
+            if ty is zl.zl_packed:
+                v, sub = values(ty, at)
+                out += sub
+                at = v
+            else:
+                at += 1
+                out.append(at + 0.5 if ty is ctypes.c_float else at)
+        return at, out
+
+    def filled(cls, vals):
+        args = []
+        for _, ty in cls._fields_:
+            args.append(filled(ty, vals) if ty is zl.zl_packed else vals.pop(0))
+        return cls(*args)
+
+    for cls, pack in ((zl.zl_packed, zl.pack_packed), (zl.zl_mlp_args, zl.pack_mlp_args), (zl.zl_norm_args, zl.pack_norm_args)):
+        vals = values(cls, 100)[1]
+        assert pack(*vals) == bytes(filled(cls, list(vals)))
+    # and the library reads them
+    _refused(INV, zl.zl_pack, 4, 64, A, 64, zl.ZL_F32, zl.pack_packed(0, A, 64, 2))
+    _refused(INV, zl.zl_pack, 4, 64, A, 64, zl.ZL_F32, zl.pack_packed(A, A, 72, 2))
+    _refused(UNS, zl.zl_mlp_act, zl.pack_mlp_args(4, 40, 0, 1, 1, A, 80, A, A, 80, 3, A, 40, 0, 0, 0, 0))
+
+
 def test_torch_layer_refuses_host_tensors_and_bad_shapes():
     """The torch functions check what the library cannot see: placement,
     shapes, types, overlapping rows."""
     x = torch.zeros(4, 64)
     with pytest.raises(ValueError, match="GPU"):
         layer.pack(x, out=layer.Packed.empty(4, 64, "cpu"))
+    with pytest.raises(ValueError, match="out must be on"):
+        layer._check_device(torch.device("cuda", 0), "x out", None, x)
     with pytest.raises(ValueError):
         layer.pack(x, out=layer.Packed.empty(3, 64, "cpu"))
     with pytest.raises(TypeError):
