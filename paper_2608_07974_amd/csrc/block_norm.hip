@@ -202,7 +202,11 @@ hipError_t launch_block_norm(const zl_norm_args& a, hipStream_t s) {
 // adds those.  What the norm after the block sums needs the gate row only once
 // for a run of rows that share it: with S1 = sum D yh and S0 = sum D,
 //   dgate = scale (w_post S1 + b_post S0),  dw_post = scale gate S1,  db_post = scale gate S0.
-// MULTI: a slot has several gate rows (whole ones) and adds up the latter two.
+// MODE 0: a slot's rows share a gate row (or have none).  1: a slot has whole gate
+// rows, short ones, and adds up the latter two; dgate is its own to write.  2: a
+// slot's rows go through all of a few long gate rows, with a partial dgate of
+// each (16384 x 4096, 4 gate rows: 215 us; in mode 0, which reads four places at a
+// time, 232, and 223 with twice the blocks).
 // The next row is loaded while this one is reduced; LEAN (registers short):
 // the row is read when it is due, weights and gate once per row (from the caches).
 template <bool BI, bool PK> struct RawY : Raw8<BI> {
@@ -212,13 +216,13 @@ template <bool BI> struct RawY<BI, true> : RawP {
   __device__ __forceinline__ void fetch(const zl_norm_args& a, int64_t r, uint32_t c) { this->load(a.y_packed, r, c); }
 };
 
-template <int NT, int G, bool LEAN, bool MULTI, bool LN, bool BI, bool PK>
+template <int NT, int G, bool LEAN, int MODE, bool LN, bool BI, bool PK>
 __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, NormPlan pl) {
   constexpr int NW = NT / 64;
   __shared__ float red[2][2][NW];
   __shared__ float comb[G == 1 ? 3 * 64 * PW : 1];  // slots 1 ..: 3 of one wave or 1 of two
-  // LEAN and MULTI: the sums over gate rows, touched once per gate row, lie in LDS
-  constexpr bool SL = LEAN && MULTI;
+  // LEAN: the sums over gate rows, touched once per gate row, lie in LDS
+  constexpr bool SL = LEAN && MODE == 1;
   __shared__ float sq[SL ? (LN ? 2 : 1) * G * PW * NT : 1];
   // waves of a slot, this wave's slot and its place there
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = NW / pl.slots, slot = wave / nw, lane = threadIdx.x & 63;
@@ -232,8 +236,8 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
     ok[k] = (int)col[k] < a.d;
   }
   // this slot's first row, the end of what it shares, and the rows from a unit
-  // of `unit` rows (one gate row where MULTI) to this slot's next
-  const int64_t unit = MULTI ? a.gate_rows : 1;
+  // of `unit` rows (one gate row in mode 1) to this slot's next
+  const int64_t unit = MODE == 1 ? a.gate_rows : 1;
   int64_t r0, end, step;
   if (pl.group > 0) {
     const int64_t gi = blockIdx.x / pl.cpg, ci = blockIdx.x % pl.cpg;
@@ -252,7 +256,7 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
     t.get(v);
   };
   float wp[G][PW], wq[G][PW], gt[G][PW];  // w_pre, w_post, scale * gate
-  // gradient sums: of the norm before the next block, S1 and S0, and MULTI's own
+  // gradient sums: of the norm before the next block, S1 and S0, and over gate rows
   float swp[G][PW], sbp[G][PW], s1[G][PW], s0[G][PW], swq[G][PW], sbq[G][PW];
   auto load_gate = [&](int64_t r) __attribute__((always_inline)) {
 #pragma unroll
@@ -276,11 +280,12 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
       if (SL && LN) sq[((G + k) * PW + i) * NT + threadIdx.x] = 0.f;
     }
   }
-  if (!LEAN && !MULTI && a.gate && r0 < end) load_gate(r0);
+  if (!LEAN && MODE == 0 && a.gate && r0 < end) load_gate(r0);
   Raw8<false> nd[G], nx[G];
   Raw8<BI> nn[G];
   RawY<BI, PK> ny[G];
   float4 nst;
+  constexpr bool LATE = LEAN && MODE == 1 && LN && !BI;  // registers shortest: y when it is due
   auto fetch = [&](int64_t r) __attribute__((always_inline)) {
     nst = *reinterpret_cast<const float4*>(a.stats + r * 4);
 #pragma unroll
@@ -291,7 +296,7 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
         nx[k].load(a.xo, r * a.ldx, col[k]);
         nn[k].load(a.dn, r * a.ldn, col[k]);
       }
-      if (post) ny[k].fetch(a, r, col[k]);
+      if (post && !LATE) ny[k].fetch(a, r, col[k]);
     }
   };
   nst = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -323,11 +328,28 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
   };
   if (!LEAN && r0 < end) fetch(r0);
   int64_t r = r0, at_unit = 0;  // this round's row and its place in its unit
+  // mode 2: whether this is the slot's first row of a gate row, which, and the row behind it
+  bool fresh = true;
+  int64_t gate_row = -1, gate_end = 0;
+  // t += f scale (w_post S1 + b_post S0)
+  auto gate_grad = [&](int k, float f, float (&t)[PW]) __attribute__((always_inline)) {
+    float w[PW], b[PW];
+    vec(a.w_post, k, w);
+    vec(LN ? a.b_post : nullptr, k, b);
+#pragma unroll
+    for (int i = 0; i < PW; ++i) t[i] += f * a.scale * (w[i] * s1[k][i] + b[i] * s0[k][i]);
+  };
+  const int64_t pstep = pl.nblk * a.d;  // floats of one array of partial rows
   // every slot takes the same number of rounds (barriers); rows past the end count nothing
   for (int64_t k0 = 0; k0 < pl.rows; ++k0) {
     const bool in = r < end;
-    const bool last = MULTI ? at_unit + 1 == unit || r + 1 >= end : true;  // of its gate row
-    const int64_t next = MULTI && at_unit + 1 < unit ? r + 1 : r + step - (MULTI ? unit - 1 : 0);
+    const int64_t next = MODE == 1 && at_unit + 1 < unit ? r + 1 : r + step - (unit - 1);
+    if (MODE == 2 && in && fresh) {
+      gate_row = r / a.gate_rows;
+      gate_end = (gate_row + 1) * a.gate_rows;
+    }
+    // the slot's last row of its gate row
+    const bool last = MODE == 1 ? at_unit + 1 == unit || r + 1 >= end : next >= gate_end || next >= end;
     if (LEAN && in) fetch(r);
     Raw8<false> rd[G], rx[G];
     Raw8<BI> rn[G];
@@ -341,7 +363,8 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
     }
     const float4 st = nst;
     if (!LEAN && next < end) fetch(next);
-    if (in && a.gate && (LEAN || (MULTI && at_unit == 0))) load_gate(r);
+    if (in && a.gate && (LEAN || (MODE == 1 && at_unit == 0) || (MODE == 2 && fresh))) load_gate(r);
+    if (MODE == 2) fresh = false;
     float dv[G][PW];
 #pragma unroll
     for (int k = 0; k < G; ++k) rd[k].get(dv[k]);
@@ -381,6 +404,7 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
 #pragma unroll
       for (int k = 0; k < G; ++k) {
         if (LEAN) vec(a.w_post, k, wq[k]);
+        if (LATE && in && ok[k]) ry[k].fetch(a, r, col[k]);
         ry[k].get(yv[k]);
 #pragma unroll
         for (int i = 0; i < PW; ++i) {
@@ -407,18 +431,21 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
         }
       }
     }
-    if (MULTI && in && last) {
-      const int64_t o = r / a.gate_rows * a.d;
+    if (MODE != 0 && in && last) {
+      if (MODE == 2) fresh = true;
 #pragma unroll
       for (int k = 0; k < G; ++k) {
         if (a.dgate && ok[k]) {
-          float t[PW], w[PW], b[PW];
-          vec(a.accumulate ? a.dgate + o : nullptr, k, t);
-          vec(a.w_post, k, w);
-          vec(LN ? a.b_post : nullptr, k, b);
-#pragma unroll
-          for (int i = 0; i < PW; ++i) t[i] += a.grad_scale * a.scale * (w[i] * s1[k][i] + b[i] * s0[k][i]);
-          store8<false>(a.dgate, o, col[k], t);
+          float t[PW] = {};
+          if (MODE == 1) {
+            const int64_t o = r / a.gate_rows * a.d;
+            vec(a.accumulate ? a.dgate + o : nullptr, k, t);
+            gate_grad(k, a.grad_scale, t);
+            store8<false>(a.dgate, o, col[k], t);
+          } else {
+            gate_grad(k, 1.f, t);
+            store8<false>(a.workspace, 4 * pstep + ((gate_row * pl.nblk + blockIdx.x) * pl.slots + slot) * a.d, col[k], t);
+          }
         }
 #pragma unroll
         for (int i = 0; i < PW; ++i) {
@@ -433,9 +460,18 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
         }
       }
     }
-    if (MULTI) at_unit = at_unit + 1 < unit ? at_unit + 1 : 0;
+    if (MODE == 1) at_unit = at_unit + 1 < unit ? at_unit + 1 : 0;
     r = next;
   }
+  // a last, shorter gate row that this slot had no row of
+  if (MODE == 2 && a.dgate)
+    for (int64_t g = gate_row + 1; g < pl.gates; ++g)
+#pragma unroll
+      for (int k = 0; k < G; ++k) {
+        const float none[PW] = {};
+        if (ok[k])
+          store8<false>(a.workspace, 4 * pstep + ((g * pl.nblk + blockIdx.x) * pl.slots + slot) * a.d, col[k], none);
+      }
   // the slots' sums, then this block's partial row `which`
   auto finish = [&](int which, int k, float (&v)[PW]) __attribute__((always_inline)) {
     if (G == 1 && pl.slots > 1) {
@@ -449,9 +485,9 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
 #pragma unroll
         for (int i = 0; i < PW; ++i) v[i] += comb[((t - 1) * PW + i) * nw * 64 + tid];
     }
-    if (ok[k]) store8<false>(a.workspace, (which * pl.nblk + blockIdx.x) * a.d, col[k], v);
+    if (ok[k]) store8<false>(a.workspace, which * pstep + blockIdx.x * (int64_t)a.d, col[k], v);
   };
-  if (!MULTI && LEAN && a.gate && r0 < end) load_gate(r0);
+  if (MODE == 0 && LEAN && a.gate && r0 < end) load_gate(r0);
 #pragma unroll
   for (int k = 0; k < G; ++k) {
     if (a.dw_pre) finish(0, k, swp[k]);
@@ -459,7 +495,7 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
     if (!post) continue;
 #pragma unroll
     for (int i = 0; i < PW; ++i) {
-      if (!MULTI) {
+      if (MODE == 0) {
         swq[k][i] = gt[k][i] * s1[k][i];
         sbq[k][i] = gt[k][i] * s0[k][i];
       } else if (SL) {
@@ -469,12 +505,9 @@ __global__ void __launch_bounds__(NT) block_norm_bwd_kernel(zl_norm_args a, Norm
     }
     if (a.dw_post) finish(2, k, swq[k]);
     if (LN && a.db_post) finish(3, k, sbq[k]);
-    if (!MULTI && a.dgate) {
-      float w[PW], b[PW], t[PW];
-      vec(a.w_post, k, w);
-      vec(LN ? a.b_post : nullptr, k, b);
-#pragma unroll
-      for (int i = 0; i < PW; ++i) t[i] = a.scale * (w[i] * s1[k][i] + b[i] * s0[k][i]);
+    if (MODE == 0 && a.dgate) {
+      float t[PW] = {};
+      gate_grad(k, 1.f, t);
       finish(4, k, t);
     }
   }
@@ -492,8 +525,8 @@ __global__ void __launch_bounds__(1024) block_norm_reduce_kernel(zl_norm_args a,
   const float* part = a.workspace + (task < 4 ? task : 4) * step;
   int64_t n = pl.nblk;
   if (task >= 4) {
-    n = pl.cpg;
-    part += (task - 4) * pl.cpg * a.d;
+    n = pl.group > 0 ? pl.cpg : pl.nblk * pl.slots;
+    part += (task - 4) * n * a.d;
     out += (int64_t)(task - 4) * a.d;
   }
   const int cl = threadIdx.x & 31, grp = threadIdx.x >> 5;
@@ -519,22 +552,31 @@ __global__ void __launch_bounds__(1024) block_norm_reduce_kernel(zl_norm_args a,
 }
 
 NormPlan norm_plan(int64_t T, int d, int64_t gate_rows) {
-  if (T <= 0) return {0, 0, 0, 0, 1};
   // rows of up to 512 columns: a wave each, four in a block, and so on
   const int slots = d <= 64 * PW ? 4 : d <= 128 * PW ? 2 : 1;
-  // as many blocks as are resident, with 8 rows each at least (partial rows cost
-  // what two rows cost) until there are fewer blocks than CUs
-  int64_t blocks = 256 * (d <= 256 * PW ? 3 : d <= 512 * PW ? 2 : 1);
+  NormPlan p = {0, 0, 0, 0, 0, 0, slots};
+  if (T <= 0) return p;
+  // as many blocks as are resident or half as many more rounds of them would gain
+  // (2048 columns and fewer: three a CU measured 66.4 us at 8192 x 2048 where two
+  // take 62.6, above one and two at 16384 x 4096 220 and 227), with 8 rows each at
+  // least (partial rows cost what two rows cost) until there are fewer than CUs
+  int64_t blocks = d <= 256 * PW ? 512 : 256;
   if (blocks > T / 8) blocks = T / 8;
   const int64_t most = (T + slots - 1) / slots;
   if (blocks < 256) blocks = most < 256 ? most : 256;
-  NormPlan p = {0, (T + blocks * slots - 1) / (blocks * slots), 0, 0, slots};
+  p.rows = (T + blocks * slots - 1) / (blocks * slots);
   if (gate_rows > T) gate_rows = T;
-  if (gate_rows >= p.rows * slots) {
+  const int64_t gates = gate_rows > 0 ? (T + gate_rows - 1) / gate_rows : 0;
+  // (above 4096 columns mode 2 lacks the registers for the next row: 4096 x 8192 157 us, 136 in mode 0)
+  if (gates > 1 && gates <= 16 && gate_rows >= 4 * blocks * slots && d <= 512 * PW) {
+    p.nblk = (T + p.rows * slots - 1) / (p.rows * slots);
+    p.gates = gates;
+    p.gate_part = gates * p.nblk * slots;
+  } else if (gate_rows >= p.rows * slots) {
     p.group = gate_rows;
     p.cpg = (gate_rows + p.rows * slots - 1) / (p.rows * slots);
     p.rows = (gate_rows + p.cpg * slots - 1) / (p.cpg * slots);
-    p.nblk = (T + gate_rows - 1) / gate_rows * p.cpg;
+    p.nblk = p.gate_part = gates * p.cpg;
   } else {
     if (gate_rows > 0) p.rows = p.rows > gate_rows ? p.rows / gate_rows * gate_rows : gate_rows;
     p.nblk = (T + p.rows * slots - 1) / (p.rows * slots);
@@ -542,26 +584,28 @@ NormPlan norm_plan(int64_t T, int d, int64_t gate_rows) {
   return p;
 }
 
-template <int NT, int G, bool LEAN, bool MULTI, bool LN>
+template <int NT, int G, bool LEAN, int MODE, bool LN>
 static void norm_bwd_types(const zl_norm_args& a, const NormPlan& pl, hipStream_t s) {
   const dim3 g((unsigned)pl.nblk), b(NT);
   const bool bi = a.in_dtype == ZL_BF16, pk = a.w_post && a.y_packed.codes;
   constexpr bool L32 = LEAN || G == 2;  // fp32 dn and y: twice the registers of a row in flight
-  if (bi && pk) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MULTI, LN, true, true>), g, b, 0, s, a, pl);
-  else if (bi) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MULTI, LN, true, false>), g, b, 0, s, a, pl);
-  else if (pk) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MULTI, LN, false, true>), g, b, 0, s, a, pl);
-  else hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, L32, MULTI, LN, false, false>), g, b, 0, s, a, pl);
+  if (bi && pk) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MODE, LN, true, true>), g, b, 0, s, a, pl);
+  else if (bi) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MODE, LN, true, false>), g, b, 0, s, a, pl);
+  else if (pk) hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, LEAN, MODE, LN, false, true>), g, b, 0, s, a, pl);
+  else hipLaunchKernelGGL((block_norm_bwd_kernel<NT, G, L32, MODE, LN, false, false>), g, b, 0, s, a, pl);
 }
 
 template <int NT, int G>
 static void norm_bwd_go(const zl_norm_args& a, const NormPlan& pl, hipStream_t s) {
-  const bool multi = a.gate && a.w_post && pl.group == 0;
+  const int mode = !a.gate || pl.group > 0 ? 0 : pl.gates > 0 ? 2 : 1;
   if (a.layernorm) {
-    if (multi) norm_bwd_types<NT, G, G == 2, true, true>(a, pl, s);
-    else norm_bwd_types<NT, G, G == 2, false, true>(a, pl, s);
+    if (mode == 0) norm_bwd_types<NT, G, G == 2, 0, true>(a, pl, s);
+    else if (mode == 1) norm_bwd_types<NT, G, G == 2, 1, true>(a, pl, s);
+    else if constexpr (G == 1) norm_bwd_types<NT, G, false, 2, true>(a, pl, s);
   } else {
-    if (multi) norm_bwd_types<NT, G, G == 2, true, false>(a, pl, s);
-    else norm_bwd_types<NT, G, false, false, false>(a, pl, s);
+    if (mode == 0) norm_bwd_types<NT, G, false, 0, false>(a, pl, s);
+    else if (mode == 1) norm_bwd_types<NT, G, G == 2, 1, false>(a, pl, s);
+    else if constexpr (G == 1) norm_bwd_types<NT, G, false, 2, false>(a, pl, s);
   }
 }
 
@@ -582,9 +626,10 @@ hipError_t launch_block_norm_bwd(const zl_norm_args& a, hipStream_t s) {
   else norm_bwd_go<512, 2>(a, pl, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const bool gate = a.dgate && pl.group > 0;
+  const bool gate = a.dgate && pl.gate_part > 0;
   if (!gate && !out[0] && !out[1] && !out[2] && !out[3]) return hipSuccess;
-  const int64_t tasks = 4 + (gate ? pl.nblk / pl.cpg : 0);  // fewer than the blocks, a few thousand
+  // one task per gate row with partial rows: fewer than the blocks, a few thousand
+  const int64_t tasks = 4 + (!gate ? 0 : pl.group > 0 ? pl.nblk / pl.cpg : pl.gates);
   hipLaunchKernelGGL(block_norm_reduce_kernel, dim3((a.d + 31) / 32, (unsigned)tasks), dim3(1024), 0, s, a, pl);
   return hipGetLastError();
 }

@@ -143,7 +143,8 @@ static zl_status check_norm(const zl_norm_args* a, bool backward) {
 
 zl_status zl_block_norm_workspace(int64_t T, int d, int64_t gate_rows, size_t* elems) {
   if (T < 0 || !cols_ok(d) || gate_rows < 0 || !elems) return bad("bad block norm workspace args");
-  *elems = (size_t)norm_plan(T, d, gate_rows).nblk * d * 5;
+  const NormPlan p = norm_plan(T, d, gate_rows);
+  *elems = (size_t)(4 * p.nblk + p.gate_part) * d;
   return ZL_OK;
 }
 zl_status zl_block_norm(const zl_norm_args* args, void* stream) {
@@ -200,7 +201,7 @@ zl_status zl_rotary(int64_t T, int n_heads, int head_dim, int rot, const void* x
   a.sign = inverse ? -1.f : 1.f;
   a.vec = rot % 16 == 0 && head_dim % 8 == 0 && ldx % 8 == 0 && ldo % 8 == 0 && aligned(x) && aligned(out);
   // powers by products of 64-bit fractions: 128 of them are off by less than the
-  // rounding to double, and cost a fifth of as many pow
+  // rounding to double, and cost less than as many pow (0.2 us for 64, 1.5)
   const long double step = powl((long double)theta, -2.0L / rot);
   long double turn = 0.5L / 3.14159265358979323846264338327950288L;
   for (int j = 0; j < a.half; ++j, turn *= step) {

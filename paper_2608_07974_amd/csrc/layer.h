@@ -21,10 +21,11 @@ hipError_t launch_mlp(const zl_mlp_args& a, bool backward, hipStream_t s);
 hipError_t launch_block_norm(const zl_norm_args& a, hipStream_t s);
 // How the backward's blocks take the rows: nblk blocks of `slots` slots; every
 // slot has up to `rows` rows, each slot in turn one of them.  group > 0: every
-// `group` rows (one gate row) have cpg blocks of their own; else, with a gate, a
-// turn is the rows of one gate row, and `rows` a multiple of them.
+// `group` rows (one gate row) have cpg blocks of their own.  gates > 0: all blocks
+// go through that many gate rows.  Else, with a gate, a turn is the rows of one
+// gate row, and `rows` a multiple of them.  gate_part: partial rows of dgate.
 struct NormPlan {
-  int64_t nblk, rows, group, cpg;
+  int64_t nblk, rows, group, cpg, gates, gate_part;
   int slots;
 };
 NormPlan norm_plan(int64_t T, int d, int64_t gate_rows);

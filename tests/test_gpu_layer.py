@@ -285,7 +285,9 @@ _NORM_CASES = [  # T, d, gate rows, parts, pad
     (17, 2056, 17, "both", 0), (2100, 520, 700, "both", 0), (2100, 1000, 3, "both", 0), (2051, 2048, 0, "both", 0),
     (40, 4104, 2, "both", 0), (9, 4096, 0, "post", 0), (50, 1024, 25, "post", 0), (9, 4096, 0, "pre", 0),
     (2048, 512, 0, "pre", 16), (3000, 136, 1000, "both", 0), (700, 8, 64, "both", 0),
-    (3, 72, 1000, "both", 0), (1000, 520, 1500, "both", 0), (4500, 64, 5, "both", 0), (1030, 8192, 300, "both", 0)]
+    (3, 72, 1000, "both", 0), (1000, 520, 1500, "both", 0), (4500, 64, 5, "both", 0), (520, 8192, 130, "both", 0),
+(9000, 72, 4100, "both", 0), (4098, 520, 4097, "both", 0), (4099, 1032, 2049, "both", 0),
+    (2111, 2056, 1055, "post", 0), (2100, 2056, 1050, "both", 0)]
 
 
 @pytest.mark.parametrize("ln", [False, True])

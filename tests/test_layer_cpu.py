@@ -108,13 +108,13 @@ def test_block_norm_refuses_more():
 
 
 def test_block_norm_workspace_is_bounded():
-    """Five partial rows per block, of a number of blocks that does not grow
-    with the rows."""
+    """Four partial rows per block and some of the gate's, of a number of blocks
+    that does not grow with the rows."""
     for T in (0, 1, 5, 255, 256, 4096, 16384, 1000000):
         for d in (8, 768, 4096, 8192):
-            for rows in (0, 1, 7, 64, 1000, T, 2 * T + 1):
-                blocks = zl.zl_block_norm_workspace(T, d, rows) // (5 * d)
-                assert min(T, 1) <= blocks <= min(2 * T, 2200), (T, d, rows)
+            for rows in (0, 1, 7, 64, 1000, 5000, T, 2 * T + 1):
+                part = zl.zl_block_norm_workspace(T, d, rows) // d
+                assert 4 * min(T, 1) <= part <= min(10 * T, 45000), (T, d, rows)
     for args in ((-1, 64, 0), (4, 60, 0), (4, 64, -1)):
         _refused(INV, zl.zl_block_norm_workspace, *args)
 
