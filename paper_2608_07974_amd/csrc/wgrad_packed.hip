@@ -186,7 +186,7 @@ struct CodeTile {
   }
 };
 
-// NST LDS stages of 32 tokens and as many register sets of codes.  In the last
+// NST LDS stages of BK tokens and as many register sets of codes.  In the last
 // slice of tile kt, behind the barrier that releases its stage: x of tile kt + NST
 // goes from its registers into the stage, the codes of tile kt + 2 NST are
 // loaded in their place, and dy of tile kt + NST starts on its way.  Codes before
@@ -195,15 +195,15 @@ struct CodeTile {
 // compile-time (16384 x 14336 x 4096: 1609 us, 1669 with a run-time stage); tiles
 // past the end are zeros by the buffers' ends, without a test per load (1519 us;
 // the bf16 GEMM of that size 1529, both at 1.26 - 1.27 PFLOP/s).
-template <int BM, int BN, int WM, int WN, int NST>
+template <int BM, int BN, int WM, int WN, int BK, int NST>
 __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, EpiArgs e, zl_packed x) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int BK = 32, MF = 32, NT = WM * WN * 64;
+  constexpr int MF = 32, NT = WM * WN * 64;
   constexpr int TM = BM / WM, TN = BN / WN, FM = TM / MF, FN = TN / MF, NS = BK / Mma<MF>::KS, NMF = FM * FN;
   constexpr uint32_t ABYTES = BM * BK * 2, STAGE = (BM + BN) * BK * 2;
   using TA = DmaTile<BM, BK, NT, false, MF>;
   constexpr int PER_TILE = TA::ITEMS + 2;
-  static_assert(NS == 2 && NMF >= 4 && NST >= 3 && (NST - 2) * PER_TILE < 64, "schedule");
+  static_assert(NS % 2 == 0 && NMF >= 2 && NST >= 3 && (NST - 2) * PER_TILE < 64, "schedule");
 
   int tm, tn;
   tile_coords(blockIdx.x, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN, tm, tn);
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, Ep
       const bf16_t* an = reinterpret_cast<const bf16_t*>(smem + (u + 1 < NST ? u + 1 : 0) * STAGE);
 #pragma unroll
       for (int q = 0; q < NS; ++q) {
-        const int cb = q, nb = q ^ 1;
+        const int cb = q & 1, nb = cb ^ 1;
         const bf16_t* src = q + 1 < NS ? as : an;
         const int qs = q + 1 < NS ? q + 1 : 0;
         if (q + 1 == NS) {
@@ -292,8 +292,8 @@ __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, Ep
           }
           if (q + 1 == NS) {
             if (t < 2) tb.store_half(c[u], sc[u], smem + u * STAGE + ABYTES, t);
-            if (t == 2) tb.load(c[u], sc[u], (kt + 2 * NST) * BK, rc, rs);
-            if (t == 3) copy_dy(lds0 + u * STAGE, (kt + NST) * BK);
+            if (t == min(2, NMF - 1)) tb.load(c[u], sc[u], (kt + 2 * NST) * BK, rc, rs);
+            if (t == min(3, NMF - 1)) copy_dy(lds0 + u * STAGE, (kt + NST) * BK);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -305,10 +305,11 @@ __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, Ep
   store_tile<BM, BN, WM, WN, MF>(acc, smem, g, e, m0, n0, wave, lane);
 }
 
-template <int BM, int BN, int WM, int WN, int NST>
+template <int BM, int BN, int WM, int WN, int BK, int NST>
 static hipError_t wgrad_mfma(const GemmDesc& g, const EpiArgs& e, const zl_packed& x, int nz, hipStream_t s) {
-  auto kern = wgrad_mfma_kernel<BM, BN, WM, WN, NST>;
-  const size_t main = (size_t)NST * (BM + BN) * 32 * sizeof(bf16_t), epi = (size_t)WM * WN * 32 * (BN / WN + 4) * sizeof(float);
+  auto kern = wgrad_mfma_kernel<BM, BN, WM, WN, BK, NST>;
+  const size_t main = (size_t)NST * (BM + BN) * BK * sizeof(bf16_t);
+  const size_t epi = (size_t)WM * WN * 32 * (BN / WN + 4) * sizeof(float);
   const size_t lds = main > epi ? main : epi;
   hipError_t err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (err != hipSuccess) return err;
@@ -332,7 +333,13 @@ static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accu
   EpiArgs e = grad_epi(a);
   e.accumulate = accumulate;
   const GemmPlan plan = plan_gemm({a.M, a.N, T, false, false, a.part != nullptr, a.part_elems, false, 0});
-  const int nz = split_k(T, plan.nz, 32, g.ksplit);
+  // One block of eight waves a CU, 64 tokens a stage, where no CU would get a second
+  // block and the splits would be short: 512 x 768 x 768 9.6 us, split 11.2;
+  // 2048 x 2048 x 2048 25.2 against 26.5 with four waves.  More tiles: 512 x 4096 x
+  // 2048 23.8 against 20.3; more tokens to split: 1024 x 256 x 256 13.1 against 11.0.
+  const int64_t tiles = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
+  const bool deep = !plan.large && tiles <= 256 && (plan.nz == 1 || T <= 768);
+  const int nz = split_k(T, deep ? 1 : plan.nz, 32, g.ksplit);
   EpiArgs ep = e;
   if (nz > 1) {
     memset(&ep, 0, sizeof(ep));
@@ -345,8 +352,9 @@ static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accu
   }
   // 4 stages for large tiles (3: 1526 us at 16384 x 14336 x 4096, 5: 1534), 3 for
   // small ones, which share a CU (4096 x 2304 x 768: 32.8; 4 stages 33.5, 8 42.2)
-  hipError_t err = plan.large ? wgrad_mfma<256, 256, 4, 2, 4>(g, ep, x, nz, s)
-                              : wgrad_mfma<128, 128, 2, 2, 3>(g, ep, x, nz, s);
+  hipError_t err = plan.large ? wgrad_mfma<256, 256, 4, 2, 32, 4>(g, ep, x, nz, s)
+                   : deep     ? wgrad_mfma<128, 128, 4, 2, 64, 3>(g, ep, x, nz, s)
+                              : wgrad_mfma<128, 128, 2, 2, 32, 3>(g, ep, x, nz, s);
   if (err != hipSuccess || nz == 1) return err;
   return launch_splitk_reduce(a.part, nz, a.M, a.N, e, s);
 }
