@@ -609,7 +609,9 @@ static void norm_bwd_go(const zl_norm_args& a, const NormPlan& pl, hipStream_t s
   }
 }
 
-hipError_t launch_block_norm_bwd(const zl_norm_args& a, hipStream_t s) {
+hipError_t launch_block_norm_bwd(const zl_norm_args& args, hipStream_t s) {
+  zl_norm_args a = args;
+  if (a.gate_rows > a.T) a.gate_rows = a.T;  // one gate row; products with it stay within 64 bits
   float* const out[4] = {a.dw_pre, a.db_pre, a.dw_post, a.db_post};
   if (a.T <= 0) {  // sums over no rows
     for (float* o : out)

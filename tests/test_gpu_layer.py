@@ -439,6 +439,23 @@ def test_block_norm_empty_batch():
     assert layer.rotary(e, torch.empty(1, 0, dtype=torch.int32, device="cuda"), bytes(8), 4, 16, 1e4).shape == (0, d)
 
 
+@pytest.mark.parametrize("T,d", [(1, 64), (3, 64), (5, 1000), (40, 64), (300, 2048), (9, 8192)])
+@pytest.mark.parametrize("rows", [(1 << 63) - 1, 1 << 62, 1 << 61])
+def test_one_gate_row_for_any_number_of_rows(T, d, rows):
+    layer = _L()
+    rng = _rng("gate", T, d)
+    x, y, post, pre, gate = _norm_case(rng, T, d, True, "both", T, BF)
+    xt, yt, gt = _dev(x, F32), _dev(y, BF), _vec(gate)
+    got = []
+    for n in (T, rows):
+        kw = dict(gate=gt, gate_rows=n, scale=0.75, layernorm=True)
+        xo, nn, st = layer.block_norm(xt, yt, _tv(post), _tv(pre), **kw)
+        g = layer.NormGrads(*(torch.empty(d, device="cuda") for _ in range(4)), torch.empty(1, d, device="cuda"))
+        got.append([xo, nn, st, *layer.block_norm_bwd(xt, nn, yt, xo, st, _tv(post), _tv(pre), grads=g, **kw), *g])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 # ---------------------------------------------------------- weight gradient
 @pytest.mark.parametrize("dt", [F32, BF])
 @pytest.mark.parametrize("T,M,N,pad", [(1, 8, 8, 0), (33, 72, 40, 16), (31, 256, 256, 0), (32, 264, 48, 0), (64, 128, 1000, 0),
