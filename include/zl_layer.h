@@ -9,7 +9,8 @@
  * device.  Matrices are row-major with a row stride (ld, in elements); a
  * contiguous dimension is a multiple of 8 elements, a row stride too, and
  * pointers are 16-byte aligned (ZL_ERR_INVALID_ARG otherwise), unless a call
- * says less.  Buffers overlap only where a call says so.  T = 0 is an empty
+ * says less; a matrix has at most 2^30 columns (ZL_ERR_UNSUPPORTED above) and a
+ * launch at most 2^32 threads (ZL_ERR_HIP above).  Buffers overlap only where a call says so.  T = 0 is an empty
  * batch: nothing is read, sums over rows are zero.  No call allocates memory;
  * all may be captured into a graph, and results do not depend on timing (no
  * atomics: every sum has a fixed order). */

@@ -167,7 +167,7 @@ static void norm_fwd_types(const zl_norm_args& a, dim3 g, hipStream_t s) {
 template <int NW, int G>
 static hipError_t norm_fwd_go(const zl_norm_args& a, hipStream_t s) {
   const int64_t nb = (a.T + 4 / NW - 1) / (4 / NW);
-  if (nb > 0x7fffffff) return hipErrorInvalidValue;
+  if (nb > MAX_BLOCKS) return hipErrorInvalidValue;
   // xo, n and the copies
   const int64_t out = a.T * a.d * ((a.w_post ? 4 : 0) + (a.w_pre ? (a.out_dtype == ZL_BF16 ? 2 : 4) : 0) +
                                    (a.y_packed.codes ? 1 : 0) + (a.n_packed.codes ? 1 : 0));

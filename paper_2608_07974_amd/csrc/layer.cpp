@@ -35,6 +35,9 @@ bool packed_ok(const zl_packed& p, int64_t n, int64_t T) {
                     p.ld_scales >= (n + 31) / 32);
 }
 bool cols_ok(int n) { return n > 0 && n % 8 == 0; }
+// column numbers, rounded up to a block's columns, stay within 32 bits
+bool wide(int64_t n) { return n > (int64_t)1 << 30; }
+zl_status too_wide() { return set_error(ZL_ERR_UNSUPPORTED, "more than 2^30 columns"); }
 
 const char* kCols = "columns must be a positive multiple of 8";
 const char* kMat = "matrix missing, not 16-byte aligned, or a bad row stride";
@@ -49,6 +52,7 @@ zl_status zl_pack(int64_t T, int n, const void* x, int64_t ldx, int dtype, const
   if (T < 0 || !out) return bad("bad pack args");
   if (!dtype_ok(dtype)) return bad("bad dtype");
   if (!cols_ok(n)) return bad(kCols);
+  if (wide(n)) return too_wide();
   if (!mat_ok(x, ldx, n, T)) return bad(kMat);
   if (!packed_ok(*out, n, T)) return bad(kPacked);
   return done(launch_pack(T, n, x, ldx, dt_of(dtype), *out, (hipStream_t)stream), "pack");
@@ -58,6 +62,7 @@ zl_status zl_unpack(int64_t T, int n, const zl_packed* in, void* x, int64_t ldx,
   if (T < 0 || !in) return bad("bad unpack args");
   if (!dtype_ok(dtype)) return bad("bad dtype");
   if (!cols_ok(n)) return bad(kCols);
+  if (wide(n)) return too_wide();
   if (!mat_ok(x, ldx, n, T)) return bad(kMat);
   if (!packed_ok(*in, n, T)) return bad(kPacked);
   return done(launch_unpack(T, n, *in, x, ldx, dt_of(dtype), (hipStream_t)stream), "unpack");
@@ -69,6 +74,7 @@ static zl_status check_mlp(const zl_mlp_args* a, bool backward) {
   if (!dtype_ok(a->in_dtype) || !dtype_ok(a->out_dtype)) return bad("bad dtype");
   if (!cols_ok(a->ff)) return bad(kCols);
   const int64_t nh = (a->kind == ZL_MLP_SWIGLU ? 2 : 1) * (int64_t)a->ff;
+  if (wide(nh)) return too_wide();
   const bool pk = a->packed.codes != nullptr;
   if (pk && a->kind == ZL_MLP_SWIGLU && a->ff % 32)
     return set_error(ZL_ERR_UNSUPPORTED, "SwiGLU with a packed h needs ff to be a multiple of 32");
@@ -163,6 +169,7 @@ zl_status zl_wgrad_packed(int64_t T, int n_out, int n_in, const void* dy, int64_
   if (T > 0x7fffffff) return set_error(ZL_ERR_UNSUPPORTED, "more than 2^31 - 1 tokens");
   if (!dtype_ok(dtype)) return bad("bad dtype");
   if (!cols_ok(n_out) || !cols_ok(n_in)) return bad(kCols);
+  if (wide(n_out) || wide(n_in)) return too_wide();
   if (!mat_ok(dy, lddy, n_out, T) || !mat_ok(dw, lddw, n_in, 1)) return bad(kMat);
   if (!packed_ok(*x, n_in, T)) return bad(kPacked);
   if (!aligned(workspace)) return bad("workspace must be 16-byte aligned");

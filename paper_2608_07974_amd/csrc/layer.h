@@ -11,6 +11,9 @@ namespace zl {
 // output and input stream past the caches.
 int streaming(int64_t out, int64_t in);
 
+// Blocks of 256 threads that one launch takes: fewer than 2^32 threads.
+constexpr int64_t MAX_BLOCKS = (1 << 24) - 1;
+
 hipError_t launch_pack(int64_t T, int n, const void* x, int64_t ldx, int dtype, const zl_packed& out,
                        hipStream_t s);
 hipError_t launch_unpack(int64_t T, int n, const zl_packed& in, void* x, int64_t ldx, int dtype,

@@ -110,7 +110,7 @@ static hipError_t launch_rows(const RowGrid& g, int nt, F&& f) {
   if (g.T <= 0) return hipSuccess;
   const bool one = few(g);
   const int64_t b = row_blocks(g, one ? 1 : U);
-  if (b > 0x7fffffff) return hipErrorInvalidValue;
+  if (b > MAX_BLOCKS) return hipErrorInvalidValue;
   const dim3 grid((unsigned)b);
   if (one) f(grid, Int<1>{}, Int<0>{});
   else if (nt == 0) f(grid, Int<U>{}, Int<0>{});
@@ -335,7 +335,7 @@ template <bool BF, int V>
 static hipError_t rotary_go(const RotaryArgs& a, hipStream_t s) {
   const int tb = LT / a.half;
   const int64_t bx = (a.T + tb - 1) / tb;
-  if (bx > 0x7fffffff) return hipErrorInvalidValue;
+  if (bx > MAX_BLOCKS) return hipErrorInvalidValue;
   // fewer than two blocks per CU: heads spread over blocks, whole lanes' worth
   // of pairs each
   int by = 1;

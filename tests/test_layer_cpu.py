@@ -71,6 +71,19 @@ def test_mlp_refuses_more():
         _refused(UNS, zl.zl_mlp_act_backward if back else zl.zl_mlp_act, _mlp(back, **kw))
 
 
+def test_more_columns_than_numbers_of_32_bits():
+    n = (1 << 30) + 32
+    p, io = _pk(n), dict(ldh=n, lda=n)
+    _refused(UNS, zl.zl_pack, 1, n, A, n, zl.ZL_BF16, p)
+    _refused(UNS, zl.zl_unpack, 1, n, p, A, n, zl.ZL_BF16)
+    _refused(UNS, zl.zl_wgrad_packed, 1, n, 64, A, n, zl.ZL_BF16, _pk(), A, 64)
+    _refused(UNS, zl.zl_wgrad_packed, 1, 64, n, A, 64, zl.ZL_BF16, p, A, n)
+    for back in (False, True):
+        fn, bw = (zl.zl_mlp_act_backward, dict(ldda=n, lddh=n)) if back else (zl.zl_mlp_act, {})
+        _refused(UNS, fn, _mlp(back, T=1, ff=n, kind=zl.ZL_MLP_GELU, **io, **bw))
+        _refused(UNS, fn, _mlp(back, T=1, ff=n // 2, **io, **bw))
+
+
 def _norm(back, **kw):
     a = dict(T=4, d=64, layernorm=0, in_dtype=zl.ZL_BF16, out_dtype=zl.ZL_BF16, eps=1e-5, scale=1.0, w_post=A, w_pre=A,
              gate=A, gate_rows=4, stats=A, xo=A, ldx=64, y=A, ldy=64, ldn=64)
