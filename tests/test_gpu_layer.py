@@ -483,6 +483,21 @@ def test_wgrad(dt, T, M, N, pad, ws):
         assert torch.isnan(dw.as_strided((M, pad), (dw.stride(0), 1), N)).all()
 
 
+@pytest.mark.parametrize("dt", [F32, BF])
+def test_one_row_of_any_stride(dt):
+    from paper_2608_07974_amd import zl
+    layer = _L()
+    rng = _rng("stride")
+    dy, x = _dev(rng.standard_normal((1, 136)), dt), _packed(_acts(rng, 1, 264))
+    ref, out = layer.wgrad(dy, x), torch.full((136, 264), float("nan"), device="cuda")
+    for ld in (1 << 30, 1 << 31, 1 << 62):
+        p = zl.zl_packed(x.codes.data_ptr(), x.scales.data_ptr(), ld, ld)
+        zl.zl_wgrad_packed(1, 136, 264, dy.data_ptr(), ld, zl.ZL_BF16 if dt == BF else zl.ZL_F32, p, out.data_ptr(), 264,
+                           stream=torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(out, ref)
+        out.fill_(float("nan"))
+
+
 def test_wgrad_non_finite_stays_in_its_column():
     """A NaN code and an infinite gradient reach their column and row only."""
     layer = _L()
