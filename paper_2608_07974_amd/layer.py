@@ -87,7 +87,8 @@ def _call(fn, dev, *args):
 
 class Packed:
     """A matrix [T, n] in 8 bits: `codes` uint8 [T, >= n rounded up to 16] and
-    `scales` uint8 [T, >= ceil(n / 32)], both with contiguous rows."""
+    `scales` uint8 [T, >= ceil(n / 32)], both with contiguous rows.  Their strides are
+    read once: for other tensors make another Packed."""
 
     __slots__ = ("codes", "scales", "n", "_ld")
 
