@@ -246,7 +246,7 @@ def block_norm(x, y, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5, 
     T, d = x.shape
     dev = x.device
     ldx = _rows("x", x, T, d, _F32)
-    stats = torch.empty(T, 4, device=dev) if stats is None else stats
+    stats = torch.empty(T, 4, dtype=torch.float32, device=dev) if stats is None else stats
     params = _norm_common(d, T, dev, post, pre, gate, gate_rows, stats)
     if (y is None) != (post is None):
         raise ValueError("y and post go together")
@@ -327,7 +327,8 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
                            not gg.is_contiguous()):
         raise ValueError("grads.gate must be a contiguous fp32 tensor like gate")
     if workspace is None:
-        workspace = torch.empty(zl.zl_block_norm_workspace(T, d, gate_rows if gate is not None else 0), device=dev)
+        workspace = torch.empty(zl.zl_block_norm_workspace(T, d, gate_rows if gate is not None else 0),
+                                dtype=torch.float32, device=dev)
     elif workspace.dtype != torch.float32 or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous fp32 tensor")
     _check_device(dev, "dxo y xo dx dy workspace w_post b_post w_pre b_pre gate", dxo, y, xo, dx, dy, workspace, gw, gb,
@@ -350,7 +351,7 @@ def wgrad(dy, x, out=None, scale=1.0, accumulate=False, workspace=None):
     lddy = _rows("dy", dy, T, M, _DT)
     p = zl.pack_packed(*_packed("x", x, T, N))
     if out is None:
-        out = (torch.zeros if accumulate else torch.empty)(M, N, device=dev)
+        out = (torch.zeros if accumulate else torch.empty)(M, N, dtype=torch.float32, device=dev)
     ld = _rows("out", out, M, N, _F32)
     if workspace is not None and (workspace.dtype != torch.float32 or not workspace.is_contiguous()):
         raise TypeError("workspace must be a contiguous fp32 tensor")

@@ -667,6 +667,27 @@ def test_captured_and_on_another_stream():
         assert all(torch.equal(x, y) for x, y in zip(again, want_b))
 
 
+def test_torchs_default_type_does_not_matter():
+    """With bf16 as torch's default type, tensors and scratch that the calls make
+    themselves are what they are without: the results, bit for bit."""
+    layer = _L()
+    s = _some(layer, 5)
+
+    def calls():
+        xo, n, st = layer.block_norm(s["x"], s["y"], s["w"], s["w"], gate=s["gate"], gate_rows=40)
+        g = layer.NormGrads(*(None if t is None else torch.empty_like(t) for t in s["g"]))
+        dxy = layer.block_norm_bwd(s["x"], n, s["y"], xo, st, s["w"], s["w"], gate=s["gate"], gate_rows=40, grads=g)
+        return [xo, n, st, *dxy, *(t for t in g if t is not None), layer.wgrad(s["y"], layer.pack(s["x"]))]
+
+    want = calls()
+    torch.set_default_dtype(torch.bfloat16)
+    try:
+        got = calls()
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert all(a.dtype == b.dtype and torch.equal(a, b) for a, b in zip(got, want))
+
+
 # ------------------------------------------------------------ a whole layer
 def test_a_layer_with_packed_activations():
     """One decoder layer with norms around both blocks, gated residuals and

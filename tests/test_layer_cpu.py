@@ -254,3 +254,39 @@ def test_torch_layer_refuses_host_tensors_and_bad_shapes():
         layer.rotary(x, torch.zeros(3, 5, dtype=torch.int32), bytes(8), 4, 16, 1e4)
     with pytest.raises(ValueError):
         layer.rotary(x, torch.zeros(3, 4, dtype=torch.int32), bytes(8), 5, 16, 1e4)
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    """The torch functions up to the library's call, on host tensors; returns the
+    list of calls (the library's function and its arguments)."""
+    calls = []
+    monkeypatch.setattr(layer, "_check_device", lambda *a: None)
+    monkeypatch.setattr(layer, "_call", lambda fn, dev, *args: calls.append((fn, args)))
+    return calls
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float16, torch.float64])
+def test_tensors_made_here_have_types_of_their_own(on_host, monkeypatch, default):
+    """Whatever torch's default type: the workspace has the bytes of the floats that
+    the library is told of, statistics and gradients are fp32."""
+    made, empty = [], torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: made.append(empty(*a, **kw)) or made[-1])
+    f32 = dict(dtype=torch.float32)
+    x, w = torch.zeros(512, 256, **f32), (torch.ones(256, **f32), None)
+    torch.set_default_dtype(default)
+    try:
+        _, n, stats = layer.block_norm(x, x, w, w)
+        dx, dy = layer.block_norm_bwd(x, x, x, x, stats, w, w)
+        dws = [layer.wgrad(x, layer.Packed.empty(512, 64, "cpu"), accumulate=a) for a in (False, True)]
+        others = [layer.pack(x).codes, layer.unpack(layer.Packed.empty(4, 64, "cpu")), layer.mlp_act(x), layer.mlp_act_bwd(x, x[:, :128])]
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert all(t.dtype == torch.float32 for t in (n, stats, dx, dy, *dws))
+    assert [t.dtype for t in others] == [torch.uint8, torch.bfloat16, torch.float32, torch.float32]
+    fn, (args,) = on_host[1]
+    args = zl.zl_norm_args.from_buffer_copy(args)
+    ws, = (t for t in made if t.data_ptr() == args.workspace)
+    need = zl.zl_block_norm_workspace(512, 256)
+    assert fn is zl.zl_block_norm_backward and args.workspace_elems >= need > 0
+    assert ws.numel() * ws.element_size() >= 4 * args.workspace_elems
