@@ -361,13 +361,14 @@ static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accu
 
 hipError_t launch_wgrad_packed(const WgradArgs& a, int dtype, hipStream_t s) {
   if (dtype != BF16) return wgrad_f32<false>(a, s);
+  if (a.T == 0) return wgrad_f32<true>(a, s);  // zeros, or dw as it is; strides may be anything
   // tokens per launch: the largest offset from a tile's origin stays below 2^31
   const int64_t dyb = a.lddy < (int64_t)1 << 31 ? 2 * a.lddy : a.lddy;  // (beyond, `most` is negative either way)
   const int64_t row = dyb > a.x.ld_codes ? dyb : a.x.ld_codes;
   const int64_t top = row > a.x.ld_scales ? row : a.x.ld_scales;
   const int64_t most = (((int64_t)1 << 31) - 1024) / top - 1024;
-  if (a.T > 0 && a.T <= most) return wgrad_segment(a, 0, (int)a.T, a.accumulate != 0, s);
-  if (a.T == 0 || most < 4096) return wgrad_f32<true>(a, s);
+  if (a.T <= most) return wgrad_segment(a, 0, (int)a.T, a.accumulate != 0, s);
+  if (most < 4096) return wgrad_f32<true>(a, s);
   const int64_t step = most / 32 * 32;
   for (int64_t t = 0; t < a.T; t += step) {
     const int64_t n = a.T - t < step ? a.T - t : step;

@@ -439,6 +439,20 @@ def test_block_norm_empty_batch():
     assert layer.rotary(e, torch.empty(1, 0, dtype=torch.int32, device="cuda"), bytes(8), 4, 16, 1e4).shape == (0, d)
 
 
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("ld", [0, -8, 1 << 62])
+def test_wgrad_of_no_tokens(dt, ld):
+    """No tokens, no operands, any strides: zeros written, nothing added."""
+    from paper_2608_07974_amd import zl
+    for acc in (0, 1):
+        dw = torch.full((64, 72), 3.0, device="cuda")
+        zl.zl_wgrad_packed(0, 64, 72, 0, ld, zl.ZL_BF16 if dt == BF else zl.ZL_F32, zl.zl_packed(0, 0, ld, ld), dw.data_ptr(), 72,
+                           accumulate=acc, stream=torch.cuda.current_stream().cuda_stream)
+        assert (dw == 3.0 * acc).all()
+    e = torch.empty(0, 64, dtype=_dt(dt), device="cuda")
+    assert (_L().wgrad(e, _L().Packed.empty(0, 72)) == 0).all()
+
+
 @pytest.mark.parametrize("T,d", [(1, 64), (3, 64), (5, 1000), (40, 64), (300, 2048), (9, 8192)])
 @pytest.mark.parametrize("rows", [(1 << 63) - 1, 1 << 62, 1 << 61])
 def test_one_gate_row_for_any_number_of_rows(T, d, rows):

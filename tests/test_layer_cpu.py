@@ -1,6 +1,9 @@
 """Refusals of the layer operators (include/zl_layer.h): every call here is
 turned down on the host, before anything is launched (no GPU)."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -290,3 +293,21 @@ def test_tensors_made_here_have_types_of_their_own(on_host, monkeypatch, default
     need = zl.zl_block_norm_workspace(512, 256)
     assert fn is zl.zl_block_norm_backward and args.workspace_elems >= need > 0
     assert ws.numel() * ws.element_size() >= 4 * args.workspace_elems
+
+
+@pytest.mark.parametrize("dtype", ["ZL_F32", "ZL_BF16"])
+@pytest.mark.parametrize("ld", [0, -8, 1 << 62])
+def test_wgrad_of_no_tokens_reads_no_stride(dtype, ld):
+    """T = 0: operands and strides may be anything.  In a process of its own that
+    sees no GPU, where the launch is what fails."""
+    code = f"""
+from paper_2608_07974_amd import zl
+try:
+    zl.zl_wgrad_packed(0, 64, 64, 0, {ld}, zl.{dtype}, zl.zl_packed(0, 0, {ld}, {ld}), {A}, 64)
+except zl.ZlError as e:
+    print("status", e.status)
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, env=dict(os.environ, HIP_VISIBLE_DEVICES="-1"),
+                       capture_output=True, text=True, timeout=120)
+    assert (r.returncode, r.stdout.split()) == (0, ["status", str(zl.ZL_ERR_HIP)]), (r.returncode, r.stdout, r.stderr)
