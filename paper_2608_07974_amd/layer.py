@@ -85,35 +85,41 @@ def _call(fn, dev, *args):
             fn(*args, _raw_stream(dev.index))
 
 
+def _packed_rows(codes, scales, n):
+    """Row strides of both tensors of a packed matrix, everything of them checked."""
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2:
+        raise TypeError("codes and scales must be uint8 matrices")
+    (T, W), (Ts, Ws), c16, c32 = codes.shape, scales.shape, _up(n, 16), (n + 31) // 32
+    if W < c16 or Ts != T or Ws < c32:
+        raise ValueError(f"codes and scales must be [{T}, >= {c16}] and [{T}, >= {c32}], not [{T}, {W}] and [{Ts}, {Ws}]")
+    if codes.device != scales.device:
+        raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
+    if codes.is_contiguous() and scales.is_contiguous():
+        return (W, Ws) if T > 1 else (c16, c32)
+    (lc, c1), (ls, s1) = codes.stride(), scales.stride()
+    if (c1 != 1 and W > 1) or (s1 != 1 and Ws > 1):
+        raise ValueError("codes and scales must have contiguous rows")
+    if T > 1 and (lc < c16 or ls < c32):
+        raise ValueError("codes and scales must not overlap themselves")
+    return (lc, ls) if T > 1 else (c16, c32)
+
+
 class Packed:
     """A matrix [T, n] in 8 bits: `codes` uint8 [T, >= n rounded up to 16] and
-    `scales` uint8 [T, >= ceil(n / 32)], both with contiguous rows.  Their strides are
-    read once: for other tensors make another Packed."""
+    `scales` uint8 [T, >= ceil(n / 32)], both with contiguous rows.  Every call takes
+    the two tensors as they are then."""
 
-    __slots__ = ("codes", "scales", "n", "_ld")
+    __slots__ = ("codes", "scales", "n")
 
     def __init__(self, codes, scales, n):
-        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2:
-            raise TypeError("codes and scales must be uint8 matrices")
-        (T, W), (Ts, Ws), c16, c32 = codes.shape, scales.shape, _up(n, 16), (n + 31) // 32
-        if W < c16 or Ts != T or Ws < c32:
-            raise ValueError(f"codes and scales must be [{T}, >= {c16}] and [{T}, >= {c32}], not [{T}, {W}] and [{Ts}, {Ws}]")
-        if codes.is_contiguous() and scales.is_contiguous():
-            self._ld = (W, Ws) if T > 1 else (c16, c32)
-        else:
-            (lc, c1), (ls, s1) = codes.stride(), scales.stride()
-            if (c1 != 1 and W > 1) or (s1 != 1 and Ws > 1):
-                raise ValueError("codes and scales must have contiguous rows")
-            if T > 1 and (lc < c16 or ls < c32):
-                raise ValueError("codes and scales must not overlap themselves")
-            self._ld = (lc, ls) if T > 1 else (c16, c32)
-        if codes.device != scales.device:
-            raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
+        _packed_rows(codes, scales, n)
         self.codes, self.scales, self.n = codes, scales, n
 
     def fields(self):
         """The matrix as the library takes it: pointers and row strides."""
-        return (self.codes.data_ptr(), self.scales.data_ptr()) + self._ld
+        codes, scales = self.codes, self.scales
+        ld = _packed_rows(codes, scales, self.n)
+        return (codes.data_ptr(), scales.data_ptr()) + ld
 
     @classmethod
     def empty(cls, T, n, device="cuda"):

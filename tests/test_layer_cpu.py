@@ -311,3 +311,44 @@ except zl.ZlError as e:
     r = subprocess.run([sys.executable, "-c", code], cwd=root, env=dict(os.environ, HIP_VISIBLE_DEVICES="-1"),
                        capture_output=True, text=True, timeout=120)
     assert (r.returncode, r.stdout.split()) == (0, ["status", str(zl.ZL_ERR_HIP)]), (r.returncode, r.stdout, r.stderr)
+
+
+def test_packed_follows_its_tensors():
+    """Tensors of a Packed that are replaced, resized or given other strides: the
+    call takes them as they are then, or refuses them."""
+    u8 = dict(dtype=torch.uint8)
+    new = lambda: layer.Packed(torch.zeros(4, 64, **u8), torch.zeros(4, 2, **u8), 64)  # noqa: E731
+    p = new()
+    wide = torch.zeros(4, 160, **u8)
+    p.codes, p.scales = wide[:, 32:96], torch.zeros(4, 8, **u8)[:, 3:5]
+    assert p.fields() == (wide.data_ptr() + 32, p.scales.data_ptr(), 160, 8)
+    assert layer._packed("p", p, 4, 64) == p.fields()
+    p = new()
+    p.codes.resize_(4, 80)
+    p.scales.set_(torch.zeros(4, 5, **u8))
+    assert p.fields()[2:] == (80, 5)
+
+    def refused(change, error=ValueError, match=None):
+        p = new()
+        change(p)
+        with pytest.raises(error, match=match):
+            p.fields()
+
+    refused(lambda p: setattr(p, "codes", torch.zeros(4, 48, **u8)))
+    refused(lambda p: setattr(p, "codes", torch.zeros(3, 64, **u8)))
+    refused(lambda p: setattr(p, "codes", torch.zeros(64, 4, **u8).t()), match="contiguous rows")
+    refused(lambda p: setattr(p, "codes", torch.zeros(1, 64, **u8).expand(4, 64)), match="overlap")
+    refused(lambda p: setattr(p, "codes", torch.zeros(4, 64)), TypeError)
+    refused(lambda p: setattr(p, "codes", torch.zeros(4, 4, 64, **u8)), TypeError)
+    refused(lambda p: setattr(p, "scales", torch.zeros(4, 1, **u8)))
+    refused(lambda p: setattr(p, "scales", torch.zeros(4, 2, device="meta", **u8)), match="scales on meta")
+    refused(lambda p: setattr(p, "n", 72))
+    refused(lambda p: p.codes.resize_(4, 32))
+    refused(lambda p: p.codes.resize_(0), TypeError)
+    refused(lambda p: p.scales.resize_(2, 2))
+    refused(lambda p: p.codes.t_())
+    with pytest.raises(ValueError):
+        p = new()
+        p.codes.resize_(3, 64)
+        p.scales.resize_(3, 2)
+        layer._packed("p", p, 4, 64)
