@@ -5,6 +5,7 @@ same name, raising ZlError on a negative status.  Pointers are plain ints
 (device addresses); streams are hipStream_t handles as ints (0 = default).
 """
 import ctypes
+import operator
 import os
 import struct
 
@@ -468,12 +469,14 @@ def zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, x, dw, lddw, scale=1.0, acc
 
 def zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes, axis_of, theta,
               inverse=0, stream=0):
-    """axis_of: bytes, one axis number per frequency (rot / 2 of them)."""
+    """axis_of: bytes or another sequence of integers, one axis number per
+    frequency (rot / 2 of them)."""
+    if type(axis_of) is not bytes:  # bytes() of an array would take its memory, of whatever type
+        axis_of = bytes(map(operator.index, axis_of))
     if rot > 0 and len(axis_of) < rot // 2:
         raise ValueError(f"axis_of must hold rot / 2 = {rot // 2} axis numbers")
     _check(load().zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes,
-                            axis_of if type(axis_of) is bytes else bytes(axis_of), theta, int(inverse),
-                            stream), "zl_rotary")
+                            axis_of, theta, int(inverse), stream), "zl_rotary")
 
 
 def zl_profile_end(h, max_entries=256):

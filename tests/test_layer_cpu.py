@@ -5,6 +5,7 @@ import os
 import subprocess
 import sys
 
+import numpy as np
 import pytest
 
 from paper_2608_07974_amd import zl
@@ -352,3 +353,31 @@ def test_packed_follows_its_tensors():
         p.codes.resize_(3, 64)
         p.scales.resize_(3, 2)
         layer._packed("p", p, 4, 64)
+
+
+@pytest.mark.parametrize("make", [bytes, list, tuple, bytearray, lambda a: memoryview(bytes(a)), np.array, torch.tensor,
+                                  lambda a: np.array(a, np.int32), lambda a: np.array(a, np.uint8),
+                                  lambda a: np.array([a, a]).T[:, 0], lambda a: torch.tensor(a, dtype=torch.uint8)])
+def test_rotary_takes_axis_numbers_one_by_one(monkeypatch, make):
+    """Axis numbers in any sequence of integers: their values, not their memory."""
+    axes, seen = [0, 1, 2, 0, 1, 2, 2, 1], []
+
+    class Lib:
+        @staticmethod
+        def zl_rotary(*a):
+            seen.append(a[11])
+            return zl.ZL_OK
+
+    monkeypatch.setattr(zl, "load", lambda: Lib)
+    monkeypatch.setattr(layer, "_check_device", lambda *a: None)
+    monkeypatch.setattr(layer, "_call", lambda fn, dev, *args: fn(*args, 0))
+    zl.zl_rotary(4, 4, 16, 16, A, 64, A, 64, zl.ZL_BF16, A, 3, make(axes), 1e4)
+    layer.rotary(torch.zeros(4, 64), torch.zeros(3, 4, dtype=torch.int32), make(axes), 4, 16, 1e4)
+    assert seen == [bytes(axes)] * 2
+
+
+@pytest.mark.parametrize("axes", [[0.0] * 8, np.zeros(8), np.zeros((8, 2), np.int64), [0] * 7 + [256], [0] * 7 + [-1], "01201201",
+                                  torch.zeros(8), [0] * 7, np.zeros(7, np.int64), torch.tensor([3])])
+def test_rotary_refuses_other_axis_numbers(axes):
+    with pytest.raises((TypeError, ValueError)):
+        zl.zl_rotary(4, 4, 16, 16, A, 64, A, 64, zl.ZL_BF16, A, 3, axes, 1e4)
