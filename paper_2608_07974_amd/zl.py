@@ -428,12 +428,18 @@ def zl_checkpoint_read_info(path):
     return {n: getattr(info, n) for n, _ in zl_checkpoint_info._fields_}
 
 
+def _int(n):
+    """A size for an int argument.  ctypes would drop the upper bits of one that does
+    not fit, so that goes in as a size that the library refuses too."""
+    return n if -0x80000000 <= n <= 0x7ffffff8 else 0x7ffffff8 if n > 0 else -8
+
+
 def zl_pack(T, n, x, ldx, dtype, out, stream=0):
-    _check(load().zl_pack(T, n, x, ldx, dtype, _ref(out), stream), "zl_pack")
+    _check(load().zl_pack(T, _int(n), x, ldx, dtype, _ref(out), stream), "zl_pack")
 
 
 def zl_unpack(T, n, packed, x, ldx, dtype, stream=0):
-    _check(load().zl_unpack(T, n, _ref(packed), x, ldx, dtype, stream), "zl_unpack")
+    _check(load().zl_unpack(T, _int(n), _ref(packed), x, ldx, dtype, stream), "zl_unpack")
 
 
 def zl_mlp_act(args, stream=0):
@@ -455,14 +461,14 @@ def zl_block_norm_backward(args, stream=0):
 def zl_block_norm_workspace(T, d, gate_rows=0):
     """Floats of workspace of zl_block_norm_backward."""
     n = ctypes.c_size_t()
-    _check(load().zl_block_norm_workspace(T, d, gate_rows, ctypes.byref(n)),
+    _check(load().zl_block_norm_workspace(T, _int(d), gate_rows, ctypes.byref(n)),
            "zl_block_norm_workspace")
     return n.value
 
 
 def zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, x, dw, lddw, scale=1.0, accumulate=0,
                     workspace=None, workspace_elems=0, stream=0):
-    _check(load().zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, _ref(x), scale,
+    _check(load().zl_wgrad_packed(T, _int(n_out), _int(n_in), dy, lddy, dtype, _ref(x), scale,
                                   int(accumulate), dw, lddw, workspace, workspace_elems, stream),
            "zl_wgrad_packed")
 
@@ -475,8 +481,8 @@ def zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes, a
         axis_of = bytes(map(operator.index, axis_of))
     if rot > 0 and len(axis_of) < rot // 2:
         raise ValueError(f"axis_of must hold rot / 2 = {rot // 2} axis numbers")
-    _check(load().zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes,
-                            axis_of, theta, int(inverse), stream), "zl_rotary")
+    _check(load().zl_rotary(T, _int(n_heads), _int(head_dim), _int(rot), x, ldx, out, ldo, dtype, pos,
+                            _int(n_axes), axis_of, theta, int(inverse), stream), "zl_rotary")
 
 
 def zl_profile_end(h, max_entries=256):

@@ -381,3 +381,28 @@ def test_rotary_takes_axis_numbers_one_by_one(monkeypatch, make):
 def test_rotary_refuses_other_axis_numbers(axes):
     with pytest.raises((TypeError, ValueError)):
         zl.zl_rotary(4, 4, 16, 16, A, 64, A, 64, zl.ZL_BF16, A, 3, axes, 1e4)
+
+
+def test_numbers_of_more_than_32_bits(monkeypatch):
+    """Sizes whose lower 32 bits alone would pass are refused."""
+    n = (1 << 32) + 64
+    wide = _pk(n)
+    _refused(UNS, zl.zl_pack, 1, n, A, n, zl.ZL_BF16, wide)
+    _refused(UNS, zl.zl_unpack, 1, n, wide, A, n, zl.ZL_BF16)
+    _refused(UNS, zl.zl_wgrad_packed, 1, n, 64, A, n, zl.ZL_BF16, _pk(), A, 64)
+    _refused(UNS, zl.zl_wgrad_packed, 1, 64, n, A, 64, zl.ZL_BF16, wide, A, n)
+    _refused(INV, zl.zl_pack, 1, -n, A, n, zl.ZL_BF16, wide)
+    _refused(INV, zl.zl_pack, 1, 64 - (1 << 32), A, n, zl.ZL_BF16, wide)
+    ok = dict(T=4, n_heads=4, head_dim=16, rot=16, x=A, ldx=1 << 40, out=A, ldo=1 << 40, dtype=zl.ZL_BF16, pos=A, n_axes=3,
+              axis_of=bytes(8), theta=1e4)
+    for key in ("n_heads", "head_dim", "rot", "n_axes"):
+        with pytest.raises((zl.ZlError, ValueError)) as e:
+            zl.zl_rotary(**{**ok, key: (1 << 32) + ok[key]})
+        assert getattr(e.value, "status", INV) in (INV, UNS)
+    assert zl.zl_block_norm_workspace(4, n) > zl.zl_block_norm_workspace(4, 1 << 20)
+    monkeypatch.setattr(layer, "_check_device", lambda *a: None)
+    monkeypatch.setattr(layer, "_raw_stream", lambda i: 0)
+    monkeypatch.setattr(layer, "_one_gpu", True)
+    x = torch.empty(1, n, dtype=torch.bfloat16, device="meta")
+    _refused(UNS, layer.pack, x)
+    _refused(UNS, layer.unpack, layer.Packed.empty(1, n, "meta"))
