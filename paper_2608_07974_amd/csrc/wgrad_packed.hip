@@ -17,7 +17,7 @@ namespace zl {
 // BT x BT tiles of four waves, v_mfma_f32_32x32x2_f32 on fp32 tiles of 2048 / BT
 // tokens in LDS; the next tile is loaded and the one after it widened while
 // this one is multiplied (one barrier per tile).  64-bit addresses: also what
-// bf16 dy takes whose rows lie too far apart for buffer offsets.  A block has
+// bf16 dy takes whose rows lie too far apart for the buffer offsets of 512 tokens.  A block has
 // tokens [z per, (z + 1) per); with splits it writes fp32 partials.  Registers for
 // three blocks a CU: 256 x 4096 x 8192 154 us (two: 173; 64 x 64 tiles on the vector
 // ALUs: 224).
@@ -362,13 +362,16 @@ static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accu
 hipError_t launch_wgrad_packed(const WgradArgs& a, int dtype, hipStream_t s) {
   if (dtype != BF16) return wgrad_f32<false>(a, s);
   if (a.T == 0) return wgrad_f32<true>(a, s);  // zeros, or dw as it is; strides may be anything
-  // tokens per launch: the largest offset from a tile's origin stays below 2^31
+  // tokens per launch: the largest offset from a tile's origin stays below 2^31.  As
+  // many launches as it takes while each has 512 tokens and more (4096 x 262144 x 4096,
+  // two of them: 8.8 ms, by 64-bit addresses and fp32 tiles 66; 4096 x 690000 x 1024,
+  // nine: 12.7 and 44), which rows of up to 699050 gradients have.
   const int64_t dyb = a.lddy < (int64_t)1 << 31 ? 2 * a.lddy : a.lddy;  // (beyond, `most` is negative either way)
   const int64_t row = dyb > a.x.ld_codes ? dyb : a.x.ld_codes;
   const int64_t top = row > a.x.ld_scales ? row : a.x.ld_scales;
   const int64_t most = (((int64_t)1 << 31) - 1024) / top - 1024;
   if (a.T <= most) return wgrad_segment(a, 0, (int)a.T, a.accumulate != 0, s);
-  if (most < 4096) return wgrad_f32<true>(a, s);
+  if (most < 512) return wgrad_f32<true>(a, s);
   const int64_t step = most / 32 * 32;
   for (int64_t t = 0; t < a.T; t += step) {
     const int64_t n = a.T - t < step ? a.T - t : step;

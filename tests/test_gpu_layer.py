@@ -565,6 +565,27 @@ def test_wgrad_in_segments_of_tokens():
         del dy, got
 
 
+@pytest.mark.parametrize("ld,T", [(262144, 3100), (524288, 1400), (690000, 1111)])
+def test_wgrad_of_wide_bf16_rows_stays_on_bf16_tiles(ld, T):
+    """A launch reaches 2^31 bytes, of rows as wide as a large vocabulary a few hundred
+    to a few thousand tokens: as many launches as it takes, each what a call of its
+    own on narrow rows gives, bit for bit (fp32 tiles add up in another order)."""
+    layer = _L()
+    rng = _rng("wide", ld)
+    M, N = 264, 72
+    near = _dev(rng.standard_normal((T, M)), BF)
+    dy = torch.empty(T, ld, dtype=torch.bfloat16, device="cuda")[:, :M]
+    dy.copy_(near)
+    p = _packed(_acts(rng, T, N))
+    step = ((2 ** 31 - 1024) // (2 * ld) - 1024) // 32 * 32
+    assert 256 <= step < T
+    want = torch.zeros(M, N, device="cuda")
+    for t in range(0, T, step):
+        e = min(T, t + step)
+        layer.wgrad(near[t:e], layer.Packed(p.codes[t:e], p.scales[t:e], N), out=want, accumulate=t > 0)
+    assert torch.equal(layer.wgrad(dy, p), want)
+
+
 def test_rows_beyond_32_bit_offsets():
     """Four rows 2^30 bytes and more apart through every other operator."""
     layer = _L()
