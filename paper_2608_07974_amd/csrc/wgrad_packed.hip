@@ -14,18 +14,18 @@
 namespace zl {
 
 // --------------------------------------------------------------- fp32 MFMA
-// BT x BT tiles of four waves, v_mfma_f32_32x32x2_f32 on fp32 tiles of 2048 / BT
-// tokens in LDS; the next tile is loaded and the one after it widened while
-// this one is multiplied (one barrier per tile).  64-bit addresses: also what
-// bf16 dy takes whose rows lie too far apart for the buffer offsets of 512 tokens.  A block has
-// tokens [z per, (z + 1) per); with splits it writes fp32 partials.  Registers for
-// three blocks a CU: 256 x 4096 x 8192 154 us (two: 173; 64 x 64 tiles on the vector
-// ALUs: 224).
+// BT x BT tiles of four waves (nx of them side by side), v_mfma_f32_32x32x2_f32 on
+// fp32 tiles of 2048 / BT tokens in LDS; the next tile is loaded and the one after
+// it widened while this one is multiplied (one barrier per tile).  64-bit
+// addresses: also what bf16 dy takes whose rows lie too far apart for the buffer
+// offsets of 512 tokens.  A block has tokens [z per, (z + 1) per); with splits it
+// writes fp32 partials.  Registers for three blocks a CU: 256 x 4096 x 8192 154 us
+// (two: 173; 64 x 64 tiles on the vector ALUs: 224).
 template <bool BF, int BT>
-__global__ void __launch_bounds__(256, 3) wgrad_f32_kernel(WgradArgs a, int64_t per, bool split) {
+__global__ void __launch_bounds__(256, 3) wgrad_f32_kernel(WgradArgs a, unsigned nx, int64_t per, bool split) {
   constexpr int VK = 2048 / BT, CH = BT / PW, F = BT / 64;  // 32 x 32 blocks per wave and side
   __shared__ __align__(16) float As[2][VK][BT], Bs[2][VK][BT];
-  const int m0 = blockIdx.y * BT, n0 = blockIdx.x * BT;
+  const int m0 = (int)(blockIdx.x / nx) * BT, n0 = (int)(blockIdx.x % nx) * BT;
   const int64_t t0 = blockIdx.z * per, t1 = min(t0 + per, a.T);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // this thread's 8 columns of one token of the tile, of dy and of x
@@ -112,7 +112,7 @@ template <bool BF, int BT>
 static hipError_t wgrad_f32_go(const WgradArgs& a, hipStream_t s) {
   constexpr int VK = 2048 / BT;
   const int64_t nx = (a.N + BT - 1) / BT, ny = (a.M + BT - 1) / BT;
-  if (ny > 65535) return hipErrorInvalidValue;
+  if (nx * ny > MAX_BLOCKS) return hipErrorInvalidValue;
   // splits of at least 256 tokens until there are two blocks per CU, four of the
   // small ones (4096 x 1024 x 2048: 158 us, with two 166)
   int64_t nz = (BT == 128 ? 512 : 1024) / (nx * ny);
@@ -123,7 +123,7 @@ static hipError_t wgrad_f32_go(const WgradArgs& a, hipStream_t s) {
   int64_t per = (a.T + nz - 1) / nz;
   per = (per + VK - 1) / VK * VK;
   nz = a.T > 0 ? (a.T + per - 1) / per : 1;
-  hipLaunchKernelGGL((wgrad_f32_kernel<BF, BT>), dim3((unsigned)nx, (unsigned)ny, (unsigned)nz), dim3(256), 0, s, a, per, nz > 1);
+  hipLaunchKernelGGL((wgrad_f32_kernel<BF, BT>), dim3((unsigned)(nx * ny), 1, (unsigned)nz), dim3(256), 0, s, a, (unsigned)nx, per, nz > 1);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || nz == 1) return e;
   return launch_splitk_reduce(a.part, (int)nz, a.M, a.N, grad_epi(a), s);

@@ -565,6 +565,21 @@ def test_wgrad_in_segments_of_tokens():
         del dy, got
 
 
+@pytest.mark.parametrize("dt,M", [(F32, 65536 * 128 + 8), (BF, 65535 * 128 + 72)])
+def test_wgrad_of_more_than_65535_tile_rows(dt, M):
+    layer = _L()
+    rng = _rng("rows", M)
+    T, N = 3, 8
+    dy = torch.empty(T, M, dtype=_dt(dt), device="cuda")
+    dy.normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    x = _packed(_acts(rng, T, N))
+    dw = layer.wgrad(dy, x, out=torch.full((M, N), float("nan"), device="cuda"))
+    v = torch.from_numpy(ol.values(*_bytes(x, T, N))).cuda()
+    d = dy.double()
+    ref, mag = (sum(a[t][:, None] * b[t] for t in range(T)) for a, b in ((d, v), (d.abs(), v.abs())))
+    assert ((dw - ref).abs() <= (T + 8) * U * mag).all()
+
+
 @pytest.mark.parametrize("ld,T", [(262144, 3100), (524288, 1400), (690000, 1111)])
 def test_wgrad_of_wide_bf16_rows_stays_on_bf16_tiles(ld, T):
     """A launch reaches 2^31 bytes, of rows as wide as a large vocabulary a few hundred

@@ -406,3 +406,20 @@ def test_numbers_of_more_than_32_bits(monkeypatch):
     x = torch.empty(1, n, dtype=torch.bfloat16, device="meta")
     _refused(UNS, layer.pack, x)
     _refused(UNS, layer.unpack, layer.Packed.empty(1, n, "meta"))
+
+
+def test_wgrad_of_more_than_65535_tile_rows():
+    """No limit on rows besides columns and threads: with no GPU the launch fails for
+    the lack of one.  In a process of its own that sees none."""
+    code = f"""
+from paper_2608_07974_amd import zl
+for M in (65536 * 128 + 8, 1 << 30):
+    try:
+        zl.zl_wgrad_packed(3, M, 8, {A}, M, zl.ZL_F32, zl.zl_packed({A}, {A}, 16, 1), {A}, 8)
+    except zl.ZlError as e:
+        print(e)
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, env=dict(os.environ, HIP_VISIBLE_DEVICES="-1"),
+                       capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.count("no ROCm-capable device") == 2, (r.returncode, r.stdout, r.stderr)
