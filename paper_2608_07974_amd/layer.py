@@ -9,8 +9,11 @@ Tensors are 2-D [T, columns], rows contiguous (any row stride that is a
 multiple of 8), bf16 or fp32, all on one GPU; work goes to that GPU's current
 stream.  Shapes, types and placement are checked here (the kernels take them
 on trust), the rest by the library, which raises zl.ZlError.  Output tensors
-may be given (and are returned); else they are made.  autograd does not see
-these calls: a layer calls the backward functions itself.
+may be given (and are returned); else they are made.  autograd does not record
+these calls: a layer calls the backward functions itself.  So in gradient mode a
+matrix that requires a gradient is refused, as are weights, biases and gates that
+autograd computed (as parameters they may require one); tensors that a call
+writes count as changed in place.
 """
 from collections import namedtuple
 
@@ -21,6 +24,7 @@ from . import zl
 _DT = {torch.float32: zl.ZL_F32, torch.bfloat16: zl.ZL_BF16}
 _KIND = {"swiglu": zl.ZL_MLP_SWIGLU, "gelu": zl.ZL_MLP_GELU}
 _NONE = (0, 0, 0, 0)  # no packed matrix
+_NO_WB = (None, None)  # no weight and bias
 _F32 = (torch.float32,)
 
 
@@ -43,8 +47,21 @@ def _check_device(dev, names, *tensors):
             raise ValueError(f"{names.split()[i]} must be on {dev}, not {t.device}")
 
 
+def _no_graph(name):
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name} must not require a gradient: autograd does not record this call (use torch.no_grad(), "
+                         "an autograd.Function, or detach())")
+
+
+# Says of tensors (a list or tuple) that a call wrote them, as torch's in-place
+# functions do: a graph that saved one of them refuses its backward.
+_wrote = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
+
+
 def _rows(name, t, T, n, dtypes):
     """Row stride of a [T, n] matrix with contiguous rows."""
+    if t.requires_grad:
+        _no_graph(name)
     if t.dtype in dtypes and t.shape == (T, n):
         s0, s1 = t.stride()
         if s1 == 1 and s0 >= n and T > 1:
@@ -64,6 +81,8 @@ def _vec(name, t, n):
         return 0
     if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 vector of {n}")
+    if t.requires_grad and not t.is_leaf:
+        _no_graph(name)
     return t.data_ptr()
 
 
@@ -155,6 +174,7 @@ def pack(x, out=None):
     p = zl.pack_packed(*_packed("out", out, T, n))
     _check_device(dev, "out", out)
     _call(zl.zl_pack, dev, T, n, x.data_ptr(), ldx, _DT[x.dtype], p)
+    _wrote((out.codes, out.scales))
     return out
 
 
@@ -166,6 +186,7 @@ def unpack(p, dtype=torch.bfloat16, out=None):
     ld = _rows("out", out, T, n, _DT)
     _check_device(dev, "out", out)
     _call(zl.zl_unpack, dev, T, n, zl.pack_packed(*p.fields()), out.data_ptr(), ld, _DT[out.dtype])
+    _wrote((out,))
     return out
 
 
@@ -192,6 +213,7 @@ def mlp_act(h, kind="swiglu", dtype=None, act=None, packed=None):
     _check_device(dev, "act packed", act, packed)
     _call(zl.zl_mlp_act, dev, zl.pack_mlp_args(T, ff, k, _DT[h.dtype], _DT[act.dtype], h.data_ptr(), ldh, *ps,
                                                act.data_ptr(), lda, 0, 0, 0, 0))
+    _wrote((act,) if packed is None else (act, packed.codes, packed.scales))
     return act
 
 
@@ -213,12 +235,12 @@ def mlp_act_bwd(h, dact, kind="swiglu", dtype=None, dh=None, act=None):
     _call(zl.zl_mlp_act_backward, dev,
           zl.pack_mlp_args(T, ff, k, _DT[dact.dtype], _DT[dh.dtype], hp, ldh, *ps, _ptr(act), lda, dact.data_ptr(), ldda,
                            dh.data_ptr(), lddh))
+    _wrote((dh,) if act is None else (dh, act))
     return dh
 
 
 NormGrads = namedtuple("NormGrads", "w_post b_post w_pre b_pre gate", defaults=(None,) * 5)
 NormGrads.__doc__ = "Gradients of block_norm's parameters (fp32; None = not wanted)."
-_NO_WB = (None, None)
 
 
 def _norm_common(d, T, dev, post, pre, gate, gate_rows, stats):
@@ -232,6 +254,8 @@ def _norm_common(d, T, dev, post, pre, gate, gate_rows, stats):
         G = -(-T // gate_rows)
         if gate.dtype != torch.float32 or gate.shape != (G, d) or not gate.is_contiguous():
             raise ValueError(f"gate must be a contiguous fp32 [{G}, {d}] tensor")
+        if gate.requires_grad and not gate.is_leaf:
+            _no_graph("gate")
         gp = gate.data_ptr()
     if stats.dtype != torch.float32 or stats.shape != (T, 4) or not stats.is_contiguous():
         raise ValueError(f"stats must be a contiguous fp32 [{T}, 4] tensor")
@@ -275,6 +299,11 @@ def block_norm(x, y, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5, 
           zl.pack_norm_args(T, d, int(layernorm), ty, tn, eps, scale, *params, x.data_ptr(), _ptr(xo), ldx, _ptr(y), ldy,
                             _ptr(n), ldn, *_packed("y_packed", y_packed, T, d), *_packed("n_packed", n_packed, T, d),
                             0, 0, 0, 0, 0, 0, 0, 0, 0, 0.0, 0, 0, 0))
+    wrote = [t for t in (xo, n, stats) if t is not None]
+    for p in (y_packed, n_packed):
+        if p is not None:
+            wrote += p.codes, p.scales
+    _wrote(wrote)
     return (x if y is None else xo), n, stats
 
 
@@ -345,6 +374,7 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
                             _ptr(dy), _vec("grads.w_post", gw, d), _vec("grads.b_post", gb, d),
                             _vec("grads.w_pre", gv, d), _vec("grads.b_pre", gc, d), _ptr(gg), grad_scale,
                             int(accumulate), workspace.data_ptr(), workspace.numel()))
+    _wrote([t for t in (dx, dy, gw, gb, gv, gc, gg, workspace) if t is not None])
     return dx, dy
 
 
@@ -364,6 +394,7 @@ def wgrad(dy, x, out=None, scale=1.0, accumulate=False, workspace=None):
     _check_device(dev, "x out workspace", x, out, workspace)
     _call(zl.zl_wgrad_packed, dev, T, M, N, dy.data_ptr(), lddy, _DT[dy.dtype], p, out.data_ptr(), ld, scale, accumulate,
           _ptr(workspace), 0 if workspace is None else workspace.numel())
+    _wrote((out,) if workspace is None else (out, workspace))
     return out
 
 
@@ -384,8 +415,11 @@ def rotary(x, pos, axis_of, n_heads, head_dim, theta, *, inverse=False, out=None
     out = torch.empty(T, W, dtype=x.dtype, device=dev) if out is None else out
     if out.dtype != x.dtype or out.dim() != 2 or out.shape[0] != T or out.shape[1] < W or out.stride(1) != 1:
         raise ValueError(f"out must be [{T}, >= {W}] of x's type with contiguous rows")
+    if x.requires_grad or out.requires_grad:
+        _no_graph("x" if x.requires_grad else "out")
     _check_device(dev, "pos out", pos, out)
     ldx, ldo = (ldx, out.stride(0)) if T > 1 else (W, W)
     _call(zl.zl_rotary, dev, T, n_heads, head_dim, 2 * len(axis_of), x.data_ptr(), ldx, out.data_ptr(), ldo, _DT[x.dtype],
           pos.data_ptr(), pos.shape[0], axis_of, theta, inverse)
+    _wrote((out,))
     return out

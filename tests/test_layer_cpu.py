@@ -423,3 +423,69 @@ for M in (65536 * 128 + 8, 1 << 30):
     r = subprocess.run([sys.executable, "-c", code], cwd=root, env=dict(os.environ, HIP_VISIBLE_DEVICES="-1"),
                        capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.count("no ROCm-capable device") == 2, (r.returncode, r.stdout, r.stderr)
+
+
+def _calls():
+    """Every torch function with tensors for each argument: name -> (function, fixed
+    arguments, tensor arguments, the ones it writes)."""
+    z = lambda *sh: torch.zeros(*sh)  # noqa: E731
+    w, v = (torch.ones(64), torch.zeros(64)), (torch.ones(64), torch.zeros(64))
+    P = lambda n: layer.Packed.empty(4, n, "cpu")  # noqa: E731
+    norm = dict(gate_rows=4, layernorm=True)
+    return dict(
+        pack=(layer.pack, {}, dict(x=z(4, 64), out=P(64)), ["out"]),
+        unpack=(layer.unpack, dict(p=P(64)), dict(out=z(4, 64)), ["out"]),
+        mlp_act=(layer.mlp_act, {}, dict(h=z(4, 64), act=z(4, 32), packed=P(64)), ["act", "packed"]),
+        mlp_act_bwd=(layer.mlp_act_bwd, {}, dict(h=z(4, 64), dact=z(4, 32), dh=z(4, 64), act=z(4, 32)), ["dh", "act"]),
+        block_norm=(layer.block_norm, dict(post=w, pre=v, **norm),
+                    dict(x=z(4, 64), y=z(4, 64), gate=z(1, 64), xo=z(4, 64), n=z(4, 64), stats=z(4, 4), y_packed=P(64), n_packed=P(64)),
+                    ["xo", "n", "stats", "y_packed", "n_packed"]),
+        block_norm_bwd=(layer.block_norm_bwd, dict(post=w, pre=v, grads=layer.NormGrads(*(z(64) for _ in range(4)), z(1, 64)), **norm),
+                        dict(dxo=z(4, 64), dn=z(4, 64), y=z(4, 64), xo=z(4, 64), stats=z(4, 4), gate=z(1, 64), dx=z(4, 64),
+                             dy=z(4, 64), workspace=z(1 << 16)), ["dx", "dy", "workspace"]),
+        wgrad=(layer.wgrad, dict(x=P(64)), dict(dy=z(4, 64), out=z(64, 64), workspace=z(1 << 16)), ["out", "workspace"]),
+        rotary=(layer.rotary, dict(pos=torch.zeros(1, 4, dtype=torch.int32), axis_of=bytes(8), n_heads=4, head_dim=16, theta=1e4),
+                dict(x=z(4, 64), out=z(4, 64)), ["out"]))
+
+
+@pytest.mark.parametrize("name", list(_calls()))
+def test_autograd_is_not_passed_by(on_host, name):
+    """No graph is made here: in gradient mode a matrix that requires a gradient is
+    refused; weights, biases and gates may be parameters, not results.  Tensors that
+    a call writes count as changed."""
+    fn, fixed, tensors, written = _calls()[name]
+    fn(**fixed, **tensors)
+    assert len(on_host) == 1
+    for key, t in tensors.items():
+        if isinstance(t, layer.Packed) or key in ("stats", "workspace"):
+            continue
+        leaf = t.clone().requires_grad_()
+        for bad in [leaf * 1.0] + ([] if key == "gate" else [leaf]):
+            with pytest.raises(ValueError, match=f"{key}.* gradient"):
+                fn(**fixed, **{**tensors, key: bad})
+            with torch.no_grad():
+                fn(**fixed, **{**tensors, key: bad})
+    for key in ("post", "pre"):
+        if key in fixed:
+            par = tuple(t.clone().requires_grad_() for t in fixed[key])
+            fn(**{**fixed, key: par}, **{**tensors, "gate": tensors["gate"].clone().requires_grad_()})
+            with pytest.raises(ValueError, match="gradient"):
+                fn(**{**fixed, key: (par[0] * 1.0, par[1])}, **tensors)
+            with pytest.raises(ValueError, match="gradient"):
+                fn(**{**fixed, key: (par[0], par[1] * 1.0)}, **tensors)
+    # a graph that saved what is written next finds out
+    for key in written:
+        for t in (tensors[key].codes, tensors[key].scales) if isinstance(tensors[key], layer.Packed) else (tensors[key],):
+            leaf = torch.ones(t.shape, requires_grad=True)
+            out = (leaf * t).sum()
+            fn(**fixed, **tensors)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                out.backward()
+    for t in fixed.get("grads", ()):
+        leaf = torch.ones(t.shape, requires_grad=True)
+        out = (leaf * t).sum()
+        fn(**fixed, **tensors)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.backward()
+    with torch.inference_mode():
+        fn(**fixed, **tensors)
