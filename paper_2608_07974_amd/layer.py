@@ -25,7 +25,7 @@ _DT = {torch.float32: zl.ZL_F32, torch.bfloat16: zl.ZL_BF16}
 _KIND = {"swiglu": zl.ZL_MLP_SWIGLU, "gelu": zl.ZL_MLP_GELU}
 _NONE = (0, 0, 0, 0)  # no packed matrix
 _NO_WB = (None, None)  # no weight and bias
-_F32 = (torch.float32,)
+_F32, _U8 = (torch.float32,), torch.uint8
 
 
 def _up(n, m):
@@ -113,8 +113,6 @@ def _packed_rows(codes, scales, n):
         raise ValueError(f"codes and scales must be [{T}, >= {c16}] and [{T}, >= {c32}], not [{T}, {W}] and [{Ts}, {Ws}]")
     if codes.device != scales.device:
         raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
-    if codes.is_contiguous() and scales.is_contiguous():
-        return (W, Ws) if T > 1 else (c16, c32)
     (lc, c1), (ls, s1) = codes.stride(), scales.stride()
     if (c1 != 1 and W > 1) or (s1 != 1 and Ws > 1):
         raise ValueError("codes and scales must have contiguous rows")
@@ -131,14 +129,21 @@ class Packed:
     __slots__ = ("codes", "scales", "n")
 
     def __init__(self, codes, scales, n):
-        _packed_rows(codes, scales, n)
         self.codes, self.scales, self.n = codes, scales, n
+        self.fields()
 
     def fields(self):
         """The matrix as the library takes it: pointers and row strides."""
-        codes, scales = self.codes, self.scales
-        ld = _packed_rows(codes, scales, self.n)
-        return (codes.data_ptr(), scales.data_ptr()) + ld
+        codes, scales, n = self.codes, self.scales, self.n
+        c, s = codes.shape, scales.shape
+        if codes.dtype is _U8 and scales.dtype is _U8 and len(c) == 2 and len(s) == 2:
+            lc, c1 = codes.stride()
+            ls, s1 = scales.stride()
+            c16, c32, T = n + 15 & -16, n + 31 >> 5, c[0]
+            if c1 == 1 and s1 == 1 and T > 1 and lc >= c16 <= c[1] and ls >= c32 <= s[1] and s[0] == T and \
+                    codes.device == scales.device:
+                return codes.data_ptr(), scales.data_ptr(), lc, ls
+        return (codes.data_ptr(), scales.data_ptr()) + _packed_rows(codes, scales, n)
 
     @classmethod
     def empty(cls, T, n, device="cuda"):
