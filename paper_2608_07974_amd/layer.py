@@ -39,11 +39,18 @@ def _ptr(t):
 # The host's share of a small call is most of it: the checks of this file are
 # written for the case that passes.
 def _check_device(dev, names, *tensors):
-    """Every tensor (or None) is on the GPU dev; names: theirs, in one text."""
+    """Every tensor, Packed or None is on the GPU dev; names: theirs, in one text."""
     if dev.type != "cuda":
         raise ValueError(f"tensors must be on a GPU, not {dev}")
+    index = dev.index
     for i, t in enumerate(tensors):
-        if t is not None and t.device != dev:
+        if t is None:
+            continue
+        if type(t) is Packed:
+            if t.scales.get_device() != index:
+                raise ValueError(f"{names.split()[i]}.scales must be on {dev}, not {t.scales.device}")
+            t = t.codes
+        if t.get_device() != index:  # (-1 off the GPUs)
             raise ValueError(f"{names.split()[i]} must be on {dev}, not {t.device}")
 
 
@@ -105,20 +112,22 @@ def _call(fn, dev, *args):
 
 
 def _packed_rows(codes, scales, n):
-    """Row strides of both tensors of a packed matrix, everything of them checked."""
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2:
+    """Rows of a packed matrix and the row strides of its tensors, whose types, shapes
+    and strides are checked."""
+    c, s, c16, c32 = codes.shape, scales.shape, n + 15 & -16, n + 31 >> 5
+    if codes.dtype is not _U8 or scales.dtype is not _U8 or len(c) != 2 or len(s) != 2:
         raise TypeError("codes and scales must be uint8 matrices")
-    (T, W), (Ts, Ws), c16, c32 = codes.shape, scales.shape, _up(n, 16), (n + 31) // 32
+    (T, W), (Ts, Ws) = c, s
     if W < c16 or Ts != T or Ws < c32:
         raise ValueError(f"codes and scales must be [{T}, >= {c16}] and [{T}, >= {c32}], not [{T}, {W}] and [{Ts}, {Ws}]")
-    if codes.device != scales.device:
-        raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
+    if codes.is_contiguous() and scales.is_contiguous():
+        return (T, W, Ws) if T > 1 else (T, c16, c32)
     (lc, c1), (ls, s1) = codes.stride(), scales.stride()
     if (c1 != 1 and W > 1) or (s1 != 1 and Ws > 1):
         raise ValueError("codes and scales must have contiguous rows")
     if T > 1 and (lc < c16 or ls < c32):
         raise ValueError("codes and scales must not overlap themselves")
-    return (lc, ls) if T > 1 else (c16, c32)
+    return (T, lc, ls) if T > 1 else (T, c16, c32)
 
 
 class Packed:
@@ -130,20 +139,16 @@ class Packed:
 
     def __init__(self, codes, scales, n):
         self.codes, self.scales, self.n = codes, scales, n
-        self.fields()
+        _packed_rows(codes, scales, n)
+        if codes.device != scales.device:
+            raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
 
     def fields(self):
         """The matrix as the library takes it: pointers and row strides."""
-        codes, scales, n = self.codes, self.scales, self.n
-        c, s = codes.shape, scales.shape
-        if codes.dtype is _U8 and scales.dtype is _U8 and len(c) == 2 and len(s) == 2:
-            lc, c1 = codes.stride()
-            ls, s1 = scales.stride()
-            c16, c32, T = n + 15 & -16, n + 31 >> 5, c[0]
-            if c1 == 1 and s1 == 1 and T > 1 and lc >= c16 <= c[1] and ls >= c32 <= s[1] and s[0] == T and \
-                    codes.device == scales.device:
-                return codes.data_ptr(), scales.data_ptr(), lc, ls
-        return (codes.data_ptr(), scales.data_ptr()) + _packed_rows(codes, scales, n)
+        codes, scales = self.codes, self.scales
+        if codes.device != scales.device:
+            raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
+        return (codes.data_ptr(), scales.data_ptr()) + _packed_rows(codes, scales, self.n)[1:]
 
     @classmethod
     def empty(cls, T, n, device="cuda"):
@@ -165,9 +170,12 @@ class Packed:
 def _packed(name, p, T, n):
     if p is None:
         return _NONE
-    if p.n != n or p.codes.shape[0] != T:
-        raise ValueError(f"{name} must be [{T}, {n}], not {list(p.shape)}")
-    return p.fields()
+    if p.n == n:
+        codes, scales = p.codes, p.scales
+        rows, lc, ls = _packed_rows(codes, scales, n)
+        if rows == T:
+            return codes.data_ptr(), scales.data_ptr(), lc, ls
+    raise ValueError(f"{name} must be [{T}, {n}], not {list(p.shape)}")
 
 
 def pack(x, out=None):
@@ -189,8 +197,8 @@ def unpack(p, dtype=torch.bfloat16, out=None):
     dev = p.device
     out = torch.empty(T, n, dtype=dtype, device=dev) if out is None else out
     ld = _rows("out", out, T, n, _DT)
-    _check_device(dev, "out", out)
-    _call(zl.zl_unpack, dev, T, n, zl.pack_packed(*p.fields()), out.data_ptr(), ld, _DT[out.dtype])
+    _check_device(dev, "p out", p, out)
+    _call(zl.zl_unpack, dev, T, n, zl.pack_packed(*_packed("p", p, T, n)), out.data_ptr(), ld, _DT[out.dtype])
     _wrote((out,))
     return out
 
@@ -233,7 +241,7 @@ def mlp_act_bwd(h, dact, kind="swiglu", dtype=None, dh=None, act=None):
     lddh = _rows("dh", dh, T, nh, _DT)
     lda = 0 if act is None else _rows("act", act, T, ff, (dh.dtype,))
     if isinstance(h, Packed):
-        hp, ldh, ps = 0, 0, h.fields()
+        hp, ldh, ps = 0, 0, _packed("h", h, T, nh)
     else:
         hp, ldh, ps = h.data_ptr(), _rows("h", h, T, nh, (dact.dtype,)), _NONE
     _check_device(dev, "h dh act", h, dh, act)

@@ -435,11 +435,11 @@ def _int(n):
 
 
 def zl_pack(T, n, x, ldx, dtype, out, stream=0):
-    _check(load().zl_pack(T, _int(n), x, ldx, dtype, _ref(out), stream), "zl_pack")
+    _check(load().zl_pack(T, _int(n) if n >> 31 else n, x, ldx, dtype, _ref(out), stream), "zl_pack")
 
 
 def zl_unpack(T, n, packed, x, ldx, dtype, stream=0):
-    _check(load().zl_unpack(T, _int(n), _ref(packed), x, ldx, dtype, stream), "zl_unpack")
+    _check(load().zl_unpack(T, _int(n) if n >> 31 else n, _ref(packed), x, ldx, dtype, stream), "zl_unpack")
 
 
 def zl_mlp_act(args, stream=0):
@@ -468,7 +468,9 @@ def zl_block_norm_workspace(T, d, gate_rows=0):
 
 def zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, x, dw, lddw, scale=1.0, accumulate=0,
                     workspace=None, workspace_elems=0, stream=0):
-    _check(load().zl_wgrad_packed(T, _int(n_out), _int(n_in), dy, lddy, dtype, _ref(x), scale,
+    if (n_out | n_in) >> 31:
+        n_out, n_in = _int(n_out), _int(n_in)
+    _check(load().zl_wgrad_packed(T, n_out, n_in, dy, lddy, dtype, _ref(x), scale,
                                   int(accumulate), dw, lddw, workspace, workspace_elems, stream),
            "zl_wgrad_packed")
 
@@ -481,8 +483,10 @@ def zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes, a
         axis_of = bytes(map(operator.index, axis_of))
     if rot > 0 and len(axis_of) < rot // 2:
         raise ValueError(f"axis_of must hold rot / 2 = {rot // 2} axis numbers")
-    _check(load().zl_rotary(T, _int(n_heads), _int(head_dim), _int(rot), x, ldx, out, ldo, dtype, pos,
-                            _int(n_axes), axis_of, theta, int(inverse), stream), "zl_rotary")
+    if (n_heads | head_dim | rot | n_axes) >> 31:
+        n_heads, head_dim, rot, n_axes = _int(n_heads), _int(head_dim), _int(rot), _int(n_axes)
+    _check(load().zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes, axis_of,
+                            theta, int(inverse), stream), "zl_rotary")
 
 
 def zl_profile_end(h, max_entries=256):

@@ -348,6 +348,22 @@ def test_packed_follows_its_tensors():
     refused(lambda p: p.codes.resize_(0), TypeError)
     refused(lambda p: p.scales.resize_(2, 2))
     refused(lambda p: p.codes.t_())
+    class On:  # stands for a tensor on GPU 1 or 2
+        def __init__(self, index):
+            self.index = self.device = index
+
+        def get_device(self):
+            return self.index
+
+    dev = torch.device("cuda", 1)
+    for codes, scales, bad in ((1, 1, None), (1, 2, "out.scales"), (2, 1, "out"), (2, 2, "out.scales")):
+        p = new()
+        p.codes, p.scales = On(codes), On(scales)
+        if bad is None:
+            layer._check_device(dev, "x out", None, p)
+        else:
+            with pytest.raises(ValueError, match=f"{bad} must be on"):
+                layer._check_device(dev, "x out", None, p)
     with pytest.raises(ValueError):
         p = new()
         p.codes.resize_(3, 64)
