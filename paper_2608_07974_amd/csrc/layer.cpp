@@ -189,11 +189,13 @@ zl_status zl_rotary(int64_t T, int n_heads, int head_dim, int rot, const void* x
   if (!(theta > 1.0) || !isfinite(theta)) return bad("theta must be > 1");
   const int64_t w = (int64_t)n_heads * head_dim;
   if (w > 0x7fffffff / 256) return set_error(ZL_ERR_UNSUPPORTED, "more than 2^23 columns of heads");
-  if (T > 0 && (!x || !out || !pos)) return bad("bad rotary args");
-  if (ldx < w || ldo < w) return bad("row stride below n_heads * head_dim");
-  const uintptr_t es = dtype == ZL_BF16 ? 2 : 4;
-  if ((uintptr_t)x % es || (uintptr_t)out % es || (uintptr_t)pos % 4) return bad("misaligned pointer");
-  if (x == out && ldx != ldo) return bad("in place needs the same row stride");
+  if (T > 0) {
+    if (!x || !out || !pos) return bad("bad rotary args");
+    if (ldx < w || ldo < w) return bad("row stride below n_heads * head_dim");
+    const uintptr_t es = dtype == ZL_BF16 ? 2 : 4;
+    if ((uintptr_t)x % es || (uintptr_t)out % es || (uintptr_t)pos % 4) return bad("misaligned pointer");
+    if (x == out && ldx != ldo) return bad("in place needs the same row stride");
+  }
   RotaryArgs a;
   memset(&a, 0, sizeof(a));
   a.T = T;

@@ -505,3 +505,20 @@ def test_autograd_is_not_passed_by(on_host, name):
             out.backward()
     with torch.inference_mode():
         fn(**fixed, **tensors)
+
+
+@pytest.mark.parametrize("ld", [0, -8, 3, 1 << 62])
+def test_empty_batches_have_no_memory(ld):
+    """T = 0: no pointers, any strides, nothing launched (the weight gradient, which
+    writes zeros, aside)."""
+    none = zl.zl_packed(0, 0, ld, ld)
+    for dt in (zl.ZL_F32, zl.ZL_BF16):
+        zl.zl_pack(0, 64, 0, ld, dt, none)
+        zl.zl_unpack(0, 64, none, 0, ld, dt)
+        zl.zl_rotary(0, 4, 16, 16, 0, ld, 0, ld + 8, dt, 0, 3, bytes(8), 1e4)
+        zl.zl_rotary(0, 4, 16, 8, A + 1, ld, A + 1, ld + 8, dt, A + 1, 1, bytes(4), 1e4, 1)
+        io = dict(T=0, in_dtype=dt, out_dtype=dt)
+        zl.zl_mlp_act(zl.zl_mlp_args(ff=64, ldh=ld, lda=ld, packed=none, **io))
+        zl.zl_mlp_act_backward(zl.zl_mlp_args(ff=64, ldh=ld, ldda=ld, lddh=ld, packed=none, **io))
+        zl.zl_block_norm(zl.zl_norm_args(d=64, eps=1e-5, w_post=A, w_pre=A, ldx=ld, ldy=ld, ldn=ld, **io))
+        zl.zl_block_norm_backward(zl.zl_norm_args(d=64, eps=1e-5, w_post=A, w_pre=A, ldx=ld, ldy=ld, ldn=ld, **io))
