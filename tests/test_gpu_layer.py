@@ -262,6 +262,78 @@ def test_mlp_act_beyond_the_exponential():
         assert np.array_equal(act[:, :8], np.maximum(np.float32(x), 0)) and np.array_equal(dh[:, :8], (x > 0) * 1.0)
 
 
+# ------------------------------------------- large calls against small ones
+def _in_rows(T, step=400):
+    """Slices of few rows: calls of at most four blocks a CU, one row per thread."""
+    return [slice(t, min(T, t + step)) for t in range(0, T, step)]
+
+
+def _rows_of(p, r):
+    return _L().Packed(p.codes[r], p.scales[r], p.n)
+
+
+def _randn(T, n, dt, seed=7):
+    return torch.empty(T, n, dtype=_dt(dt), device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(seed))
+
+
+def _equal_packed(p, q):
+    assert torch.equal(p.codes[:, : p.n], q.codes[:, : p.n]) and torch.equal(p.scales, q.scales)
+
+
+# Outputs above 32 MB are stored past the caches, inputs above 384 MB are loaded so
+# too; many rows go several to a thread.  The same values, bit for bit, as in
+# pieces that do neither (those are what the tests above compare with the oracle).
+@pytest.mark.parametrize("dt,T", [(BF, 2051), (F32, 2051), (BF, 8195), (F32, 8195), (BF, 49157), (F32, 24579)])
+def test_pack_and_unpack_of_many_rows(dt, T):
+    layer = _L()
+    n = 4104
+    x = _randn(T, n, dt)
+    p, q = layer.pack(x), layer.Packed.empty(T, n)
+    for r in _in_rows(T):
+        layer.pack(x[r], out=_rows_of(q, r))
+    _equal_packed(p, q)
+    del x
+    for odt in (BF, F32):
+        got = layer.unpack(p, dtype=_dt(odt))
+        assert all(torch.equal(got[r], layer.unpack(_rows_of(p, r), dtype=_dt(odt))) for r in _in_rows(T))
+
+
+@pytest.mark.parametrize("kind,inp,out,T,ff", [
+    ("swiglu", BF, BF, 2051, 2080), ("swiglu", F32, BF, 2051, 2080), ("swiglu", BF, F32, 2051, 2080), ("swiglu", F32, F32, 2051, 2080),
+    ("gelu", BF, BF, 2051, 2088), ("gelu", F32, F32, 2051, 2088), ("gelu", F32, BF, 2051, 2088),
+    ("swiglu", BF, BF, 4099, 2080), ("swiglu", F32, F32, 4099, 2080), ("gelu", BF, BF, 8195, 2088), ("gelu", F32, BF, 8195, 2088),
+    ("swiglu", BF, BF, 48403, 2080), ("gelu", F32, BF, 48403, 2088)])
+def test_mlp_act_of_many_rows(kind, inp, out, T, ff):
+    layer = _L()
+    n = (2 if kind == "swiglu" else 1) * ff
+    h, da = _randn(T, n, inp), _randn(T, ff, inp, 8)
+    for saved in (True, False):
+        p, q = (layer.Packed.empty(T, n) if saved else None for _ in range(2))
+        act = layer.mlp_act(h, kind, dtype=_dt(out), packed=p)
+        again = torch.empty_like(act)
+        src = p if saved else h
+        dh = layer.mlp_act_bwd(src, da, kind, dtype=_dt(out), act=again)
+        for r in _in_rows(T):
+            a = layer.mlp_act(h[r], kind, dtype=_dt(out), packed=_rows_of(q, r) if saved else None)
+            assert torch.equal(act[r], a)
+            b = torch.empty_like(a)
+            d = layer.mlp_act_bwd(_rows_of(p, r) if saved else h[r], da[r], kind, dtype=_dt(out), act=b)
+            assert torch.equal(dh[r], d) and torch.equal(again[r], b)
+        if saved:
+            _equal_packed(p, q)
+
+
+@pytest.mark.parametrize("dt,T,H,hd,rot", [(BF, 4099, 40, 128, 128), (BF, 4099, 40, 128, 96), (BF, 8195, 40, 64, 64), (F32, 4099, 24, 128, 128)])
+def test_rotary_of_many_rows(dt, T, H, hd, rot):
+    layer = _L()
+    x = _randn(T, H * hd + 16, dt)
+    pos = torch.randint(0, 100000, (3, T), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(9))
+    axes = bytes(i % 3 for i in range(rot // 2))
+    got = layer.rotary(x, pos, axes, H, hd, 5e5)
+    for r in _in_rows(T):
+        assert torch.equal(got[r], layer.rotary(x[r], pos[:, r].contiguous(), axes, H, hd, 5e5))
+
+
 # -------------------------------------------------------- norms around a block
 def _norm_case(rng, T, d, ln, parts, rows, inp):
     x = _acts(rng, T, d) + (0.5 if ln else 0.0)
@@ -398,6 +470,17 @@ def test_block_norm_backward(ln, inp, out, saved, T, d, rows, parts, pad):
     dx0, _ = layer.block_norm_bwd(None, *args, **gkw) if pre else (None, None)
     if pre:
         _near(_np(dx0), ref0["dx"], k * tD, what="dx without dxo")
+
+
+@pytest.mark.parametrize("ln,inp,out,saved", [(False, BF, BF, True), (True, F32, F32, False), (True, BF, F32, False), (False, F32, BF, True)])
+@pytest.mark.parametrize("T,d,rows,slots", [(16400, 72, 8195, 4), (8200, 8, 8199, 4), (8195, 1000, 4097, 2), (6150, 2048, 2050, 1)])
+def test_block_norm_backward_through_long_gate_rows(ln, inp, out, saved, T, d, rows, slots):
+    """Few long gate rows, every one of them gone through by all blocks with 4, 2 and 1
+    rows in turn, the last gate row short in some."""
+    from paper_2608_07974_amd import zl
+    blocks, gates = zl.zl_block_norm_workspace(T, d) // (4 * d), -(-T // rows)
+    assert zl.zl_block_norm_workspace(T, d, rows) == (4 + gates * slots) * blocks * d  # what this plan needs
+    test_block_norm_backward(ln, inp, out, saved, T, d, rows, "both", 0)
 
 
 def test_block_norm_rows_of_one_value():
@@ -736,6 +819,33 @@ def test_torchs_default_type_does_not_matter():
     finally:
         torch.set_default_dtype(torch.float32)
     assert all(a.dtype == b.dtype and torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_in_an_autograd_function():
+    """A function whose forward and backward are these calls, between operations that
+    autograd records."""
+    layer = _L()
+
+    class Act(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, h):
+            ctx.h = layer.Packed.empty(*h.shape)
+            return layer.mlp_act(h, packed=ctx.h)
+
+        @staticmethod
+        def backward(ctx, da):
+            return layer.mlp_act_bwd(ctx.h, da.contiguous())
+
+    x, w = _randn(40, 64, F32), _randn(40, 32, F32, 8)
+    leaf = x.clone().requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        layer.mlp_act(leaf * 2.0)
+    y = Act.apply(leaf * 2.0)
+    (y * w).sum().backward()
+    h = _np(x) * 2.0
+    _near(_np(y), ol.mlp_act(h, "swiglu"), (2 * np.abs(h[:, :32]) + 16) * U * np.abs(ol.mlp_act(h, "swiglu")) + 2.0 ** -126)
+    want = 2.0 * layer.mlp_act_bwd(layer.pack(x * 2.0), w)
+    assert torch.equal(leaf.grad, want)
 
 
 # ------------------------------------------------------------ a whole layer
