@@ -140,7 +140,7 @@ class Packed:
     def __init__(self, codes, scales, n):
         self.codes, self.scales, self.n = codes, scales, n
         _packed_rows(codes, scales, n)
-        if codes.device != scales.device:
+        if codes.get_device() != scales.get_device():
             raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
 
     def fields(self):
@@ -193,12 +193,13 @@ def pack(x, out=None):
 
 def unpack(p, dtype=torch.bfloat16, out=None):
     """The values of a Packed matrix."""
-    T, n = p.shape
-    dev = p.device
+    codes, scales, n = p.codes, p.scales, p.n
+    T, lc, ls = _packed_rows(codes, scales, n)
+    dev = codes.device
     out = torch.empty(T, n, dtype=dtype, device=dev) if out is None else out
     ld = _rows("out", out, T, n, _DT)
-    _check_device(dev, "p out", p, out)
-    _call(zl.zl_unpack, dev, T, n, zl.pack_packed(*_packed("p", p, T, n)), out.data_ptr(), ld, _DT[out.dtype])
+    _check_device(dev, "scales out", scales, out)
+    _call(zl.zl_unpack, dev, T, n, zl.pack_packed(codes.data_ptr(), scales.data_ptr(), lc, ls), out.data_ptr(), ld, _DT[out.dtype])
     _wrote((out,))
     return out
 
@@ -312,7 +313,11 @@ def block_norm(x, y, post, pre, *, gate=None, gate_rows=0, scale=1.0, eps=1e-5, 
           zl.pack_norm_args(T, d, int(layernorm), ty, tn, eps, scale, *params, x.data_ptr(), _ptr(xo), ldx, _ptr(y), ldy,
                             _ptr(n), ldn, *_packed("y_packed", y_packed, T, d), *_packed("n_packed", n_packed, T, d),
                             0, 0, 0, 0, 0, 0, 0, 0, 0, 0.0, 0, 0, 0))
-    wrote = [t for t in (xo, n, stats) if t is not None]
+    wrote = [stats]
+    if y is not None:
+        wrote.append(xo)
+    if pre is not None:
+        wrote.append(n)
     for p in (y_packed, n_packed):
         if p is not None:
             wrote += p.codes, p.scales
