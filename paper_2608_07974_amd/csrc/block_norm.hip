@@ -573,6 +573,9 @@ NormPlan norm_plan(int64_t T, int d, int64_t gate_rows) {
     p.gates = gates;
     p.gate_part = gates * p.nblk * slots;
   } else if (gate_rows >= p.rows * slots) {
+    // blocks of their own for every gate row, or (below) whole gate rows for a slot, which
+    // leaves slots idle just below the border (128 and 127 rows at 65536 x 256: 61 and 152 us;
+    // 64 and 63 at 16384 x 1024: 60 and 66; 32 and 31 at 16384 x 512: 42 and 44)
     p.group = gate_rows;
     p.cpg = (gate_rows + p.rows * slots - 1) / (p.rows * slots);
     p.rows = (gate_rows + p.cpg * slots - 1) / (p.cpg * slots);

@@ -192,9 +192,10 @@ struct CodeTile {
 // loaded in their place, and dy of tile kt + NST starts on its way.  Codes before
 // dy: waiting for the oldest codes then leaves the newest copies of dy in flight.
 // The loop runs whole rounds of NST tiles, so that stages and register sets are
-// compile-time (16384 x 14336 x 4096: 1609 us, 1669 with a run-time stage); tiles
-// past the end are zeros by the buffers' ends, without a test per load (1519 us;
-// the bf16 GEMM of that size 1529, both at 1.26 - 1.27 PFLOP/s).
+// compile-time (16384 x 14336 x 4096, a run-time stage: 4 % more); tiles past the
+// end are zeros by the buffers' ends, without a test per load (6 % more).  Of that
+// size 1505 to 1585 us by card and clock, 1.21 to 1.28 PFLOP/s; the bf16 GEMM in turn
+// with it on one card takes 1 to 3 % more.
 template <int BM, int BN, int WM, int WN, int BK, int NST>
 __global__ void __launch_bounds__(WM * WN * 64) wgrad_mfma_kernel(GemmDesc g, EpiArgs e, zl_packed x) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -334,9 +335,12 @@ static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accu
   e.accumulate = accumulate;
   const GemmPlan plan = plan_gemm({a.M, a.N, T, false, false, a.part != nullptr, a.part_elems, false, 0});
   // One block of eight waves a CU, 64 tokens a stage, where no CU would get a second
-  // block and the splits would be short: 512 x 768 x 768 9.6 us, split 11.2;
-  // 2048 x 2048 x 2048 25.2 against 26.5 with four waves.  More tiles: 512 x 4096 x
-  // 2048 23.8 against 20.3; more tokens to split: 1024 x 256 x 256 13.1 against 11.0.
+  // block and nothing is split, or the splits would be short.  Unsplit, against four
+  // waves: 512 x 768 x 768 9.9 us and 11.4, 2048 x 2048 x 2048 25.2 and 26.7; without
+  // room for partials at any T (4096 x 768 x 768 35.0 and 40.0, 8192 x 256 x 256 62.5 and
+  // 66.4; at the least 64 x 2048 x 2048 10.5 and 10.2).  Instead of splits: 512 x 256 x
+  // 256 9.5 and 11.1, 768 x 256 x 256 10.8 and 10.4, 800 x 256 x 256 12.1 and 10.5.  More
+  // tiles: 512 x 4096 x 2048 23.8 and 20.3.
   const int64_t tiles = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
   const bool deep = !plan.large && tiles <= 256 && (plan.nz == 1 || T <= 768);
   const int nz = split_k(T, deep ? 1 : plan.nz, 32, g.ksplit);
@@ -350,7 +354,7 @@ static hipError_t wgrad_segment(const WgradArgs& a, int64_t t0, int T, bool accu
     ep.scale = 1.f;
     ep.zstride = (int64_t)a.M * a.N;
   }
-  // 4 stages for large tiles (3: 1526 us at 16384 x 14336 x 4096, 5: 1534), 3 for
+  // 4 stages for large tiles (3 or 5: up to 1 % more at 16384 x 14336 x 4096), 3 for
   // small ones, which share a CU (4096 x 2304 x 768: 32.8; 4 stages 33.5, 8 42.2)
   hipError_t err = plan.large ? wgrad_mfma<256, 256, 4, 2, 32, 4>(g, ep, x, nz, s)
                    : deep     ? wgrad_mfma<128, 128, 4, 2, 64, 3>(g, ep, x, nz, s)

@@ -399,7 +399,8 @@ def block_norm_bwd(dxo, dn, y, xo, stats, post, pre, *, gate=None, gate_rows=0, 
 def wgrad(dy, x, out=None, scale=1.0, accumulate=False, workspace=None):
     """dw [n_out, n_in] fp32 = scale * dy^T x (added to `out` with
     accumulate); dy [T, n_out], x a Packed [T, n_in].  workspace: fp32 scratch
-    that lets a small dw split the sum over T."""
+    that lets a small dw split the sum over T, each part as large as dw (bf16,
+    T = 4096, dw 768 x 768: 21 us with 6 parts, 35 without a workspace)."""
     T, M = dy.shape
     N, dev = x.n, dy.device
     lddy = _rows("dy", dy, T, M, _DT)
