@@ -46,7 +46,7 @@ def _check_device(dev, names, *tensors):
     for i, t in enumerate(tensors):
         if t is None:
             continue
-        if type(t) is Packed:
+        if isinstance(t, Packed):
             if t.scales.get_device() != index:
                 raise ValueError(f"{names.split()[i]}.scales must be on {dev}, not {t.scales.device}")
             t = t.codes
@@ -420,8 +420,8 @@ def wgrad(dy, x, out=None, scale=1.0, accumulate=False, workspace=None):
 def rotary(x, pos, axis_of, n_heads, head_dim, theta, *, inverse=False, out=None):
     """x [T, >= n_heads * head_dim] with the heads rotated by pos [axes, T]
     (int32, contiguous); returns [T, n_heads * head_dim].  axis_of: bytes (or
-    another sequence of integers), the axis of each frequency; 2 len(axis_of) columns of a head are rotated,
-    the others copied.  inverse: the gradient's way back.  out may be x."""
+    another sequence of integers), the axis of each frequency; 2 len(axis_of)
+    columns of a head are rotated, the others copied.  inverse: the gradient's way back.  out may be x."""
     T, W = x.shape[0], n_heads * head_dim
     dev = x.device
     if x.dim() != 2 or x.shape[1] < W:

@@ -364,6 +364,9 @@ def test_packed_follows_its_tensors():
         else:
             with pytest.raises(ValueError, match=f"{bad} must be on"):
                 layer._check_device(dev, "x out", None, p)
+    p = type("Own", (layer.Packed,), {})(torch.zeros(4, 64, **u8), torch.zeros(4, 2, **u8), 64)
+    with pytest.raises(ValueError, match="out.scales must be on"):  # a class of the user's
+        layer._check_device(dev, "x out", None, p)
     with pytest.raises(ValueError):
         p = new()
         p.codes.resize_(3, 64)
