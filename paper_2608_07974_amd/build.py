@@ -19,7 +19,7 @@ SOURCES = ["gemm_kk.hip", "gemm_kn.hip", "gemm_mn.hip", "gemm_mk.hip", "gemm_f32
            "gemm_skinny.hip", "gemm.hip",
            "attention.hip", "attention_mfma.hip", "rowops.hip",
            "objective.hip", "optim.hip", "layer.hip", "block_norm.hip", "wgrad_packed.hip",
-           "layer.cpp", "zl.cpp", "runtime.cpp", "noalloc.hip"]
+           "logit_loss.hip", "head_loss.hip", "layer.cpp", "loss.cpp", "zl.cpp", "runtime.cpp", "noalloc.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -37,7 +37,8 @@ NO_SCRATCH = {"gemm_kk.hip": "gemm_dma_kernel", "gemm_kn.hip": "gemm_dma_kernel"
               "gemm_mn.hip": "gemm_dma_kernel", "gemm_mk.hip": "gemm_dma_kernel",
               "attention_mfma.hip": "attn_", "gemm_skinny.hip": "kernel", "gemm_f32.hip": "kernel",
               "gemm.hip": "kernel", "rowops.hip": "kernel", "objective.hip": "kernel",
-              "layer.hip": "kernel", "block_norm.hip": "kernel", "wgrad_packed.hip": "kernel"}
+              "layer.hip": "kernel", "block_norm.hip": "kernel", "wgrad_packed.hip": "kernel",
+              "logit_loss.hip": "kernel", "head_loss.hip": "kernel"}
 
 
 def _scratch_users(stderr, pattern):

@@ -858,11 +858,18 @@ __device__ inline void wait_vmcnt() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
+// Whether an epilogue takes its tile transposed: the operands of every matrix
+// instruction change places, so that register r of lane l holds row l % MF and
+// column Mma<MF>::row(l, r), four consecutive columns of one row at a time.
+// An epilogue type of its own overloads store_tile.
+template <typename E> struct EpiTransposed { static constexpr bool value = false; };
+
 // NST-stage pipeline: the tile NST - 1 steps ahead is in flight while the
 // current one is multiplied; one barrier per BK-deep tile.  bl is the
 // block's index among the tiles of its problem.
-template <int BM, int BN, int WM, int WN, int BK, int NST, int DS, bool AK, bool BKM, bool RA, bool RB, int MF>
-__device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const EpiArgs& e, const int bl,
+template <int BM, int BN, int WM, int WN, int BK, int NST, int DS, bool AK, bool BKM, bool RA, bool RB, int MF,
+          typename E>
+__device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const E& e, const int bl,
                                               unsigned char* smem) {
   constexpr int NT = WM * WN * 64;
   constexpr int TM = BM / WM, TN = BN / WN;
@@ -915,6 +922,11 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const EpiArgs& 
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r = 0; r < M::NR; ++r) acc[i][j][r] = 0.f;
+
+  auto mma = [](const bf16x8_t a, const bf16x8_t b, const acc_t c) __attribute__((always_inline)) {
+    if constexpr (EpiTransposed<E>::value) return M::run(b, a, c);
+    else return M::run(a, b, c);
+  };
 
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(smem);
   const int nk = (klen + BK - 1) / BK;
@@ -982,7 +994,7 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const EpiArgs& 
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < NMF; ++t) {
-        acc[t / FN][t % FN] = M::run(af[cb][t / FN], bfr[cb][t % FN], acc[t / FN][t % FN]);
+        acc[t / FN][t % FN] = mma(af[cb][t / FN], bfr[cb][t % FN], acc[t / FN][t % FN]);
         if constexpr (FB == 2) {
 #pragma unroll
           for (int r = 0; r < NRD; ++r) {
@@ -1043,7 +1055,7 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const EpiArgs& 
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j)
-          acc[i][j] = M::run(af[cb][i], bfr[cb][j], acc[i][j]);
+          acc[i][j] = mma(af[cb][i], bfr[cb][j], acc[i][j]);
       __builtin_amdgcn_sched_barrier(0);
     }
 #endif
@@ -1052,7 +1064,8 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const EpiArgs& 
   }
   dma_wait();  // the zero-fill copies past K must land before LDS is reused
   __syncthreads();
-  if (g.K2 > 0 && kz == 0) {
+  // (transposed tiles have no second segment: its registers would not fit)
+  if (!EpiTransposed<E>::value && g.K2 > 0 && kz == 0) {
     // second K segment (same layouts): one BK-deep tile at a time through
     // stage 0, copied and multiplied without overlap (K2 is a few tiles);
     // with split K the first split carries it
@@ -1078,7 +1091,7 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const EpiArgs& 
         for (int i = 0; i < FM; ++i)
 #pragma unroll
           for (int j = 0; j < FN; ++j)
-            acc[i][j] = M::run(af[0][i], bfr[0][j], acc[i][j]);
+            acc[i][j] = mma(af[0][i], bfr[0][j], acc[i][j]);
       }
       __syncthreads();
     }

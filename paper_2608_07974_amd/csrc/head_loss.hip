@@ -1,0 +1,892 @@
+// Loss of a readout head z = x w^T without its logits (include/zl_loss.h).
+//
+// Forward: the product's tiles leave, per row and column block, the largest logit
+// and the sum of exponentials (the matrix unit's accumulators are the only place
+// where z exists); the few logits that the targets name are products of their own; a
+// kernel over the rows joins both.
+// Backward, a piece of the vocabulary at a time: the product again, whose tiles
+// write dL/dz (bf16 or fp32); the named columns' values over it; two products from
+// there.
+#include <string.h>
+
+#include "gemm_tiles.h"
+#include "loss.h"
+#include "loss_rows.h"
+
+namespace zl {
+
+// ----------------------------------------------------------------- epilogues
+// Tiles are taken transposed (EpiTransposed): a lane holds, for one row each of FM
+// row blocks, four consecutive columns at a time, so a row's sums need two steps
+// across lanes and its constants one load.
+
+// Partial sums.  PAIR false: (max z, sum exp((z - max) c)).  PAIR true: those of
+// z at c = 1 over all columns and of z at c over the columns without a mask bit.
+struct StatEpi {
+  int pair;
+  float c2;               // log2(e) / tau
+  float* part;            // [blocks, T, 2 or 4]
+  int64_t T;
+  const uint32_t* mask;   // [T, ldm] or null
+  int64_t ldm;
+};
+// dL/dz of the columns [0, N) of a piece, zeros up to the row stride.
+struct GradEpi {
+  const float4* coef;     // [T]: c1, l1, ct, lt
+  int two;                // c1 exp(z - l1) + ct exp(z / tau - lt), else the latter alone
+  float inv;
+  void* dz;
+  int64_t ldz;
+  int dtype;
+};
+// out = (accumulate ? out : 0) + scale * *gmax * C, or fp32 partials of split z.
+struct OutEpi {
+  void* out;
+  int64_t ldo;
+  int dtype;
+  float scale;
+  const float* gmax;      // or null
+  int accumulate;
+  int64_t zstride;
+};
+template <> struct EpiTransposed<StatEpi> { static constexpr bool value = true; };
+template <> struct EpiTransposed<GradEpi> { static constexpr bool value = true; };
+template <> struct EpiTransposed<OutEpi> { static constexpr bool value = true; };
+
+// The lanes that hold one row are MF apart.
+template <int MF, typename F>
+__device__ __forceinline__ float across(float x, F&& f) {
+#pragma unroll
+  for (int o = MF; o < 64; o <<= 1) x = f(x, __shfl_xor(x, o, 64));
+  return x;
+}
+
+template <int BM, int BN, int WM, int WN, int MF = 32>
+__device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[BM / WM / MF][BN / WN / MF],
+                                           unsigned char*, const GemmDesc& g, const StatEpi& e, int m0, int n0,
+                                           int wave, int lane) {
+  constexpr int TM = BM / WM, TN = BN / WN, FM = TM / MF, FN = TN / MF, NR = Mma<MF>::NR;
+  const int wm = wave / WN, wn = wave % WN;
+  const int nb = n0 + wn * TN;
+  if (nb >= g.N) return;
+  const bool cut = nb + TN > g.N;
+  const int64_t block = nb / TN;
+  auto fmax2 = [](float a, float b) { return fmaxf(a, b); };
+  auto add2 = [](float a, float b) { return a + b; };
+  static_for<0, FM>([&](auto ic) __attribute__((always_inline)) {
+    constexpr int i = decltype(ic)::value;
+    const int m = m0 + wm * TM + i * MF + (lane & (MF - 1));
+    float v[FN * NR];
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) v[j * NR + r] = acc[i][j][r];
+    if (cut)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+          if (nb + j * MF + Mma<MF>::row(lane, r) >= g.N) v[j * NR + r] = -INFINITY;
+    auto sums = [&](float c2, float& mx, float& s) __attribute__((always_inline)) {
+      mx = across<MF>(max_of(v), fmax2);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      s = 0.f;
+#pragma unroll
+      for (int k = 0; k < FN * NR; ++k) s += __builtin_amdgcn_exp2f((v[k] - ref) * c2);
+      s = across<MF>(s, add2);
+    };
+    float mx, s;
+    if (!e.pair) {
+      sums(e.c2, mx, s);
+      if (lane < MF && m < g.M) *reinterpret_cast<float2*>(e.part + (block * e.T + m) * 2) = make_float2(mx, s);
+    } else {
+      float mt, st;
+      sums(LOG2E, mx, s);
+      if (e.mask && m < g.M) {
+        const uint32_t* w = e.mask + m * e.ldm + (nb >> 5);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          const uint32_t bits = w[(j * MF) >> 5];
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+            if (bits >> ((j * MF & 31) + Mma<MF>::row(lane, r)) & 1) v[j * NR + r] = -INFINITY;
+        }
+      }
+      sums(e.c2, mt, st);
+      if (lane < MF && m < g.M)
+        *reinterpret_cast<float4*>(e.part + (block * e.T + m) * 4) = make_float4(mx, s, mt, st);
+    }
+  });
+}
+
+template <int BM, int BN, int WM, int WN, int MF = 32>
+__device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[BM / WM / MF][BN / WN / MF],
+                                           unsigned char*, const GemmDesc& g, const GradEpi& e, int m0, int n0,
+                                           int wave, int lane) {
+  constexpr int TM = BM / WM, TN = BN / WN, FM = TM / MF, FN = TN / MF, NR = Mma<MF>::NR;
+  const int wm = wave / WN, wn = wave % WN;
+  static_for<0, FM>([&](auto ic) __attribute__((always_inline)) {
+    constexpr int i = decltype(ic)::value;
+    const int m = m0 + wm * TM + i * MF + (lane & (MF - 1));
+    const float4 c = m < g.M ? e.coef[m] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r0 = 0; r0 < NR; r0 += 4) {
+        const int n = n0 + wn * TN + j * MF + Mma<MF>::row(lane, r0);
+        float o[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float v = acc[i][j][r0 + r];
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v, e.inv, -c.w) * LOG2E);
+          o[r] = c.z != 0.f ? c.z * p : 0.f;
+          if (e.two) {
+            const float q = __builtin_amdgcn_exp2f((v - c.y) * LOG2E);
+            o[r] += c.x != 0.f ? c.x * q : 0.f;
+          }
+          if (n + r >= g.N) o[r] = 0.f;
+        }
+        if (m < g.M && n < e.ldz) {
+          if (e.dtype == BF16)
+            *reinterpret_cast<uint2*>(static_cast<bf16_t*>(e.dz) + m * e.ldz + n) =
+                make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+          else
+            *reinterpret_cast<float4*>(static_cast<float*>(e.dz) + m * e.ldz + n) = make_float4(o[0], o[1], o[2], o[3]);
+        }
+      }
+  });
+}
+
+template <int BM, int BN, int WM, int WN, int MF = 32>
+__device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[BM / WM / MF][BN / WN / MF],
+                                           unsigned char*, const GemmDesc& g, const OutEpi& e, int m0, int n0,
+                                           int wave, int lane) {
+  constexpr int TM = BM / WM, TN = BN / WN, FM = TM / MF, FN = TN / MF, NR = Mma<MF>::NR;
+  const int wm = wave / WN, wn = wave % WN;
+  const float scale = e.zstride ? 1.f : e.gmax ? e.scale * *e.gmax : e.scale;
+  static_for<0, FM>([&](auto ic) __attribute__((always_inline)) {
+    constexpr int i = decltype(ic)::value;
+    const int64_t m = m0 + wm * TM + i * MF + (lane & (MF - 1));
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r0 = 0; r0 < NR; r0 += 4) {
+        const int n = n0 + wn * TN + j * MF + Mma<MF>::row(lane, r0);
+        // N is a multiple of 8: four columns are all there or none
+        if (m >= g.M || n >= g.N) continue;
+        float4 v = make_float4(acc[i][j][r0], acc[i][j][r0 + 1], acc[i][j][r0 + 2], acc[i][j][r0 + 3]);
+        v.x *= scale;
+        v.y *= scale;
+        v.z *= scale;
+        v.w *= scale;
+        if (e.dtype == BF16) {
+          *reinterpret_cast<uint2*>(static_cast<bf16_t*>(e.out) + m * e.ldo + n) =
+              make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+        } else {
+          float4* o = reinterpret_cast<float4*>(static_cast<float*>(e.out) + blockIdx.z * e.zstride + m * e.ldo + n);
+          if (e.accumulate) {
+            const float4 f = *o;
+            v.x += f.x;
+            v.y += f.y;
+            v.z += f.z;
+            v.w += f.w;
+          }
+          *o = v;
+        }
+      }
+  });
+}
+
+// ------------------------------------------------------------------ products
+template <int BM, int BN, int WM, int WN, int BK, int NST, bool AK, bool BKM, int MF, typename E>
+__global__ void __launch_bounds__(WM * WN * 64) head_gemm_kernel(GemmDesc g, E e) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  gemm_dma_body<BM, BN, WM, WN, BK, NST, 1, AK, BKM, false, false, MF>(g, e, blockIdx.x, smem);
+}
+
+template <int BM, int BN, int WM, int WN, bool AK, bool BKM, typename E>
+static hipError_t run_head_tiles(const GemmDesc& g, const E& e, int nz, hipStream_t s) {
+  constexpr int BK = KTile<AK, BKM>::BK, NST = KTile<AK, BKM>::NST, MF = KTile<AK, BKM>::MF;
+  auto kern = head_gemm_kernel<BM, BN, WM, WN, BK, NST, AK, BKM, MF, E>;
+  constexpr size_t lds = (size_t)NST * (BM + BN) * BK * sizeof(bf16_t);
+  static_assert(lds <= 160 * 1024, "pipeline exceeds LDS");
+  if (lds > 64 * 1024) {
+    const hipError_t err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (err != hipSuccess) return err;
+  }
+  const int nb = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
+  hipLaunchKernelGGL(kern, dim3(nb, 1, nz), dim3(WM * WN * 64), lds, s, g, e);
+  return hipGetLastError();
+}
+template <bool AK, bool BKM, typename E>
+static hipError_t run_head(const GemmDesc& g, const E& e, bool large, hipStream_t s, int nz = 1) {
+  if (large) return run_head_tiles<256, 256, 4, 2, AK, BKM>(g, e, nz, s);
+  return run_head_tiles<128, 128, 2, 2, AK, BKM>(g, e, nz, s);
+}
+
+// fp32: 128 x 128 tiles of four waves, v_mfma_f32_32x32x2_f32, 16 of K a step; the
+// next step is loaded while one is multiplied (two LDS buffers, one barrier a step).
+constexpr int SK = 16, ST = 128, SLD = ST + 4;
+template <bool KMAJ>
+struct F32Stage {
+  float4 v[2];
+  // rows r0 .. of R valid ones, k0 .. of kmax
+  __device__ __forceinline__ void load(const float* base, int64_t ld, int r0, int R, int k0, int kmax) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = (int)threadIdx.x + 256 * i;
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (KMAJ) {
+        const int r = r0 + (t >> 2), k = k0 + (t & 3) * 4;  // kmax is a multiple of 4
+        if (r < R && k < kmax) v[i] = *reinterpret_cast<const float4*>(base + r * ld + k);
+      } else {
+        const int k = k0 + (t >> 5), r = r0 + (t & 31) * 4;
+        if (k < kmax && r < R) v[i] = *reinterpret_cast<const float4*>(base + k * ld + r);  // padded rows
+      }
+    }
+  }
+  __device__ __forceinline__ void store(float (*s)[SLD]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = (int)threadIdx.x + 256 * i;
+      if (KMAJ) {
+        const int r = t >> 2, k = (t & 3) * 4;
+        s[k][r] = v[i].x;
+        s[k + 1][r] = v[i].y;
+        s[k + 2][r] = v[i].z;
+        s[k + 3][r] = v[i].w;
+      } else {
+        *reinterpret_cast<float4*>(&s[t >> 5][(t & 31) * 4]) = v[i];
+      }
+    }
+  }
+};
+template <bool AK, bool BKM, typename E>
+__global__ void __launch_bounds__(256) head_f32_kernel(GemmDesc g, E e) {
+  __shared__ __align__(16) float As[2][SK][SLD], Bs[2][SK][SLD];
+  const int nbm = (g.M + ST - 1) / ST, nbn = (g.N + ST - 1) / ST;
+  int tm, tn;
+  tile_coords(blockIdx.x, nbm, nbn, tm, tn);
+  const int m0 = tm * ST, n0 = tn * ST;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64, lr = lane & 31, lk = lane >> 5;
+  const int k_lo = blockIdx.z * g.ksplit, k_hi = min(g.K, k_lo + g.ksplit);
+  const int ka = min(g.ka, k_hi), kb = min(g.kb, k_hi);
+  const float* A = static_cast<const float*>(g.A);
+  const float* B = static_cast<const float*>(g.B);
+  Mma<32>::acc_t acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  F32Stage<AK> sa;
+  F32Stage<BKM> sb;
+  sa.load(A, g.lda, m0, g.M, k_lo, ka);
+  sb.load(B, g.ldb, n0, g.N, k_lo, kb);
+  sa.store(As[0]);
+  sb.store(Bs[0]);
+  int cur = 0;
+  for (int k0 = k_lo; k0 < k_hi; k0 += SK) {
+    __syncthreads();
+    sa.load(A, g.lda, m0, g.M, k0 + SK, ka);
+    sb.load(B, g.ldb, n0, g.N, k0 + SK, kb);
+#pragma unroll
+    for (int k = 0; k < SK; k += 2) {
+      float a[2], b[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        a[i] = As[cur][k + lk][wm + 32 * i + lr];
+        b[i] = Bs[cur][k + lk][wn + 32 * i + lr];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j], a[i], acc[i][j], 0, 0, 0);
+    }
+    cur ^= 1;
+    sa.store(As[cur]);
+    sb.store(Bs[cur]);
+  }
+  store_tile<ST, ST, 2, 2, 32>(acc, nullptr, g, e, m0, n0, wave, lane);
+}
+template <bool AK, bool BKM, typename E>
+static hipError_t run_head_f32(const GemmDesc& g, const E& e, hipStream_t s, int nz = 1) {
+  const int nb = ((g.M + ST - 1) / ST) * ((g.N + ST - 1) / ST);
+  hipLaunchKernelGGL((head_f32_kernel<AK, BKM, E>), dim3(nb, 1, nz), dim3(256), 0, s, g, e);
+  return hipGetLastError();
+}
+
+// --------------------------------------------------------------- target rows
+// A wave per row: the teacher's ids with absent ones and repetitions as -1, then the
+// label (-1: none), to tid [T, k + 1]; with a mask, a bit per named column.
+__global__ void __launch_bounds__(256) head_targets_kernel(int64_t T, int V, zl_targets t, int32_t* tid, uint32_t* mask,
+                                                           int64_t ldm) {
+  __shared__ int32_t ids[4][ZL_TARGETS_MAX_K];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = t.k;
+  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+  constexpr int PER = ZL_TARGETS_MAX_K / 64;
+  int32_t mine[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = lane + 64 * i;
+    mine[i] = -1;
+    if (row < T && e < k) {
+      const int32_t id = t.ids[row * k + e];
+      if (id >= 0 && id < V) mine[i] = id;
+    }
+    ids[wave][e] = mine[i];
+  }
+  if (row < T && mask)
+    for (int64_t w = lane; w < ldm; w += 64) mask[row * ldm + w] = 0;
+  __threadfence_block();
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = lane + 64 * i;
+    if (row >= T || e >= k) continue;
+    int32_t id = mine[i];
+    // the words of the mask are formed whole, by the first entry in each
+    uint32_t bits = 0;
+    bool first = true;
+    for (int f = 0; f < k && mine[i] >= 0; ++f) {
+      const int32_t o = ids[wave][f];
+      if (o < 0) continue;
+      if (f < e && o == mine[i]) id = -1;
+      if (o >> 5 == mine[i] >> 5) {
+        bits |= 1u << (o & 31);
+        first &= f >= e;
+      }
+    }
+    tid[row * (k + 1) + e] = id;
+    if (mask && mine[i] >= 0 && first) mask[row * ldm + (mine[i] >> 5)] = bits;
+  }
+  if (row < T && lane == 0) {
+    const int32_t y = t.labels ? t.labels[row] : -1;
+    tid[row * (k + 1) + k] = y >= 0 && y < V ? y : -1;
+  }
+}
+
+// The logits that the targets name: a wave per entry, x and w read 16 bytes a lane.
+// Column of stats: the label's 3, id e's 4 + e.
+template <bool BF>
+__global__ void __launch_bounds__(256) head_named_kernel(int64_t n, int d, int k, const void* x, int64_t ldx,
+                                                         const void* w, int64_t ldw, const int32_t* tid, float* stats) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= n) return;
+  const int64_t row = at / (k + 1);
+  const int e = (int)(at - row * (k + 1));
+  const int32_t id = tid[at];
+  float s = 0.f;
+  if (id >= 0) {
+    for (int c = lane * 8; c < d; c += 512) {
+      float a[8], b[8];
+      ldv_act(x, BF ? BF16 : F32, row * ldx + c, a);
+      ldv_act(w, BF ? BF16 : F32, id * ldw + c, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += a[i] * b[i];
+    }
+    s = wave_sum(s);
+  }
+  if (lane == 0) stats[row * (4 + k) + (e == k ? 3 : 4 + e)] = s;
+}
+
+// The teacher's distribution over a row's entries, a wave per row.
+struct WaveTeacher {
+  static constexpr int PER = ZL_TARGETS_MAX_K / 64;
+  float t[PER], p[PER];
+  bool on, rest;
+  float L, r, u;
+  __device__ __forceinline__ WaveTeacher(const zl_targets& q, int64_t row, const int32_t* id, int lane) {
+    const float inv = 1.f / q.temperature;
+    bool any = false, bad = false;
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = lane + 64 * i;
+      t[i] = -INFINITY;
+      if (e < q.k && id[e] >= 0) {
+        any = true;
+        t[i] = q.values[row * q.k + e] * inv;
+        bad |= t[i] != t[i];
+        m = fmaxf(m, t[i]);
+      }
+    }
+    u = q.rest ? q.rest[row] : -INFINITY;
+    m = fmaxf(wave_max(m), u);
+    on = __ballot(any) != 0 && (m != -INFINITY || __ballot(bad) != 0 || u != u);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) s += expf(t[i] - ref);
+    s = wave_sum(s) + expf(u - ref);
+    L = ref + logf(s);
+    rest = u != -INFINITY;
+    r = on && rest ? expf(u - L) : 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) p[i] = on ? expf(t[i] - L) : 0.f;
+  }
+};
+
+// Joins the partial sums of R rows, 256 / R strands of blocks each, then a wave per
+// row forms its losses.  PAIR: both log-sums; masked: the second leaves the
+// teacher's ids out.
+template <int R, bool PAIR>
+__global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int blocks, const float* part, zl_targets t, float a,
+                                                        float b, bool masked, const int32_t* tid, float* loss,
+                                                        float* stats) {
+  constexpr int S = 256 / R;
+  __shared__ float4 red[S][R];
+  const int r = threadIdx.x % R, st = threadIdx.x / R, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row0 = (int64_t)blockIdx.x * R;
+  const float inv = t.ids ? 1.f / t.temperature : 1.f, c2 = inv * LOG2E;
+  LogSum x, y;
+  if (row0 + r < T) {
+#pragma unroll 4
+    for (int j = st; j < blocks; j += S) {
+      if constexpr (PAIR) {
+        const float4 v = *reinterpret_cast<const float4*>(part + ((int64_t)j * T + row0 + r) * 4);
+        x.merge(v.x, v.y, LOG2E);
+        y.merge(v.z, v.w, c2);
+      } else {
+        const float2 v = *reinterpret_cast<const float2*>(part + ((int64_t)j * T + row0 + r) * 2);
+        y.merge(v.x, v.y, c2);
+      }
+    }
+  }
+  red[st][r] = make_float4(x.m, x.s, y.m, y.s);
+  __syncthreads();
+  for (int i = wave; i < R; i += 4) {
+    const int64_t row = row0 + i;
+    if (row >= T) break;
+    // the strands in a fixed tree over the lanes
+    LogSum p, q;
+    for (int j = lane; j < S; j += 64) {
+      const float4 v = red[j][i];
+      p.merge(v.x, v.y, LOG2E);
+      q.merge(v.z, v.w, c2);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      // both lanes of a pair must see the sums before either changes
+      const float pm = __shfl_xor(p.m, o, 64), ps = __shfl_xor(p.s, o, 64);
+      const float qm = __shfl_xor(q.m, o, 64), qs = __shfl_xor(q.s, o, 64);
+      p.merge(pm, ps, LOG2E);
+      q.merge(qm, qs, c2);
+    }
+    const int32_t* id = tid + row * (t.k + 1);
+    float* out = stats + row * (4 + t.k);
+    const bool label = id[t.k] >= 0;
+    float total = 0.f, lt = 0.f, other = 0.f, l1 = 0.f;
+    bool on = false;
+    if (t.ids) {
+      const WaveTeacher w(t, row, id, lane);
+      on = w.on;
+      float z[WaveTeacher::PER], kl = 0.f;
+      LogSum n;
+#pragma unroll
+      for (int j = 0; j < WaveTeacher::PER; ++j) {
+        const int e = lane + 64 * j;
+        z[j] = 0.f;
+        if (e < t.k && id[e] >= 0) {
+          z[j] = out[4 + e];
+          n.raise(z[j], c2);
+          n.s += n.m == -INFINITY ? 0.f : expf((z[j] - n.m) * inv);
+        }
+        if (w.p[j] > 0.f || w.p[j] != w.p[j]) kl += w.p[j] * (w.t[j] - z[j] * inv);
+      }
+      if (masked) {
+        other = q.log(inv);
+        const float nm = wave_max(n.m);
+        const float ns = wave_sum(n.m == -INFINITY ? n.s : n.s * expf((n.m - nm) * inv));
+        q.merge(nm, ns, c2);
+      }
+      lt = q.log(inv);
+      kl = wave_sum(kl) + lt - w.L;
+      if (masked && w.r != 0.f) kl += w.r * (w.u - other);
+      if (on) total = b * t.temperature * t.temperature * kl;
+    } else {
+      lt = q.log(inv);
+    }
+    l1 = PAIR ? p.log(1.f) : lt;
+    if (lane == 0) {
+      if (label) total += a * (l1 - out[3]);
+      if (!label && !on) total = 0.f;
+      loss[row] = total;
+      out[0] = label ? l1 : 0.f;
+      out[1] = on ? lt : 0.f;
+      out[2] = on && masked ? other : 0.f;
+    }
+  }
+}
+
+// The largest |dloss| (0 and what is not finite count as 1).
+__global__ void __launch_bounds__(1024) head_gmax_kernel(int64_t T, const float* dloss, float* gmax) {
+  __shared__ float red[16];
+  float m = 0.f;
+  for (int64_t i = threadIdx.x; i < T; i += 1024) m = fmaxf(m, dloss ? fabsf(dloss[i]) : 1.f);
+  m = block_max<1024>(m, red);
+  if (threadIdx.x == 0) *gmax = m > 0.f && m < INFINITY ? m : 1.f;
+}
+
+// Per row what dL/dz takes (GradEpi), and the named columns' values; a wave per row.
+__global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, zl_targets t, float a, float b, bool two,
+                                                        const float* stats, const float* dloss, const float* gmax,
+                                                        int32_t* tid, float* tval, float4* coef, int32_t* live) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= T) return;
+  const float* s = stats + row * (4 + t.k);
+  int32_t* id = tid + row * (t.k + 1);
+  float* val = tval + row * (t.k + 1);
+  const float l1 = s[0], ls = s[1], lo = s[2];
+  const int y = id[t.k];
+  const float up = (dloss ? dloss[row] : 1.f) / *gmax;
+  const float c1 = y >= 0 ? a * up : 0.f;
+  float ct = 0.f, lt = ls, inv = 1.f;
+  bool named = false, on = false;
+  if (t.ids) {
+    const WaveTeacher w(t, row, id, lane);
+    inv = 1.f / t.temperature;
+    on = w.on;
+    const float f = on ? b * t.temperature * up : 0.f;
+    ct = f;
+    if (on && t.rest) {
+      lt = lo;
+      ct = lo == -INFINITY ? 0.f : f * (expf(lo - ls) - w.r);
+    }
+#pragma unroll
+    for (int i = 0; i < WaveTeacher::PER; ++i) {
+      const int e = lane + 64 * i;
+      if (e < t.k && id[e] >= 0) {
+        const float z = s[4 + e];
+        float g = on ? f * (expf(z * inv - ls) - w.p[i]) : 0.f;
+        if (y >= 0) g += c1 * (id[e] == y ? expm1f(z - l1) : expf(z - l1));
+        val[e] = g;
+        named |= id[e] == y;
+      }
+    }
+  }
+  named = __ballot(named) != 0;
+  if (lane == 0) {
+    if (y >= 0 && !named) {
+      float g = c1 * expm1f(s[3] - l1);
+      if (ct != 0.f) g += ct * expf(s[3] * inv - lt);
+      val[t.k] = g;
+    }
+    float4 c = make_float4(c1, l1, ct, lt);
+    if (!two) {
+      // one exponential: labels or a teacher alone, or both at tau = 1 without a rest
+      c.z = ct + c1;
+      if (!on) c.w = l1;
+    }
+    coef[row] = c;
+    live[row] = on || y >= 0;
+  }
+  // an entry of the label that an id names too is that id's
+  if (named && lane == 0) id[t.k] = -2 - y;
+}
+
+// The named columns of the piece [v0, v0 + n) over what the product wrote.
+__global__ void __launch_bounds__(256) head_put_kernel(int64_t count, int k, int v0, int n, const int32_t* tid,
+                                                       const float* tval, void* dz, int64_t ldz, int dtype) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= count) return;
+  const int32_t id = tid[i];
+  if (id < v0 || id >= v0 + n) return;
+  st_act(dz, dtype, i / (k + 1) * ldz + (id - v0), tval[i]);
+}
+
+// x with zeros in the rows that have no target (0 times NaN would spoil dw).
+__global__ void __launch_bounds__(256) head_clean_kernel(int64_t T, int d, const int32_t* live, const void* x,
+                                                         int64_t ldx, void* xc, int dtype) {
+  const int per = d / 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = i / per;
+  if (row >= T) return;
+  const int c = (int)(i - row * per) * 8;
+  const bool on = live[row] != 0;
+  if (dtype == BF16) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (on) v = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(x) + row * ldx + c);
+    *reinterpret_cast<uint4*>(static_cast<bf16_t*>(xc) + row * d + c) = v;
+  } else {
+    float4 v[2] = {};
+    if (on) {
+      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + row * ldx + c);
+      v[0] = p[0];
+      v[1] = p[1];
+    }
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(xc) + row * d + c);
+    o[0] = v[0];
+    o[1] = v[1];
+  }
+}
+
+// out = (accumulate ? out : 0) + scale * gmax * the sum of nz fp32 [rows, d], in order.
+__global__ void __launch_bounds__(256) head_finish_kernel(int64_t rows, int d, const float* in, int nz, float scale,
+                                                          const float* gmax, void* out, int64_t ldo, int dtype,
+                                                          int accumulate) {
+  const int per = d / 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = i / per;
+  if (row >= rows) return;
+  const int c = (int)(i - row * per) * 8;
+  const float f = gmax ? scale * *gmax : scale;
+  float v[8], u[8];
+  ldv_f32(in + row * d + c, v);
+  for (int z = 1; z < nz; ++z) {
+    ldv_f32(in + z * rows * d + row * d + c, u);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += u[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] *= f;
+  if (accumulate) {
+    ldv_f32(static_cast<const float*>(out) + row * ldo + c, u);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += u[k];
+  }
+  stv_act(out, dtype, row * ldo + c, v);
+}
+
+__global__ void __launch_bounds__(256) head_zero_kernel(int64_t rows, int d, void* out, int64_t ldo, int dtype) {
+  const int per = d / 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * per) return;
+  const float v[8] = {};
+  stv_act(out, dtype, i / per * ldo + i % per * 8, v);
+}
+
+// ------------------------------------------------------------------ launches
+static unsigned grid(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
+
+HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool rest, bool backward, bool need_dx, bool need_dw,
+                   int columns) {
+  HeadPlan p;
+  memset(&p, 0, sizeof(p));
+  const int64_t es = dtype == BF16 ? 2 : 4;
+  if (dtype == BF16) {
+    GemmShape sh = {(int)T, V, d, true, true, false, 0, false, 0};
+    p.large = plan_gemm(sh).large;
+  }
+  const int width = p.large ? 128 : 64;  // columns of a wave tile
+  p.blocks = (V + width - 1) / width;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += (bytes + 255) / 256 * 256;
+    return o;
+  };
+  p.tid = take(T * (k + 1) * 4);
+  if (!backward) {
+    p.part = take((size_t)p.blocks * T * 16);
+    p.ldm = ((int64_t)V + 127) / 128 * 4;
+    if (rest) p.mask = take(T * p.ldm * 4);
+  } else {
+    // a piece of dL/dz has at most 1 GiB
+    const int64_t all = ((int64_t)V + 255) / 256 * 256;
+    int64_t most = ((int64_t)1 << 30) / (es * (T ? T : 1)) / 256 * 256;
+    if (most < 256) most = 256;
+    int64_t c = columns ? ((int64_t)columns + 255) / 256 * 256 : most;
+    if (c > most) c = most;
+    if (c > all) c = all;
+    p.columns = (int)c;
+    p.ldz = c;
+    p.tval = take(T * (k + 1) * 4);
+    p.gmax = take(4);
+    p.coef = take(T * 16);
+    p.live = take(T * 4);
+    p.dz = take(T * p.ldz * es);
+    if (need_dx) p.dxa = take(T * (int64_t)d * 4);
+    if (need_dw) p.xc = take(T * (int64_t)d * es);
+    const int64_t rows = need_dw && c > T ? c : T;
+    int64_t n = 64 * rows * d;
+    if (n > (int64_t)1 << 24) n = (int64_t)1 << 24;
+    p.split_elems = (size_t)n;
+    p.split = take(n * 4);
+  }
+  p.bytes = at;
+  return p;
+}
+
+static GemmDesc head_gemm(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, bool ak, const void* B,
+                          int64_t ldb, bool bk) {
+  GemmDesc g;
+  memset(&g, 0, sizeof(g));
+  g.M = (int)M;
+  g.N = (int)N;
+  g.K = g.ka = g.kb = g.ksplit = (int)K;
+  g.A = A;
+  g.lda = lda;
+  g.a_kmajor = ak;
+  g.B = B;
+  g.ldb = ldb;
+  g.b_kmajor = bk;
+  return g;
+}
+
+#define ZL_TRY(x)                        \
+  do {                                   \
+    const hipError_t err_ = (x);         \
+    if (err_ != hipSuccess) return err_; \
+  } while (0)
+
+hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
+  const int64_t T = a.T;
+  if (T == 0) return hipSuccess;
+  const zl_targets& t = a.targets;
+  const bool bf = a.dtype == BF16, hard = t.labels != nullptr, soft = t.ids != nullptr, masked = soft && t.rest;
+  const bool pair = hard && soft && (masked || t.temperature != 1.f);
+  const HeadPlan p = head_plan(T, a.V, a.d, bf ? BF16 : F32, t.k, masked, false, false, false, 0);
+  char* ws = static_cast<char*>(a.workspace);
+  int32_t* tid = reinterpret_cast<int32_t*>(ws + p.tid);
+  float* part = reinterpret_cast<float*>(ws + p.part);
+  uint32_t* mask = masked ? reinterpret_cast<uint32_t*>(ws + p.mask) : nullptr;
+  float wa, wb;
+  loss_weights(t, wa, wb);
+  hipLaunchKernelGGL(head_targets_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, a.V, t, tid, mask, p.ldm);
+  const int64_t named = T * (t.k + 1);
+  if (bf)
+    hipLaunchKernelGGL((head_named_kernel<true>), dim3(grid(named, 4)), dim3(256), 0, s, named, a.d, t.k, a.x, a.ldx, a.w,
+                       a.ldw, tid, a.stats);
+  else
+    hipLaunchKernelGGL((head_named_kernel<false>), dim3(grid(named, 4)), dim3(256), 0, s, named, a.d, t.k, a.x, a.ldx, a.w,
+                       a.ldw, tid, a.stats);
+  // a masked sum is always the second of a pair
+  const int two = pair || masked;
+  const StatEpi e = {two, soft ? LOG2E / t.temperature : LOG2E, part, T, mask, p.ldm};
+  const GemmDesc g = head_gemm(T, a.V, a.d, a.x, a.ldx, true, a.w, a.ldw, true);
+  if (bf) ZL_TRY((run_head<true, true>(g, e, p.large, s)));
+  else ZL_TRY((run_head_f32<true, true>(g, e, s)));
+  auto rows = [&](auto rc, auto pc) {
+    constexpr int R = decltype(rc)::value;
+    constexpr bool P = decltype(pc)::value;
+    hipLaunchKernelGGL((head_rows_kernel<R, P>), dim3(grid(T, R)), dim3(256), 0, s, T, p.blocks, part, t, wa, wb, masked,
+                       tid, a.loss, a.stats);
+  };
+  using std::integral_constant;
+  auto by_rows = [&](auto pc) {
+    if (T >= 4096) rows(integral_constant<int, 32>{}, pc);
+    else if (T >= 64) rows(integral_constant<int, 4>{}, pc);
+    else rows(integral_constant<int, 1>{}, pc);
+  };
+  if (two) by_rows(std::true_type{});
+  else by_rows(std::false_type{});
+  return hipGetLastError();
+}
+
+// Splits of an fp32 product's K: up to two blocks a CU, 128 of K each at least.
+static int f32_splits(int64_t M, int64_t N, int64_t K, size_t elems, int& ksplit) {
+  const int64_t tiles = ((M + ST - 1) / ST) * ((N + ST - 1) / ST);
+  int64_t nz = tiles >= 256 ? 1 : 512 / tiles;
+  if (nz > K / 128) nz = K / 128;
+  if (nz > (int64_t)(elems / (size_t)(M * N))) nz = (int64_t)(elems / (size_t)(M * N));
+  if (nz < 1) nz = 1;
+  return split_k((int)K, (int)nz, SK, ksplit);
+}
+
+hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
+  const int64_t T = a.T;
+  const int d = a.d;
+  const bool bf = a.dtype == BF16;
+  const int dt = bf ? BF16 : F32, dxt = a.dx_dtype == ZL_BF16 ? BF16 : F32, dwt = a.dw_dtype == ZL_BF16 ? BF16 : F32;
+  if (T == 0) {
+    if (a.dw && !a.accumulate)
+      hipLaunchKernelGGL(head_zero_kernel, dim3(grid((int64_t)a.V * (d / 8), 256)), dim3(256), 0, s, a.V, d, a.dw, a.lddw, dwt);
+    return hipGetLastError();
+  }
+  const zl_targets& t = a.targets;
+  const bool hard = t.labels != nullptr, soft = t.ids != nullptr, rest = soft && t.rest;
+  const int two = hard && soft && (rest || t.temperature != 1.f);
+  const HeadPlan p = head_plan(T, a.V, d, dt, t.k, rest, true, a.dx != nullptr, a.dw != nullptr, a.columns);
+  char* ws = static_cast<char*>(a.workspace);
+  int32_t* tid = reinterpret_cast<int32_t*>(ws + p.tid);
+  float* tval = reinterpret_cast<float*>(ws + p.tval);
+  float* gmax = reinterpret_cast<float*>(ws + p.gmax);
+  float4* coef = reinterpret_cast<float4*>(ws + p.coef);
+  int32_t* live = reinterpret_cast<int32_t*>(ws + p.live);
+  float* dxa = reinterpret_cast<float*>(ws + p.dxa);
+  float* split = reinterpret_cast<float*>(ws + p.split);
+  void* dz = ws + p.dz;
+  void* xc = ws + p.xc;
+  float wa, wb;
+  loss_weights(t, wa, wb);
+  hipLaunchKernelGGL(head_targets_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, a.V, t, tid, (uint32_t*)nullptr, (int64_t)0);
+  hipLaunchKernelGGL(head_gmax_kernel, dim3(1), dim3(1024), 0, s, T, a.dloss, gmax);
+  hipLaunchKernelGGL(head_coef_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, t, wa, wb, two != 0, a.stats, a.dloss, gmax,
+                     tid, tval, coef, live);
+  if (a.dw)
+    hipLaunchKernelGGL(head_clean_kernel, dim3(grid(T * (d / 8), 256)), dim3(256), 0, s, T, d, live, a.x, a.ldx, xc, dt);
+  ZL_TRY(hipGetLastError());
+  const size_t es = bf ? 2 : 4;
+  for (int v0 = 0; v0 < a.V; v0 += p.columns) {
+    const int n = a.V - v0 < p.columns ? a.V - v0 : p.columns;
+    const int n8 = (n + 7) / 8 * 8;
+    const char* w = static_cast<const char*>(a.w) + (size_t)v0 * a.ldw * es;
+    {
+      const GradEpi e = {coef, two, soft ? 1.f / t.temperature : 1.f, dz, p.ldz, dt};
+      const GemmDesc g = head_gemm(T, n, d, a.x, a.ldx, true, w, a.ldw, true);
+      GemmShape sh = {(int)T, n, d, true, true, false, 0, false, 0};
+      if (bf) ZL_TRY((run_head<true, true>(g, e, plan_gemm(sh).large, s)));
+      else ZL_TRY((run_head_f32<true, true>(g, e, s)));
+    }
+    const int64_t named = T * (t.k + 1);
+    hipLaunchKernelGGL(head_put_kernel, dim3(grid(named, 256)), dim3(256), 0, s, named, t.k, v0, n, tid, tval, dz, p.ldz, dt);
+    ZL_TRY(hipGetLastError());
+    if (a.dx) {
+      GemmDesc g = head_gemm(T, d, n8, dz, p.ldz, true, w, a.ldw, false);
+      g.kb = n;
+      if (bf) {
+        g.part = split;
+        g.part_elems = p.split_elems;
+        EpiArgs e;
+        memset(&e, 0, sizeof(e));
+        e.kind = EPI_GRAD;
+        e.out = dxa;
+        e.ldo = d;
+        e.out_dtype = F32;
+        e.scale = 1.f;
+        e.accumulate = v0 > 0;
+        ZL_TRY(launch_gemm(g, e, BF16, s));
+      } else {
+        const int nz = f32_splits(T, d, n8, p.split_elems, g.ksplit);
+        OutEpi e = {dxa, d, F32, 1.f, nullptr, v0 > 0, 0};
+        if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, T * d};
+        ZL_TRY((run_head_f32<true, false>(g, e, s, nz)));
+        if (nz > 1)
+          hipLaunchKernelGGL(head_finish_kernel, dim3(grid(T * (d / 8), 256)), dim3(256), 0, s, T, d, split, nz, 1.f,
+                             (const float*)nullptr, dxa, (int64_t)d, (int)F32, (int)(v0 > 0));
+      }
+    }
+    if (a.dw) {
+      GemmDesc g = head_gemm(n, d, T, dz, p.ldz, false, xc, d, false);
+      char* out = static_cast<char*>(a.dw) + (size_t)v0 * a.lddw * (dwt == BF16 ? 2 : 4);
+      int nz = 1;
+      bool large = false;
+      if (bf) {
+        GemmShape sh = {n, d, (int)T, false, false, true, p.split_elems, false, 0};
+        const GemmPlan pl = plan_gemm(sh);
+        large = pl.large;
+        nz = split_k((int)T, pl.nz, KTile<false, false>::BK, g.ksplit);
+      } else {
+        nz = f32_splits(n, d, T, p.split_elems, g.ksplit);
+      }
+      OutEpi e = {out, a.lddw, dwt, a.scale, gmax, a.accumulate, 0};
+      if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, (int64_t)n * d};
+      if (bf) ZL_TRY((run_head<false, false>(g, e, large, s, nz)));
+      else ZL_TRY((run_head_f32<false, false>(g, e, s, nz)));
+      if (nz > 1)
+        hipLaunchKernelGGL(head_finish_kernel, dim3(grid((int64_t)n * (d / 8), 256)), dim3(256), 0, s, (int64_t)n, d, split,
+                           nz, a.scale, gmax, (void*)out, a.lddw, dwt, a.accumulate);
+    }
+  }
+  if (a.dx)
+    hipLaunchKernelGGL(head_finish_kernel, dim3(grid(T * (d / 8), 256)), dim3(256), 0, s, T, d, dxa, 1, a.scale, gmax, a.dx,
+                       a.lddx, dxt, 0);
+  return hipGetLastError();
+}
+
+}  // namespace zl

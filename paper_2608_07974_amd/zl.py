@@ -1,4 +1,4 @@
-"""ctypes binding of libzl (include/zl.h, zl_inspect.h, zl_runtime.h, zl_layer.h).
+"""ctypes binding of libzl (include/zl.h, zl_inspect.h, zl_runtime.h, zl_layer.h, zl_loss.h).
 
 Argument marshalling only: every function here forwards to the C call of the
 same name, raising ZlError on a negative status.  Pointers are plain ints
@@ -19,6 +19,7 @@ ZL_F32, ZL_BF16 = 0, 1
 ZL_KL_REVERSE, ZL_KL_FORWARD = 0, 1
 ZL_ADAMW, ZL_SGD = 0, 1
 ZL_MLP_SWIGLU, ZL_MLP_GELU = 0, 1
+ZL_TARGETS_MAX_K = 256
 
 EXPORTED = [
     "zl_param_layout", "zl_workspace_size", "zl_chunk_create", "zl_chunk_destroy",
@@ -33,6 +34,8 @@ EXPORTED = [
     "zl_kernel_attention_bwd_noalloc",
     "zl_pack", "zl_unpack", "zl_mlp_act", "zl_mlp_act_backward", "zl_block_norm",
     "zl_block_norm_backward", "zl_block_norm_workspace", "zl_wgrad_packed", "zl_rotary",
+    "zl_top_logits", "zl_logit_loss", "zl_logit_loss_backward", "zl_head_loss", "zl_head_loss_backward",
+    "zl_head_loss_workspace",
 ]
 
 
@@ -120,10 +123,29 @@ class zl_norm_args(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_elems", ctypes.c_size_t)]
 
 
+class zl_targets(ctypes.Structure):
+    _fields_ = [("labels", ctypes.c_void_p), ("ids", ctypes.c_void_p), ("values", ctypes.c_void_p),
+                ("rest", ctypes.c_void_p), ("k", ctypes.c_int), ("alpha", ctypes.c_float),
+                ("temperature", ctypes.c_float)]
+
+
+class zl_head_args(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("V", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("w", ctypes.c_void_p),
+                ("ldw", ctypes.c_int64), ("targets", zl_targets), ("stats", ctypes.c_void_p),
+                ("loss", ctypes.c_void_p), ("dloss", ctypes.c_void_p), ("scale", ctypes.c_float),
+                ("columns", ctypes.c_int), ("dx", ctypes.c_void_p), ("lddx", ctypes.c_int64),
+                ("dx_dtype", ctypes.c_int), ("dw", ctypes.c_void_p), ("lddw", ctypes.c_int64),
+                ("dw_dtype", ctypes.c_int), ("accumulate", ctypes.c_int),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 # The same argument structures as bytes, made in one step (a ctypes structure of 40
 # fields takes three times the launch): functions below take either.
 pack_packed = struct.Struct("@PPqq").pack
 pack_mlp_args = struct.Struct("@qiiiiPq" "PPqq" "PqPqPq").pack
+pack_targets = struct.Struct("@PPPPiff0P").pack
+pack_head_args = struct.Struct("@qiiiPqPq" "PPPPiff0P" "PPPfiPqiPqiiPN").pack
 pack_norm_args = struct.Struct("@qiiiiffPPPPPqPPPqPqPq" "PPqq" "PPqq" "PPPPPPPPPfiPN").pack
 
 
@@ -197,6 +219,12 @@ def load(path=None):
                             vp],
         "zl_rotary": [i64, c, c, c, vp, i64, vp, i64, c, vp, c, ctypes.c_char_p, ctypes.c_double, c,
                       vp],
+        "zl_top_logits": [i64, c, vp, i64, c, c, ctypes.c_float, vp, vp, vp, vp],
+        "zl_logit_loss": [i64, c, vp, i64, c, vp, vp, vp, vp],
+        "zl_logit_loss_backward": [i64, c, vp, i64, c, vp, vp, vp, ctypes.c_float, vp, i64, vp],
+        "zl_head_loss": [vp, vp],
+        "zl_head_loss_backward": [vp, vp],
+        "zl_head_loss_workspace": [i64, c, c, c, c, c, c, c, c, c, P(sz)],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -487,6 +515,38 @@ def zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes, a
         n_heads, head_dim, rot, n_axes = _int(n_heads), _int(head_dim), _int(rot), _int(n_axes)
     _check(load().zl_rotary(T, n_heads, head_dim, rot, x, ldx, out, ldo, dtype, pos, n_axes, axis_of,
                             theta, int(inverse), stream), "zl_rotary")
+
+
+def zl_top_logits(T, V, x, ldx, dtype, k, temperature, ids, values, rest, stream=0):
+    if (V | k) >> 31:
+        V, k = _int(V), _int(k)
+    _check(load().zl_top_logits(T, V, x, ldx, dtype, k, temperature, ids, values, rest, stream), "zl_top_logits")
+
+
+def zl_logit_loss(T, V, z, ldz, dtype, targets, loss, stats, stream=0):
+    _check(load().zl_logit_loss(T, _int(V) if V >> 31 else V, z, ldz, dtype, _ref(targets), loss, stats, stream),
+           "zl_logit_loss")
+
+
+def zl_logit_loss_backward(T, V, z, ldz, dtype, targets, stats, dloss, scale, dz, lddz, stream=0):
+    _check(load().zl_logit_loss_backward(T, _int(V) if V >> 31 else V, z, ldz, dtype, _ref(targets), stats, dloss, scale,
+                                         dz, lddz, stream), "zl_logit_loss_backward")
+
+
+def zl_head_loss(args, stream=0):
+    _check(load().zl_head_loss(_ref(args), stream), "zl_head_loss")
+
+
+def zl_head_loss_backward(args, stream=0):
+    _check(load().zl_head_loss_backward(_ref(args), stream), "zl_head_loss_backward")
+
+
+def zl_head_loss_workspace(T, V, d, dtype, k=0, has_rest=0, backward=0, need_dx=1, need_dw=0, columns=0):
+    """Bytes of workspace of zl_head_loss, or of zl_head_loss_backward."""
+    n = ctypes.c_size_t()
+    _check(load().zl_head_loss_workspace(T, _int(V), _int(d), dtype, _int(k), int(has_rest), int(backward), int(need_dx),
+                                         int(need_dw), _int(columns), ctypes.byref(n)), "zl_head_loss_workspace")
+    return n.value
 
 
 def zl_profile_end(h, max_entries=256):
