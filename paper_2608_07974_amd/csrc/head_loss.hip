@@ -22,19 +22,25 @@ namespace zl {
 
 // Partial sums.  PAIR false: (max z, sum exp((z - max) c)).  PAIR true: those of
 // z at c = 1 over all columns and of z at c over the columns without a mask bit.
+template <bool PAIR>
 struct StatEpi {
-  int pair;
   float c2;               // log2(e) / tau
   float* part;            // [blocks, T, 2 or 4]
   int64_t T;
   const uint32_t* mask;   // [T, ldm] or null
   int64_t ldm;
 };
-// dL/dz of the columns [0, N) of a piece, zeros up to the row stride.
+// dL/dz of the columns [0, N) of a piece, zeros up to the row stride:
+//   GRAD_ONE   ct exp(z / tau - lt)
+//   GRAD_TWO   c1 exp(z - l1) + ct exp(z / tau - lt)
+//   GRAD_SQUARE  the same at tau = 2, where with e = exp(z / 2 - lt) the first term is
+//     c1 exp(2 lt - l1) e^2 (c1 holds the product): one exponential for two, 16 of the
+//     44 cycles that a wave spends per element
+enum { GRAD_ONE, GRAD_TWO, GRAD_SQUARE };
+template <int MODE>
 struct GradEpi {
   const float4* coef;     // [T]: c1, l1, ct, lt
-  int two;                // c1 exp(z - l1) + ct exp(z / tau - lt), else the latter alone
-  float inv;
+  float inv;              // 1 / tau
   void* dz;
   int64_t ldz;
   int dtype;
@@ -49,8 +55,8 @@ struct OutEpi {
   int accumulate;
   int64_t zstride;
 };
-template <> struct EpiTransposed<StatEpi> { static constexpr bool value = true; };
-template <> struct EpiTransposed<GradEpi> { static constexpr bool value = true; };
+template <bool PAIR> struct EpiTransposed<StatEpi<PAIR>> { static constexpr bool value = true; };
+template <int MODE> struct EpiTransposed<GradEpi<MODE>> { static constexpr bool value = true; };
 template <> struct EpiTransposed<OutEpi> { static constexpr bool value = true; };
 
 // The lanes that hold one row are MF apart.
@@ -61,9 +67,41 @@ __device__ __forceinline__ float across(float x, F&& f) {
   return x;
 }
 
-template <int BM, int BN, int WM, int WN, int MF = 32>
+// bf16 results of MF rows of a wave's tile, four columns a lane, leave through LDS as
+// rows of 16 bytes a lane: straight from the accumulators a store would touch 16 or
+// 32 rows with 32 or 16 bytes each (dL/dz of 4096 x 50257 x 768: 419 us, 366 so).  The
+// region is the wave's own; its accesses to LDS stay in order.
+template <int TN, int MF>
+struct RowsOut {
+  static constexpr int LD = TN + 8;  // elements; 16 bytes of padding spread the rows over the banks
+  static constexpr int BYTES = MF * LD * 2;
+  bf16_t* lds;
+  int lane;
+  __device__ __forceinline__ RowsOut(unsigned char* smem, int wave, int lane_)
+      : lds(reinterpret_cast<bf16_t*>(smem + wave * BYTES)), lane(lane_) {}
+  // columns n .. n + 3 of this lane's row
+  __device__ __forceinline__ void put(int n, uint2 v) { *reinterpret_cast<uint2*>(lds + (lane & (MF - 1)) * LD + n) = v; }
+  // f(row, column, 8 values)
+  template <typename F>
+  __device__ __forceinline__ void flush(F&& f) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    constexpr int LPR = TN / 8;
+#pragma unroll
+    for (int it = 0; it < MF * LPR / 64; ++it) {
+      const int r = it * (64 / LPR) + lane / LPR, c = lane % LPR * 8;
+      f(r, c, *reinterpret_cast<const uint4*>(lds + r * LD + c));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+};
+
+template <int BM, int BN, int WM, int WN, int MF = 32, bool PAIR>
 __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[BM / WM / MF][BN / WN / MF],
-                                           unsigned char*, const GemmDesc& g, const StatEpi& e, int m0, int n0,
+                                           unsigned char*, const GemmDesc& g, const StatEpi<PAIR>& e, int m0, int n0,
                                            int wave, int lane) {
   constexpr int TM = BM / WM, TN = BN / WN, FM = TM / MF, FN = TN / MF, NR = Mma<MF>::NR;
   const int wm = wave / WN, wn = wave % WN;
@@ -96,7 +134,7 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
       s = across<MF>(s, add2);
     };
     float mx, s;
-    if (!e.pair) {
+    if constexpr (!PAIR) {
       sums(e.c2, mx, s);
       if (lane < MF && m < g.M) *reinterpret_cast<float2*>(e.part + (block * e.T + m) * 2) = make_float2(mx, s);
     } else {
@@ -119,51 +157,75 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
   });
 }
 
-template <int BM, int BN, int WM, int WN, int MF = 32>
+// In fp32 the exponent's argument is a difference before it is scaled; where the
+// result is rounded to bf16 one fused operation does (off by |lt| 2^-24 at most, 2^-8
+// follow).  Rows without a target have coefficients 0; their logits may be NaN, so
+// the finished words are masked.
+template <int BM, int BN, int WM, int WN, int MF = 32, int MODE>
 __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[BM / WM / MF][BN / WN / MF],
-                                           unsigned char*, const GemmDesc& g, const GradEpi& e, int m0, int n0,
+                                           unsigned char* smem, const GemmDesc& g, const GradEpi<MODE>& e, int m0, int n0,
                                            int wave, int lane) {
   constexpr int TM = BM / WM, TN = BN / WN, FM = TM / MF, FN = TN / MF, NR = Mma<MF>::NR;
   const int wm = wave / WN, wn = wave % WN;
+  const int nb = n0 + wn * TN;
+  const bool cut = nb + TN > g.N, bf = e.dtype == BF16;
+  RowsOut<TN, MF> rows(smem, wave, lane);
+  const float ci = e.inv * LOG2E;
   static_for<0, FM>([&](auto ic) __attribute__((always_inline)) {
     constexpr int i = decltype(ic)::value;
     const int m = m0 + wm * TM + i * MF + (lane & (MF - 1));
-    const float4 c = m < g.M ? e.coef[m] : make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (m < g.M) c = e.coef[m];
+    const uint32_t live = c.x != 0.f || c.z != 0.f ? 0xffffffffu : 0u;  // (NaN is not 0)
+    const float wt = c.w * LOG2E, w1 = c.y * LOG2E;
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r0 = 0; r0 < NR; r0 += 4) {
-        const int n = n0 + wn * TN + j * MF + Mma<MF>::row(lane, r0);
+        const int n = nb + j * MF + Mma<MF>::row(lane, r0);
         float o[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float v = acc[i][j][r0 + r];
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v, e.inv, -c.w) * LOG2E);
-          o[r] = c.z != 0.f ? c.z * p : 0.f;
-          if (e.two) {
-            const float q = __builtin_amdgcn_exp2f((v - c.y) * LOG2E);
-            o[r] += c.x != 0.f ? c.x * q : 0.f;
+          const float p = __builtin_amdgcn_exp2f(bf ? __builtin_fmaf(v, ci, -wt) : __builtin_fmaf(v, e.inv, -c.w) * LOG2E);
+          if constexpr (MODE == GRAD_ONE) {
+            o[r] = c.z * p;
+          } else if constexpr (MODE == GRAD_SQUARE) {
+            o[r] = p * __builtin_fmaf(p, c.x, c.z);
+          } else {
+            const float q = __builtin_amdgcn_exp2f(bf ? __builtin_fmaf(v, LOG2E, -w1) : (v - c.y) * LOG2E);
+            o[r] = __builtin_fmaf(c.x, q, c.z * p);
           }
-          if (n + r >= g.N) o[r] = 0.f;
         }
-        if (m < g.M && n < e.ldz) {
-          if (e.dtype == BF16)
-            *reinterpret_cast<uint2*>(static_cast<bf16_t*>(e.dz) + m * e.ldz + n) =
-                make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
-          else
-            *reinterpret_cast<float4*>(static_cast<float*>(e.dz) + m * e.ldz + n) = make_float4(o[0], o[1], o[2], o[3]);
+        if (cut) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r >= g.N) o[r] = 0.f;
         }
+        if (bf)
+          rows.put(n - nb, make_uint2(pack_bf16(o[0], o[1]) & live, pack_bf16(o[2], o[3]) & live));
+        else if (m < g.M && n < e.ldz)
+          *reinterpret_cast<uint4*>(static_cast<float*>(e.dz) + m * e.ldz + n) =
+              make_uint4(__builtin_bit_cast(uint32_t, o[0]) & live, __builtin_bit_cast(uint32_t, o[1]) & live,
+                         __builtin_bit_cast(uint32_t, o[2]) & live, __builtin_bit_cast(uint32_t, o[3]) & live);
       }
+    if (bf)
+      rows.flush([&](int r, int c, uint4 v) __attribute__((always_inline)) {
+        const int mr = m0 + wm * TM + i * MF + r;
+        if (mr < g.M && nb + c < e.ldz) *reinterpret_cast<uint4*>(static_cast<bf16_t*>(e.dz) + mr * e.ldz + nb + c) = v;
+      });
   });
 }
 
 template <int BM, int BN, int WM, int WN, int MF = 32>
 __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[BM / WM / MF][BN / WN / MF],
-                                           unsigned char*, const GemmDesc& g, const OutEpi& e, int m0, int n0,
+                                           unsigned char* smem, const GemmDesc& g, const OutEpi& e, int m0, int n0,
                                            int wave, int lane) {
   constexpr int TM = BM / WM, TN = BN / WN, FM = TM / MF, FN = TN / MF, NR = Mma<MF>::NR;
   const int wm = wave / WN, wn = wave % WN;
+  const int nb = n0 + wn * TN;
   const float scale = e.zstride ? 1.f : e.gmax ? e.scale * *e.gmax : e.scale;
+  RowsOut<TN, MF> rows(smem, wave, lane);
   static_for<0, FM>([&](auto ic) __attribute__((always_inline)) {
     constexpr int i = decltype(ic)::value;
     const int64_t m = m0 + wm * TM + i * MF + (lane & (MF - 1));
@@ -171,18 +233,15 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r0 = 0; r0 < NR; r0 += 4) {
-        const int n = n0 + wn * TN + j * MF + Mma<MF>::row(lane, r0);
-        // N is a multiple of 8: four columns are all there or none
-        if (m >= g.M || n >= g.N) continue;
+        const int n = nb + j * MF + Mma<MF>::row(lane, r0);
         float4 v = make_float4(acc[i][j][r0], acc[i][j][r0 + 1], acc[i][j][r0 + 2], acc[i][j][r0 + 3]);
         v.x *= scale;
         v.y *= scale;
         v.z *= scale;
         v.w *= scale;
         if (e.dtype == BF16) {
-          *reinterpret_cast<uint2*>(static_cast<bf16_t*>(e.out) + m * e.ldo + n) =
-              make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-        } else {
+          rows.put(n - nb, make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)));
+        } else if (m < g.M && n < g.N) {  // N is a multiple of 8: four columns are all there or none
           float4* o = reinterpret_cast<float4*>(static_cast<float*>(e.out) + blockIdx.z * e.zstride + m * e.ldo + n);
           if (e.accumulate) {
             const float4 f = *o;
@@ -194,6 +253,11 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
           *o = v;
         }
       }
+    if (e.dtype == BF16)
+      rows.flush([&](int r, int c, uint4 v) __attribute__((always_inline)) {
+        const int64_t mr = m0 + wm * TM + i * MF + r;
+        if (mr < g.M && nb + c < g.N) *reinterpret_cast<uint4*>(static_cast<bf16_t*>(e.out) + mr * e.ldo + nb + c) = v;
+      });
   });
 }
 
@@ -210,6 +274,7 @@ static hipError_t run_head_tiles(const GemmDesc& g, const E& e, int nz, hipStrea
   auto kern = head_gemm_kernel<BM, BN, WM, WN, BK, NST, AK, BKM, MF, E>;
   constexpr size_t lds = (size_t)NST * (BM + BN) * BK * sizeof(bf16_t);
   static_assert(lds <= 160 * 1024, "pipeline exceeds LDS");
+  static_assert(WM * WN * RowsOut<BN / WN, MF>::BYTES <= lds, "rows of the epilogue exceed LDS");
   if (lds > 64 * 1024) {
     const hipError_t err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (err != hipSuccess) return err;
@@ -263,7 +328,9 @@ struct F32Stage {
 };
 template <bool AK, bool BKM, typename E>
 __global__ void __launch_bounds__(256) head_f32_kernel(GemmDesc g, E e) {
-  __shared__ __align__(16) float As[2][SK][SLD], Bs[2][SK][SLD];
+  __shared__ __align__(16) float lds[4][SK][SLD];
+  float (*As)[SK][SLD] = lds, (*Bs)[SK][SLD] = lds + 2;
+  static_assert(4 * RowsOut<ST / 2, 32>::BYTES <= sizeof(lds), "rows of the epilogue exceed LDS");
   const int nbm = (g.M + ST - 1) / ST, nbn = (g.N + ST - 1) / ST;
   int tm, tn;
   tile_coords(blockIdx.x, nbm, nbn, tm, tn);
@@ -309,7 +376,8 @@ __global__ void __launch_bounds__(256) head_f32_kernel(GemmDesc g, E e) {
     sa.store(As[cur]);
     sb.store(Bs[cur]);
   }
-  store_tile<ST, ST, 2, 2, 32>(acc, nullptr, g, e, m0, n0, wave, lane);
+  __syncthreads();
+  store_tile<ST, ST, 2, 2, 32>(acc, reinterpret_cast<unsigned char*>(lds), g, e, m0, n0, wave, lane);
 }
 template <bool AK, bool BKM, typename E>
 static hipError_t run_head_f32(const GemmDesc& g, const E& e, hipStream_t s, int nz = 1) {
@@ -532,7 +600,7 @@ __global__ void __launch_bounds__(1024) head_gmax_kernel(int64_t T, const float*
 }
 
 // Per row what dL/dz takes (GradEpi), and the named columns' values; a wave per row.
-__global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, zl_targets t, float a, float b, bool two,
+__global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, zl_targets t, float a, float b, int mode,
                                                         const float* stats, const float* dloss, const float* gmax,
                                                         int32_t* tid, float* tval, float4* coef, int32_t* live) {
   const int lane = threadIdx.x & 63;
@@ -577,11 +645,19 @@ __global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, zl_targets t,
       val[t.k] = g;
     }
     float4 c = make_float4(c1, l1, ct, lt);
-    if (!two) {
-      // one exponential: labels or a teacher alone, or both at tau = 1 without a rest
+    if (mode == GRAD_ONE) {
+      // labels or a teacher alone, or both at tau = 1 without a rest
+      c.x = 0.f;
       c.z = ct + c1;
       if (!on) c.w = l1;
+    } else if (mode == GRAD_SQUARE) {
+      if (!on || lt == -INFINITY) c.w = lt = 0.5f * l1;  // any shift does for the square alone
+      c.x = c1 == 0.f ? 0.f : c1 * expf(2.f * lt - l1);
     }
+    // a term that is not there vanishes also where its exponential would overflow
+    if (c.z == 0.f && c.x == 0.f) c.w = INFINITY;
+    if (mode == GRAD_TWO && c.z == 0.f) c.w = INFINITY;
+    if (c.x == 0.f) c.y = INFINITY;
     coef[row] = c;
     live[row] = on || y >= 0;
   }
@@ -756,11 +832,14 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
     hipLaunchKernelGGL((head_named_kernel<false>), dim3(grid(named, 4)), dim3(256), 0, s, named, a.d, t.k, a.x, a.ldx, a.w,
                        a.ldw, tid, a.stats);
   // a masked sum is always the second of a pair
-  const int two = pair || masked;
-  const StatEpi e = {two, soft ? LOG2E / t.temperature : LOG2E, part, T, mask, p.ldm};
+  const bool two = pair || masked;
   const GemmDesc g = head_gemm(T, a.V, a.d, a.x, a.ldx, true, a.w, a.ldw, true);
-  if (bf) ZL_TRY((run_head<true, true>(g, e, p.large, s)));
-  else ZL_TRY((run_head_f32<true, true>(g, e, s)));
+  auto sums = [&](auto pc) -> hipError_t {
+    const StatEpi<decltype(pc)::value> e = {soft ? LOG2E / t.temperature : LOG2E, part, T, mask, p.ldm};
+    return bf ? run_head<true, true>(g, e, p.large, s) : run_head_f32<true, true>(g, e, s);
+  };
+  if (two) ZL_TRY(sums(std::true_type{}));
+  else ZL_TRY(sums(std::false_type{}));
   auto rows = [&](auto rc, auto pc) {
     constexpr int R = decltype(rc)::value;
     constexpr bool P = decltype(pc)::value;
@@ -800,7 +879,8 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
   }
   const zl_targets& t = a.targets;
   const bool hard = t.labels != nullptr, soft = t.ids != nullptr, rest = soft && t.rest;
-  const int two = hard && soft && (rest || t.temperature != 1.f);
+  const bool two = hard && soft && (rest || t.temperature != 1.f);
+  const int mode = !two ? GRAD_ONE : t.temperature == 2.f ? GRAD_SQUARE : GRAD_TWO;
   const HeadPlan p = head_plan(T, a.V, d, dt, t.k, rest, true, a.dx != nullptr, a.dw != nullptr, a.columns);
   char* ws = static_cast<char*>(a.workspace);
   int32_t* tid = reinterpret_cast<int32_t*>(ws + p.tid);
@@ -816,7 +896,7 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
   loss_weights(t, wa, wb);
   hipLaunchKernelGGL(head_targets_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, a.V, t, tid, (uint32_t*)nullptr, (int64_t)0);
   hipLaunchKernelGGL(head_gmax_kernel, dim3(1), dim3(1024), 0, s, T, a.dloss, gmax);
-  hipLaunchKernelGGL(head_coef_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, t, wa, wb, two != 0, a.stats, a.dloss, gmax,
+  hipLaunchKernelGGL(head_coef_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, t, wa, wb, mode, a.stats, a.dloss, gmax,
                      tid, tval, coef, live);
   if (a.dw)
     hipLaunchKernelGGL(head_clean_kernel, dim3(grid(T * (d / 8), 256)), dim3(256), 0, s, T, d, live, a.x, a.ldx, xc, dt);
@@ -827,11 +907,15 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
     const int n8 = (n + 7) / 8 * 8;
     const char* w = static_cast<const char*>(a.w) + (size_t)v0 * a.ldw * es;
     {
-      const GradEpi e = {coef, two, soft ? 1.f / t.temperature : 1.f, dz, p.ldz, dt};
       const GemmDesc g = head_gemm(T, n, d, a.x, a.ldx, true, w, a.ldw, true);
       GemmShape sh = {(int)T, n, d, true, true, false, 0, false, 0};
-      if (bf) ZL_TRY((run_head<true, true>(g, e, plan_gemm(sh).large, s)));
-      else ZL_TRY((run_head_f32<true, true>(g, e, s)));
+      auto grads = [&](auto mc) -> hipError_t {
+        const GradEpi<decltype(mc)::value> e = {coef, soft ? 1.f / t.temperature : 1.f, dz, p.ldz, dt};
+        return bf ? run_head<true, true>(g, e, plan_gemm(sh).large, s) : run_head_f32<true, true>(g, e, s);
+      };
+      if (mode == GRAD_ONE) ZL_TRY(grads(std::integral_constant<int, GRAD_ONE>{}));
+      else if (mode == GRAD_TWO) ZL_TRY(grads(std::integral_constant<int, GRAD_TWO>{}));
+      else ZL_TRY(grads(std::integral_constant<int, GRAD_SQUARE>{}));
     }
     const int64_t named = T * (t.k + 1);
     hipLaunchKernelGGL(head_put_kernel, dim3(grid(named, 256)), dim3(256), 0, s, named, t.k, v0, n, tid, tval, dz, p.ldz, dt);

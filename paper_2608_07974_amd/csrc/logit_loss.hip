@@ -6,83 +6,85 @@
 
 namespace zl {
 
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+template <bool STREAM>
+__device__ __forceinline__ u32x4_t load16(const void* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const u32x4_t*>(p));
+  else return *static_cast<const u32x4_t*>(p);
+}
+template <bool STREAM>
+__device__ __forceinline__ void store16(void* p, u32x4_t v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<u32x4_t*>(p));
+  else *static_cast<u32x4_t*>(p) = v;
+}
+
 // ------------------------------------------------------------ rows of logits
-// Columns in groups of 8, whose memory is 16-byte aligned from the first full group
-// on, wherever the row starts: group g holds columns 8 g - pad .. 8 g - pad + 7 as
-// far as they lie in [0, V); only the first and the last may be cut.
+// Columns in groups of W = 8 (fp32: 4), 16 bytes aligned from the first full group on,
+// wherever the row starts: group g holds columns W g - pad .. W g - pad + W - 1 as far as
+// they lie in [0, V); only the first and the last may be cut.
 template <bool BF>
 struct Row {
   using E = typename std::conditional<BF, bf16_t, float>::type;
+  static constexpr int W = 16 / sizeof(E);
   const E* p;
   int V, pad, full0, full1;  // full groups [full0, full1)
   __device__ __forceinline__ Row(const void* base, int64_t off, int V_) : p(static_cast<const E*>(base) + off), V(V_) {
     const int skip = (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(E);
-    pad = (8 - skip) & 7;
+    pad = (W - skip) & (W - 1);
     full0 = pad ? 1 : 0;
-    full1 = (V + pad) >> 3;
+    full1 = (V + pad) / W;
   }
-  __device__ __forceinline__ int groups() const { return (V + pad + 7) >> 3; }
+  __device__ __forceinline__ int groups() const { return (V + pad + W - 1) / W; }
   // the cut groups: c = 0, 1; -1 where there is none
   __device__ __forceinline__ int cut(int c) const {
     if (c == 0) return pad ? 0 : -1;
-    return ((V + pad) & 7) && full1 >= full0 ? full1 : -1;
+    return ((V + pad) & (W - 1)) && full1 >= full0 ? full1 : -1;
   }
-  __device__ __forceinline__ int group_of(int v) const { return (v + pad) >> 3; }
+  __device__ __forceinline__ int group_of(int v) const { return (v + pad) / W; }
   __device__ __forceinline__ float at(int v) const { return Elem<E>::load(p, v); }
-  struct Raw { uint4 u[BF ? 1 : 2]; };
-  __device__ __forceinline__ Raw load(int g) const {
-    Raw r;
-    const uint4* q = reinterpret_cast<const uint4*>(p + (8 * (int64_t)g - pad));
-    r.u[0] = q[0];
-    if constexpr (!BF) r.u[1] = q[1];
-    return r;
+  template <bool STREAM = false>
+  __device__ __forceinline__ u32x4_t load(int g) const {
+    return load16<STREAM>(p + (W * (int64_t)g - pad));
   }
-  __device__ static __forceinline__ void get(const Raw& r, float (&v)[8]) {
-    if constexpr (BF) {
-      const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
+  __device__ static __forceinline__ void get(u32x4_t r, float (&v)[W]) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[2 * k] = __builtin_bit_cast(float, w[k] << 16);
-        v[2 * k + 1] = __builtin_bit_cast(float, w[k] & 0xffff0000u);
-      }
-    } else {
-      const uint32_t w[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[1].x, r.u[1].y, r.u[1].z, r.u[1].w};
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = __builtin_bit_cast(float, w[k]);
+    for (int k = 0; k < W; ++k) {
+      if constexpr (BF) v[k] = __builtin_bit_cast(float, k & 1 ? r[k / 2] & 0xffff0000u : r[k / 2] << 16);
+      else v[k] = __builtin_bit_cast(float, (uint32_t)r[k]);
     }
   }
   // a cut group, -inf outside the row
-  __device__ __forceinline__ void get_cut(int g, float (&v)[8]) const {
+  __device__ __forceinline__ void get_cut(int g, float (&v)[W]) const {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int c = 8 * g - pad + k;
+    for (int k = 0; k < W; ++k) {
+      const int c = W * g - pad + k;
       v[k] = c >= 0 && c < V ? at(c) : -INFINITY;
     }
   }
   // f(group, values) for this thread's groups, U loads in flight
-  template <int NT, int U, typename F>
+  template <int NT, int U, bool STREAM = false, typename F>
   __device__ __forceinline__ void each(F&& f) const {
     int g = full0 + (int)threadIdx.x;
     for (; g + (U - 1) * NT < full1; g += U * NT) {
-      Raw r[U];
+      u32x4_t r[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) r[u] = load(g + u * NT);
+      for (int u = 0; u < U; ++u) r[u] = load<STREAM>(g + u * NT);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        float v[8];
+        float v[W];
         get(r[u], v);
         f(g + u * NT, v);
       }
     }
     for (; g < full1; g += NT) {
-      float v[8];
-      get(load(g), v);
+      float v[W];
+      get(load<STREAM>(g), v);
       f(g, v);
     }
     if (threadIdx.x < 2) {
       const int c = cut((int)threadIdx.x);
       if (c >= 0) {
-        float v[8];
+        float v[W];
         get_cut(c, v);
         f(c, v);
       }
@@ -92,31 +94,37 @@ struct Row {
 
 // --------------------------------------------------- a row's named columns
 // The label and the teacher's ids, found again while the row streams by: a bit for
-// every group of 8 columns (exact up to 262144 columns; beyond, groups share
-// bits), and behind it chains of entries.  A test costs one broadcast LDS read per
-// 8 columns; comparing every column with k ids would cost k.
-constexpr int NAME_BITS = 32768, NAME_HEADS = 512, MAX_ENTRIES = ZL_TARGETS_MAX_K + 1;
+// every group of columns (beyond BITS groups, several share one), and behind it chains
+// of entries.  A test costs one broadcast LDS read per group; comparing every column
+// with k ids would cost k.
+template <int BITS, int HEADS, int K>
 struct Names {
-  uint32_t bits[NAME_BITS / 32];
-  int head[NAME_HEADS];
-  int id[MAX_ENTRIES];    // column, -1: absent
-  int next[MAX_ENTRIES];
-  float val[MAX_ENTRIES];
+  static constexpr int MAX_K = K;
+  uint32_t bits[BITS / 32];
+  int head[HEADS];
+  int id[K + 1];    // column, -1: absent
+  int next[K + 1];
+  float val[K + 1];
 
   template <int NT>
   __device__ __forceinline__ void clear() {
-    for (int i = threadIdx.x; i < NAME_BITS / 32; i += NT) bits[i] = 0;
-    for (int i = threadIdx.x; i < NAME_HEADS; i += NT) head[i] = -1;
+    for (int i = threadIdx.x; i < BITS / 32; i += NT) bits[i] = 0;
+    for (int i = threadIdx.x; i < HEADS; i += NT) head[i] = -1;
   }
   __device__ __forceinline__ void add(int e, int column, int group) {
     id[e] = column;
-    atomicOr(&bits[(group >> 5) & (NAME_BITS / 32 - 1)], 1u << (group & 31));
-    next[e] = atomicExch(&head[group & (NAME_HEADS - 1)], e);
+    atomicOr(&bits[(group >> 5) & (BITS / 32 - 1)], 1u << (group & 31));
+    next[e] = atomicExch(&head[group & (HEADS - 1)], e);
   }
+  __device__ __forceinline__ int first(int group) const { return head[group & (HEADS - 1)]; }
   __device__ __forceinline__ bool maybe(int group) const {
-    return bits[(group >> 5) & (NAME_BITS / 32 - 1)] >> (group & 31) & 1;
+    return bits[(group >> 5) & (BITS / 32 - 1)] >> (group & 31) & 1;
   }
 };
+
+// Those of a block of NT threads.  A wave of its own takes short rows of few ids.
+template <int NT> struct NamesOf { using type = Names<32768, 512, ZL_TARGETS_MAX_K>; };
+template <> struct NamesOf<64> { using type = Names<1024, 64, 64>; };
 
 // What every thread of a block knows of its row's targets.
 struct RowTargets {
@@ -132,10 +140,10 @@ struct RowTargets {
 };
 
 // Reads the targets of row t, enters the ids (and, with `both`, the label as entry k)
-// into `names`.  NT >= ZL_TARGETS_MAX_K.  Ends with a barrier.
+// into `names`.  k <= NT.  Ends with a barrier.
 template <int NT, bool BF>
-__device__ __forceinline__ RowTargets row_targets(const LogitLossArgs& a, int64_t row, const Row<BF>& z, Names& names,
-                                                  bool both, float* red) {
+__device__ __forceinline__ RowTargets row_targets(const LogitLossArgs& a, int64_t row, const Row<BF>& z,
+                                                  typename NamesOf<NT>::type& names, bool both, float* red) {
   RowTargets q;
   const int tid = threadIdx.x, k = a.t.k, V = a.V;
   q.y = a.t.labels ? a.t.labels[row] : -1;
@@ -162,11 +170,11 @@ __device__ __forceinline__ RowTargets row_targets(const LogitLossArgs& a, int64_
   // the first entry of a column counts
   bool twice = false;
   if (q.here)
-    for (int e = names.head[z.group_of(q.id) & (NAME_HEADS - 1)]; e >= 0; e = names.next[e])
+    for (int e = names.first(z.group_of(q.id)); e >= 0; e = names.next[e])
       twice |= e < tid && names.id[e] == q.id;
   bool named = false;
   if (both && tid == 0 && q.label)
-    for (int e = names.head[z.group_of(q.y) & (NAME_HEADS - 1)]; e >= 0; e = names.next[e])
+    for (int e = names.first(z.group_of(q.y)); e >= 0; e = names.next[e])
       named |= e < k && names.id[e] == q.y;
   __syncthreads();
   if (twice) {
@@ -198,12 +206,24 @@ __device__ __forceinline__ RowTargets row_targets(const LogitLossArgs& a, int64_
   return q;
 }
 
+// How many exponentials an element takes: one (labels or a teacher alone, or both at
+// tau = 1 without a rest); two; or one for two at tau = 2, where exp(z) is the square
+// of exp(z / 2).
+enum { EXP_ONE, EXP_TWO, EXP_SQUARE };
+
 // ---------------------------------------------------------------- forward
-// TWO: log-sums of z and of z / tau; REST: the latter without the teacher's ids.
-template <bool BF, int NT, bool TWO, bool REST>
+// Log-sums of z (unless EXP_ONE) and of z / tau; REST: the latter without the teacher's
+// ids.  The sums are taken relative to the largest of the row's first columns: no
+// running maximum (8 instead of 10 cycles of the vector units per element, which come
+// near the memory's time).  Where that reference is so far off that a sum overflows, or
+// that of the columns beside the teacher's nearly vanishes, the row goes by once more
+// with running maxima.
+template <bool BF, int NT, int MODE, bool REST, bool STREAM>
 __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
-  __shared__ Names names;
+  __shared__ typename NamesOf<NT>::type names;
   __shared__ float red[NT / 64];
+  constexpr bool TWO = MODE != EXP_ONE;
+  constexpr int W = Row<BF>::W;
   const int64_t row = blockIdx.x;
   const Row<BF> z(a.z, row * a.ldz, a.V);
   const RowTargets q = row_targets<NT, BF>(a, row, z, names, false, red);
@@ -216,48 +236,74 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
   }
   const float inv = a.t.ids ? 1.f / a.t.temperature : 1.f;
   const float c2 = inv * LOG2E;  // of the teacher's log-sum
-  LogSum s1, st;                 // of z, of z / tau (not TWO: st alone, at 1 / tau)
-  z.template each<NT, 4>([&](int g, float (&v)[8]) __attribute__((always_inline)) {
-    if constexpr (TWO) {
-      s1.raise(max_of(v), LOG2E);
-      const float ref = s1.ref();
-      if constexpr (REST) {
+  // the named columns of group g out of v
+  auto without = [&](int g, float (&v)[W]) __attribute__((always_inline)) {
+    for (int e = names.first(g); e >= 0; e = names.next[e]) {
+      const int c = names.id[e];
+      if (c >= 0 && z.group_of(c) == g) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s1.s += __builtin_amdgcn_exp2f((v[k] - ref) * LOG2E);
-      } else {
-        // one maximum serves both
-        if (s1.m > st.m) {
-          st.s *= __builtin_amdgcn_exp2f((st.m - s1.m) * c2);
-          st.m = s1.m;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float x = v[k] - ref;
-          s1.s += __builtin_amdgcn_exp2f(x * LOG2E);
-          st.s += __builtin_amdgcn_exp2f(x * c2);
-        }
+        for (int k = 0; k < W; ++k) v[k] = W * g - z.pad + k == c ? -INFINITY : v[k];
       }
+    }
+  };
+  LogSum s1, st;  // of z, of z / tau (EXP_ONE: st alone, at 1 / tau)
+  float first = -INFINITY;
+  if ((int)threadIdx.x < z.groups()) {
+    const int g = threadIdx.x;
+    float v[W];
+    if (g >= z.full0 && g < z.full1) z.get(z.load(g), v);
+    else z.get_cut(g, v);
+    first = max_of(v);
+  }
+  float ref = block_max<NT>(first, red);
+  if (!(fabsf(ref) < INFINITY)) ref = 0.f;
+  s1.m = st.m = ref;
+  z.template each<NT, 4, STREAM>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
+    if constexpr (MODE == EXP_TWO) {
+#pragma unroll
+      for (int k = 0; k < W; ++k) s1.s += __builtin_amdgcn_exp2f((v[k] - ref) * LOG2E);
     }
     if constexpr (REST) {
       if (q.teacher && names.maybe(g)) {
-        for (int e = names.head[g & (NAME_HEADS - 1)]; e >= 0; e = names.next[e]) {
-          const int c = names.id[e];
-          if (c >= 0 && z.group_of(c) == g) {
+        if constexpr (MODE == EXP_SQUARE) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = 8 * g - z.pad + k == c ? -INFINITY : v[k];
-          }
+          for (int k = 0; k < W; ++k) s1.s += __builtin_amdgcn_exp2f((v[k] - ref) * LOG2E);
         }
+        without(g, v);
+#pragma unroll
+        for (int k = 0; k < W; ++k) st.s += __builtin_amdgcn_exp2f((v[k] - ref) * c2);
+        return;
       }
     }
-    if constexpr (!TWO || REST) {
-      st.raise(max_of(v), c2);
-      const float ref = st.ref();
 #pragma unroll
-      for (int k = 0; k < 8; ++k) st.s += __builtin_amdgcn_exp2f((v[k] - ref) * c2);
+    for (int k = 0; k < W; ++k) {
+      const float p = __builtin_amdgcn_exp2f((v[k] - ref) * c2);
+      st.s += p;
+      if constexpr (MODE == EXP_SQUARE) s1.s = __builtin_fmaf(p, p, s1.s);
     }
   });
-  st = block_logsum<NT>(st, c2, red);
-  if constexpr (TWO) s1 = block_logsum<NT>(s1, LOG2E, red);
+  st.s = block_sum<NT>(st.s, red);
+  if constexpr (TWO) s1.s = block_sum<NT>(s1.s, red);
+  if (!(st.s < INFINITY && st.s > 1e-18f && (!TWO || s1.s < INFINITY))) {
+    s1 = st = LogSum();
+    z.template each<NT, 1>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
+      if constexpr (TWO) {
+        s1.raise(max_of(v), LOG2E);
+        const float r = s1.ref();
+#pragma unroll
+        for (int k = 0; k < W; ++k) s1.s += __builtin_amdgcn_exp2f((v[k] - r) * LOG2E);
+      }
+      if constexpr (REST) {
+        if (q.teacher && names.maybe(g)) without(g, v);
+      }
+      st.raise(max_of(v), c2);
+      const float r = st.ref();
+#pragma unroll
+      for (int k = 0; k < W; ++k) st.s += __builtin_amdgcn_exp2f((v[k] - r) * c2);
+    });
+    st = block_logsum<NT>(st, c2, red);
+    if constexpr (TWO) s1 = block_logsum<NT>(s1, LOG2E, red);
+  }
   float other = 0.f, lt = 0.f;
   if constexpr (REST) {
     // the named columns' share again, for the log-sum over all
@@ -272,7 +318,7 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
     st.merge(n.m, n.s, c2);
   }
   lt = st.log(inv);
-  const float l1 = TWO ? s1.log(1.f) : lt;  // (not TWO: tau = 1 where there are labels)
+  const float l1 = TWO ? s1.log(1.f) : lt;  // (EXP_ONE: tau = 1 where there are labels)
   float kl = 0.f;
   if (a.t.ids) {
     kl = block_sum<NT>(q.p > 0.f || q.p != q.p ? q.p * (q.t - q.zi * inv) : 0.f, red) + lt - q.L;
@@ -289,56 +335,56 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
 }
 
 // --------------------------------------------------------------- backward
-// The named columns' values are formed first and put in as those come by, so that
-// each element is written once.
-template <bool BF>
-__device__ __forceinline__ void store8(typename Row<BF>::E* p, const float (&v)[8]) {
-  if constexpr (BF) {
-    uint4 u = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    *reinterpret_cast<uint4*>(p) = u;
-  } else {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-  }
+// Off the named columns c1 exp(z - l1) + ct exp(z / tau - lt): the softmax itself, or with
+// a rest what is left of it once the teacher's share of the rest is taken off.  The
+// named columns' values are formed first and put in as those come by, so that each
+// element is written once.  Differences are taken before the scaling by log2(e), which
+// would overflow in a row of the type's lowest values.
+template <bool STREAM>
+__device__ __forceinline__ void store_group(bf16_t* p, const float (&v)[8]) {
+  store16<STREAM>(p, u32x4_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_group(float* p, const float (&v)[4]) {
+  store16<STREAM>(p, __builtin_bit_cast(u32x4_t, v));
 }
 
-template <bool BF, int NT, bool TWO>
+template <bool BF, int NT, int MODE, bool STREAM>
 __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
   using E = typename Row<BF>::E;
-  __shared__ Names names;
+  constexpr int W = Row<BF>::W;
+  __shared__ typename NamesOf<NT>::type names;
   __shared__ float red[NT / 64];
   const int64_t row = blockIdx.x;
   const Row<BF> z(a.z, row * a.ldz, a.V);
   E* out = static_cast<E*>(a.dz) + row * a.lddz;
   const bool vec = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(z.p)) & 15) == 0;
-  auto put = [&](int g, const float (&v)[8]) __attribute__((always_inline)) {
-    const int c0 = 8 * g - z.pad;
-    if (vec && c0 >= 0 && c0 + 8 <= z.V) {
-      store8<BF>(out + c0, v);
+  auto put = [&](int g, const float (&v)[W]) __attribute__((always_inline)) {
+    const int c0 = W * g - z.pad;
+    if (vec && c0 >= 0 && c0 + W <= z.V) {
+      store_group<STREAM>(out + c0, v);
     } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
+      for (int k = 0; k < W; ++k)
         if (c0 + k >= 0 && c0 + k < z.V) Elem<E>::store(out, c0 + k, v[k]);
     }
   };
   const RowTargets q = row_targets<NT, BF>(a, row, z, names, true, red);
   if (!q.label && !q.teacher) {
-    const float none[8] = {};
+    const float none[W] = {};
     for (int g = threadIdx.x; g < z.groups(); g += NT) put(g, none);
     return;
   }
   const float4 s = *reinterpret_cast<const float4*>(a.stats + 4 * row);
   const float up = a.scale * (a.dloss ? a.dloss[row] : 1.f);
   const float tau = a.t.ids ? a.t.temperature : 1.f, inv = 1.f / tau;
-  const float c1 = q.label ? a.a * up : 0.f, f = q.teacher ? a.b * tau * up : 0.f;
-  // off the named columns c1 exp(z - l1) + ct exp(z / tau - lt): the softmax itself, or
-  // with a rest what is left of it once the teacher's share of the rest is taken off
+  float c1 = q.label ? a.a * up : 0.f, l1 = s.x;
+  const float f = q.teacher ? a.b * tau * up : 0.f;
   float ct = f, lt = s.y;
   if (q.teacher && a.t.rest) {
     lt = s.z;
     ct = lt == -INFINITY ? 0.f : f * (expf(s.z - s.y) - q.r);
   }
-  // the named columns
   if (q.here) {
     float g = f * (expf(q.zi * inv - s.y) - q.p);
     if (q.label) g += c1 * (q.id == q.y ? expm1f(q.zi - s.x) : expf(q.zi - s.x));
@@ -350,29 +396,37 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
     names.val[a.t.k] = g;
   }
   __syncthreads();
-  if constexpr (!TWO) {
-    // one exponential: labels or a teacher alone, or both at tau = 1 without a rest
+  if constexpr (MODE == EXP_ONE) {
     if (!q.teacher) lt = s.x;
     ct += c1;
+  } else if constexpr (MODE == EXP_SQUARE) {
+    if (!q.teacher || lt == -INFINITY) lt = 0.5f * s.x;  // any shift does for the square alone
+    c1 = c1 == 0.f ? 0.f : c1 * expf(2.f * lt - s.x);
   }
-  z.template each<NT, 4>([&](int g, float (&v)[8]) __attribute__((always_inline)) {
-    float o[8];
+  // a term that is not there vanishes also where its exponential would overflow
+  if (ct == 0.f && (MODE != EXP_SQUARE || c1 == 0.f)) lt = INFINITY;
+  if (c1 == 0.f) l1 = INFINITY;
+  z.template each<NT, 4, STREAM>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
+    float o[W];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < W; ++k) {
       const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], inv, -lt) * LOG2E);
-      o[k] = ct != 0.f ? ct * p : 0.f;
-      if constexpr (TWO) {
-        const float p1 = __builtin_amdgcn_exp2f((v[k] - s.x) * LOG2E);
-        o[k] += c1 != 0.f ? c1 * p1 : 0.f;
+      if constexpr (MODE == EXP_ONE) {
+        o[k] = ct * p;
+      } else if constexpr (MODE == EXP_SQUARE) {
+        o[k] = p * __builtin_fmaf(p, c1, ct);
+      } else {
+        const float p1 = __builtin_amdgcn_exp2f((v[k] - l1) * LOG2E);
+        o[k] = __builtin_fmaf(c1, p1, ct * p);
       }
     }
     if (names.maybe(g)) {
-      for (int e = names.head[g & (NAME_HEADS - 1)]; e >= 0; e = names.next[e]) {
+      for (int e = names.first(g); e >= 0; e = names.next[e]) {
         const int c = names.id[e];
         if (c >= 0 && z.group_of(c) == g) {
           const float w = names.val[e];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) o[k] = 8 * g - z.pad + k == c ? w : o[k];
+          for (int k = 0; k < W; ++k) o[k] = W * g - z.pad + k == c ? w : o[k];
         }
       }
     }
@@ -382,13 +436,13 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
 
 // --------------------------------------------------------------- top logits
 // 1. The row streams by once; the largest values of 1024 strands of it (a strand:
-//    four of every 8 columns of one thread) go to LDS.  The (k + 1)-th largest of
+//    half of every group of one thread) go to LDS.  The (k + 1)-th largest of
 //    them, cut to 16 bits, is a bound: at least k + 1 columns reach it, and with
 //    columns in no special order few more do.
 // 2. The row streams by again (mostly out of the caches): columns that reach the
 //    bound are listed, the others go into the rest's sum.
 // 3. The list is ordered by rank: keys are distinct (value, then lower column first).
-// Where the list overflows (many equal values) a radix search by 8 bits finds the
+// Where the list overflows (many equal values), or there is a NaN, a radix search by 8 bits finds the
 // (k + 1)-th largest exactly and a last pass lists what is above it and, in order of
 // the columns, what equals it.
 constexpr int TT = 512, TOP_CAP = 1024;
@@ -406,6 +460,7 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 template <bool BF>
 __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, int64_t ldx, int k, float inv,
                                                         int32_t* ids, float* values, float* rest) {
+  constexpr int W = Row<BF>::W;
   __shared__ uint32_t strands[2 * TT];
   __shared__ unsigned long long list[TOP_CAP];
   __shared__ float red[TT / 64];
@@ -418,9 +473,12 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
   const float c2 = inv * LOG2E;
 
   float m0 = -INFINITY, m1 = -INFINITY;
-  z.template each<TT, 4>([&](int, float (&v)[8]) __attribute__((always_inline)) {
-    m0 = fmaxf(m0, fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
-    m1 = fmaxf(m1, fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+  z.template each<TT, 4>([&](int, float (&v)[W]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < W / 2; ++e) {
+      m0 = fmaxf(m0, v[e]);
+      m1 = fmaxf(m1, v[W / 2 + e]);
+    }
   });
   strands[tid] = order_of(m0);
   strands[TT + tid] = order_of(m1);
@@ -445,26 +503,35 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
   uint32_t bound = bound_s;
   float sum = 0.f;  // of exp((x - ref) c) below the bound
   float ref = value_of(bound);
-  if (!(ref > -INFINITY && ref < INFINITY)) ref = 0.f;
-  z.template each<TT, 4>([&](int g, float (&v)[8]) __attribute__((always_inline)) {
+  const bool all = !(ref > -INFINITY && ref < INFINITY);  // no bound among numbers
+  if (all) ref = 0.f;
+  z.template each<TT, 4>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
+    // a group below the bound, most of them, costs its maximum and its exponentials
+    // (NaN passes here and shows in the sum)
+    if (all || max_of(v) >= ref) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = 8 * g - z.pad + e;
-      const uint32_t o = order_of(v[e]);
-      if (o >= bound) {
-        if (c >= 0 && c < V) {
-          const uint32_t at = atomicAdd(&count_s, 1u);
-          if (at < TOP_CAP) list[at] = (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)c);
+      for (int e = 0; e < W; ++e) {
+        const int c = W * g - z.pad + e;
+        const uint32_t o = order_of(v[e]);
+        if (o >= bound) {
+          if (c >= 0 && c < V) {
+            const uint32_t at = atomicAdd(&count_s, 1u);
+            if (at < TOP_CAP) list[at] = (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)c);
+          }
+        } else {
+          sum += __builtin_amdgcn_exp2f((v[e] - ref) * c2);
         }
-      } else {
-        sum += __builtin_amdgcn_exp2f((v[e] - ref) * c2);
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e) sum += __builtin_amdgcn_exp2f((v[e] - ref) * c2);
     }
   });
+  const bool nan = block_max<TT>(sum == sum ? 0.f : 1.f, red) > 0.f;
   __syncthreads();
   uint32_t n = count_s;
   float ties = 0.f;  // columns equal to the bound that are not listed
-  if (n > TOP_CAP) {
+  if (n > TOP_CAP || nan) {
     // the want-th largest, 8 bits at a time: `above` columns are larger
     uint32_t key = 0, above = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
@@ -472,10 +539,10 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
       if (tid < 256) hist[tid] = 0;
       __syncthreads();
       const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-      z.template each<TT, 1>([&](int g, float (&v)[8]) __attribute__((always_inline)) {
+      z.template each<TT, 1>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = 8 * g - z.pad + e;
+        for (int e = 0; e < W; ++e) {
+          const int c = W * g - z.pad + e;
           const uint32_t o = order_of(v[e]);
           if (c >= 0 && c < V && (o & mask) == key) atomicAdd(&hist[o >> shift & 255], 1u);
         }
@@ -504,14 +571,14 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
     const int groups = z.groups();
     for (int g0 = 0; g0 < groups; g0 += TT) {
       const int g = g0 + tid;
-      float v[8];
+      float v[W];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = 0.f;
+      for (int e = 0; e < W; ++e) v[e] = 0.f;
       if (g < groups) z.get_cut(g, v);
       uint32_t eq = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = 8 * g - z.pad + e;
+      for (int e = 0; e < W; ++e) {
+        const int c = W * g - z.pad + e;
         if (g >= groups || c < 0 || c >= V) continue;
         const uint32_t o = order_of(v[e]);
         if (o > bound) {
@@ -539,10 +606,10 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
         all += (uint32_t)scan[w];
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < W; ++e)
         if (eq >> e & 1) {
           if (rank < need)
-            list[above + rank] = (unsigned long long)bound << 32 | (0xffffffffu - (uint32_t)(8 * g - z.pad + e));
+            list[above + rank] = (unsigned long long)bound << 32 | (0xffffffffu - (uint32_t)(W * g - z.pad + e));
           ++rank;
         }
       seen += all;
@@ -594,33 +661,68 @@ hipError_t launch_top_logits(int64_t T, int V, const void* x, int64_t ldx, int d
   return hipGetLastError();
 }
 
-template <bool BF, int NT>
-static void logit_forward(const LogitLossArgs& a, bool two, bool rest, hipStream_t s) {
-  const dim3 g((unsigned)a.T), b(NT);
-  if (two && rest) hipLaunchKernelGGL((logit_loss_kernel<BF, NT, true, true>), g, b, 0, s, a);
-  else if (two) hipLaunchKernelGGL((logit_loss_kernel<BF, NT, true, false>), g, b, 0, s, a);
-  else if (rest) hipLaunchKernelGGL((logit_loss_kernel<BF, NT, false, true>), g, b, 0, s, a);
-  else hipLaunchKernelGGL((logit_loss_kernel<BF, NT, false, false>), g, b, 0, s, a);
+// Which blocks take the rows (times in us; forward / backward, labels alone):
+//  - short rows a wave each: bf16 16384 x 1000 11.8 / 19.9, four waves 24.5 / 29.7.  Up to
+//    128 groups; the forward up to 512 where there are rows enough (bf16 16384 x 4096
+//    28.3 against 39.4; the backward 53.9 against 51.1);
+//  - long rows 16 waves in the backward, whose reads and writes come in longer runs then
+//    (bf16 4096 x 32000 95.5, four waves 106; 8192 x 16384 93.3 and 92.1), in the forward
+//    only where rows are few (16 x 128256 10.3 and 11.9; 1024 x 128256 51.3 and 48.8);
+//  - else four waves.
+enum { ROW_WAVE, ROW_BLOCK, ROW_WIDE };
+template <bool BF>
+static int row_kind(const LogitLossArgs& a, bool backward) {
+  constexpr int W = Row<BF>::W;
+  if (a.t.k <= 64 && (a.V <= 128 * W || (!backward && a.V <= 512 * W && a.T >= 2048))) return ROW_WAVE;
+  if (a.V >= 24576 && (backward || a.T <= 512)) return ROW_WIDE;
+  return ROW_BLOCK;
 }
-template <bool BF, int NT>
-static void logit_backward(const LogitLossArgs& a, bool two, hipStream_t s) {
+// Whether loads and stores stream past the caches: where the logits outgrow the L2s
+// (forward bf16 1024 x 128256 53.1 without, 48.8 with; 16 x 128256 11.9 and 16.0).
+template <bool BF>
+static bool row_streams(const LogitLossArgs& a) {
+  return streaming(a.T * a.V * (BF ? 2 : 4), 0) > 0;
+}
+
+template <bool BF, int NT, int MODE, bool STREAM>
+static void logit_forward(const LogitLossArgs& a, bool rest, hipStream_t s) {
   const dim3 g((unsigned)a.T), b(NT);
-  if (two) hipLaunchKernelGGL((logit_loss_bwd_kernel<BF, NT, true>), g, b, 0, s, a);
-  else hipLaunchKernelGGL((logit_loss_bwd_kernel<BF, NT, false>), g, b, 0, s, a);
+  if (rest) hipLaunchKernelGGL((logit_loss_kernel<BF, NT, MODE, true, STREAM>), g, b, 0, s, a);
+  else hipLaunchKernelGGL((logit_loss_kernel<BF, NT, MODE, false, STREAM>), g, b, 0, s, a);
+}
+template <bool BF, int MODE>
+static void logit_mode(const LogitLossArgs& a, bool rest, bool backward, hipStream_t s) {
+  const dim3 g((unsigned)a.T);
+  const int kind = row_kind<BF>(a, backward);
+  const bool stream = row_streams<BF>(a);
+  if (!backward) {
+    if (kind == ROW_WAVE) logit_forward<BF, 64, MODE, false>(a, rest, s);
+    else if (kind == ROW_WIDE) logit_forward<BF, 1024, MODE, false>(a, rest, s);
+    else if (stream) logit_forward<BF, 256, MODE, true>(a, rest, s);
+    else logit_forward<BF, 256, MODE, false>(a, rest, s);
+  } else if (kind == ROW_WAVE) {
+    hipLaunchKernelGGL((logit_loss_bwd_kernel<BF, 64, MODE, false>), g, dim3(64), 0, s, a);
+  } else if (kind == ROW_WIDE) {
+    if (stream) hipLaunchKernelGGL((logit_loss_bwd_kernel<BF, 1024, MODE, true>), g, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((logit_loss_bwd_kernel<BF, 1024, MODE, false>), g, dim3(1024), 0, s, a);
+  } else {
+    if (stream) hipLaunchKernelGGL((logit_loss_bwd_kernel<BF, 256, MODE, true>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((logit_loss_bwd_kernel<BF, 256, MODE, false>), g, dim3(256), 0, s, a);
+  }
+}
+template <bool BF>
+static void logit_launch(const LogitLossArgs& a, bool backward, hipStream_t s) {
+  const bool hard = a.t.labels != nullptr, soft = a.t.ids != nullptr, rest = soft && a.t.rest;
+  const bool two = hard && soft && (rest || a.t.temperature != 1.f);
+  if (!two) logit_mode<BF, EXP_ONE>(a, rest, backward, s);
+  else if (a.t.temperature == 2.f) logit_mode<BF, EXP_SQUARE>(a, rest, backward, s);
+  else logit_mode<BF, EXP_TWO>(a, rest, backward, s);
 }
 
 hipError_t launch_logit_loss(const LogitLossArgs& a, int dtype, bool backward, hipStream_t s) {
   if (a.T == 0) return hipSuccess;
-  const bool hard = a.t.labels != nullptr, soft = a.t.ids != nullptr, rest = soft && a.t.rest;
-  const bool two = hard && soft && (rest || a.t.temperature != 1.f);
-  const bool bf = dtype == BF16;
-  if (!backward) {
-    if (bf) logit_forward<true, 256>(a, two, rest, s);
-    else logit_forward<false, 256>(a, two, rest, s);
-  } else {
-    if (bf) logit_backward<true, 256>(a, two, s);
-    else logit_backward<false, 256>(a, two, s);
-  }
+  if (dtype == BF16) logit_launch<true>(a, backward, s);
+  else logit_launch<false>(a, backward, s);
   return hipGetLastError();
 }
 

@@ -7,6 +7,10 @@
 
 namespace zl {
 
+// 0, or which accesses of a call with so many bytes of output and input stream past the
+// caches (layer.hip).
+int streaming(int64_t out, int64_t in);
+
 constexpr int TOP_MAX_K = 256;
 
 hipError_t launch_top_logits(int64_t T, int V, const void* x, int64_t ldx, int dtype, int k, float temperature,
