@@ -289,176 +289,219 @@ static hipError_t run_head(const GemmDesc& g, const E& e, bool large, hipStream_
   return run_head_tiles<128, 128, 2, 2, AK, BKM>(g, e, nz, s);
 }
 
-// fp32: 128 x 128 tiles of four waves, v_mfma_f32_32x32x2_f32, 16 of K a step; the
-// next step is loaded while one is multiplied (two LDS buffers, one barrier a step).
-constexpr int SK = 16, ST = 128, SLD = ST + 4;
-template <bool KMAJ>
+// fp32: tiles of four waves, v_mfma_f32_32x32x2_f32, 32 of K a step, the next step's
+// operands in registers while one is multiplied.  A matrix instruction takes k and k + 16
+// of the step (the order of a sum is free), so that a lane's share of a K-major row is 16
+// consecutive floats, read 16 bytes at a time from rows as they came.
+constexpr int SK = 32;
+template <int R, bool KMAJ>
 struct F32Stage {
-  float4 v[2];
-  // rows r0 .. of R valid ones, k0 .. of kmax
-  __device__ __forceinline__ void load(const float* base, int64_t ld, int r0, int R, int k0, int kmax) {
+  static constexpr int LD = KMAJ ? SK + 4 : R + 4, ITEMS = R * SK / 4 / 256;
+  static constexpr int FLOATS = KMAJ ? R * LD : SK * LD;
+  static_assert(ITEMS >= 1, "a step fills the threads");
+  float4 v[ITEMS];
+  // rows r0 .., those below rmax valid; k0 .., those below kmax
+  __device__ __forceinline__ void load(const float* base, int64_t ld, int r0, int rmax, int k0, int kmax) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
       const int t = (int)threadIdx.x + 256 * i;
       v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (KMAJ) {
-        const int r = r0 + (t >> 2), k = k0 + (t & 3) * 4;  // kmax is a multiple of 4
-        if (r < R && k < kmax) v[i] = *reinterpret_cast<const float4*>(base + r * ld + k);
+        const int r = r0 + (t >> 3), k = k0 + (t & 7) * 4;  // kmax is a multiple of 4
+        if (r < rmax && k < kmax) v[i] = *reinterpret_cast<const float4*>(base + r * ld + k);
       } else {
-        const int k = k0 + (t >> 5), r = r0 + (t & 31) * 4;
-        if (k < kmax && r < R) v[i] = *reinterpret_cast<const float4*>(base + k * ld + r);  // padded rows
+        const int k = k0 + t / (R / 4), r = r0 + t % (R / 4) * 4;
+        if (k < kmax && r < rmax) v[i] = *reinterpret_cast<const float4*>(base + k * ld + r);  // padded rows
       }
     }
   }
-  __device__ __forceinline__ void store(float (*s)[SLD]) const {
+  __device__ __forceinline__ void store(float* s) const {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
       const int t = (int)threadIdx.x + 256 * i;
-      if (KMAJ) {
-        const int r = t >> 2, k = (t & 3) * 4;
-        s[k][r] = v[i].x;
-        s[k + 1][r] = v[i].y;
-        s[k + 2][r] = v[i].z;
-        s[k + 3][r] = v[i].w;
-      } else {
-        *reinterpret_cast<float4*>(&s[t >> 5][(t & 31) * 4]) = v[i];
-      }
+      *reinterpret_cast<float4*>(s + (KMAJ ? (t >> 3) * LD + (t & 7) * 4 : t / (R / 4) * LD + t % (R / 4) * 4)) = v[i];
+    }
+  }
+  // row r at k + 0 .. 3
+  __device__ static __forceinline__ void read(const float* s, int r, int k, float (&o)[4]) {
+    if constexpr (KMAJ) {
+      const float4 f = *reinterpret_cast<const float4*>(s + r * LD + k);
+      o[0] = f.x; o[1] = f.y; o[2] = f.z; o[3] = f.w;
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) o[q] = s[(k + q) * LD + r];
     }
   }
 };
-template <bool AK, bool BKM, typename E>
+template <int BM, int BN, int WM, int WN, bool AK, bool BKM, typename E>
 __global__ void __launch_bounds__(256) head_f32_kernel(GemmDesc g, E e) {
-  __shared__ __align__(16) float lds[4][SK][SLD];
-  float (*As)[SK][SLD] = lds, (*Bs)[SK][SLD] = lds + 2;
-  static_assert(4 * RowsOut<ST / 2, 32>::BYTES <= sizeof(lds), "rows of the epilogue exceed LDS");
-  const int nbm = (g.M + ST - 1) / ST, nbn = (g.N + ST - 1) / ST;
+  constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
+  static_assert(WM * WN == 4, "four waves");
+  using SA = F32Stage<BM, AK>;
+  using SB = F32Stage<BN, BKM>;
+  constexpr int OUT = 4 * RowsOut<TN, 32>::BYTES / 4;
+  constexpr int LDS = SA::FLOATS + SB::FLOATS > OUT ? SA::FLOATS + SB::FLOATS : OUT;
+  __shared__ __align__(16) float lds[LDS];
+  float *As = lds, *Bs = lds + SA::FLOATS;
+  const int nbm = (g.M + BM - 1) / BM, nbn = (g.N + BN - 1) / BN;
   int tm, tn;
   tile_coords(blockIdx.x, nbm, nbn, tm, tn);
-  const int m0 = tm * ST, n0 = tn * ST;
+  const int m0 = tm * BM, n0 = tn * BN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64, lr = lane & 31, lk = lane >> 5;
+  const int wm = wave / WN * TM, wn = wave % WN * TN, lr = lane & 31, lk = (lane >> 5) * (SK / 2);
   const int k_lo = blockIdx.z * g.ksplit, k_hi = min(g.K, k_lo + g.ksplit);
   const int ka = min(g.ka, k_hi), kb = min(g.kb, k_hi);
   const float* A = static_cast<const float*>(g.A);
   const float* B = static_cast<const float*>(g.B);
-  Mma<32>::acc_t acc[2][2];
+  Mma<32>::acc_t acc[FM][FN];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  F32Stage<AK> sa;
-  F32Stage<BKM> sb;
+  SA sa;
+  SB sb;
   sa.load(A, g.lda, m0, g.M, k_lo, ka);
   sb.load(B, g.ldb, n0, g.N, k_lo, kb);
-  sa.store(As[0]);
-  sb.store(Bs[0]);
-  int cur = 0;
   for (int k0 = k_lo; k0 < k_hi; k0 += SK) {
+    __syncthreads();  // the step before is fully read
+    sa.store(As);
+    sb.store(Bs);
     __syncthreads();
     sa.load(A, g.lda, m0, g.M, k0 + SK, ka);
     sb.load(B, g.ldb, n0, g.N, k0 + SK, kb);
 #pragma unroll
-    for (int k = 0; k < SK; k += 2) {
-      float a[2], b[2];
+    for (int k = 0; k < SK / 2; k += 4) {
+      float a[FM][4], b[FN][4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        a[i] = As[cur][k + lk][wm + 32 * i + lr];
-        b[i] = Bs[cur][k + lk][wn + 32 * i + lr];
-      }
+      for (int i = 0; i < FM; ++i) SA::read(As, wm + 32 * i + lr, lk + k, a[i]);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < FN; ++j) SB::read(Bs, wn + 32 * j + lr, lk + k, b[j]);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j], a[i], acc[i][j], 0, 0, 0);
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j][q], a[i][q], acc[i][j], 0, 0, 0);
     }
-    cur ^= 1;
-    sa.store(As[cur]);
-    sb.store(Bs[cur]);
   }
   __syncthreads();
-  store_tile<ST, ST, 2, 2, 32>(acc, reinterpret_cast<unsigned char*>(lds), g, e, m0, n0, wave, lane);
+  store_tile<BM, BN, WM, WN, 32>(acc, reinterpret_cast<unsigned char*>(lds), g, e, m0, n0, wave, lane);
 }
+template <int BM, int BN, int WM, int WN, bool AK, bool BKM, typename E>
+static hipError_t run_f32_tiles(const GemmDesc& g, const E& e, hipStream_t s, int nz) {
+  const int nb = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
+  hipLaunchKernelGGL((head_f32_kernel<BM, BN, WM, WN, AK, BKM, E>), dim3(nb, 1, nz), dim3(256), 0, s, g, e);
+  return hipGetLastError();
+}
+// 32 rows of a tile where there are no more (of a product with K-major A: dw has a row
+// per column of the vocabulary).
+static int f32_rows(int64_t M, bool ak) { return ak && M <= 32 ? 32 : 128; }
 template <bool AK, bool BKM, typename E>
 static hipError_t run_head_f32(const GemmDesc& g, const E& e, hipStream_t s, int nz = 1) {
-  const int nb = ((g.M + ST - 1) / ST) * ((g.N + ST - 1) / ST);
-  hipLaunchKernelGGL((head_f32_kernel<AK, BKM, E>), dim3(nb, 1, nz), dim3(256), 0, s, g, e);
-  return hipGetLastError();
+  if constexpr (AK) {
+    if (f32_rows(g.M, AK) == 32) return run_f32_tiles<32, 128, 1, 4, AK, BKM>(g, e, s, nz);
+  }
+  return run_f32_tiles<128, 128, 2, 2, AK, BKM>(g, e, s, nz);
 }
 
 // --------------------------------------------------------------- target rows
-// A wave per row: the teacher's ids with absent ones and repetitions as -1, then the
-// label (-1: none), to tid [T, k + 1]; with a mask, a bit per named column.
-__global__ void __launch_bounds__(256) head_targets_kernel(int64_t T, int V, zl_targets t, int32_t* tid, uint32_t* mask,
-                                                           int64_t ldm) {
-  __shared__ int32_t ids[4][ZL_TARGETS_MAX_K];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = t.k;
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+// The ids of a row, absent ones and repetitions as -1, into `ids` [256]: entries lane,
+// lane + 64, ... of every lane.  Whole waves, each a row of its own (or none).
+__device__ __forceinline__ void row_ids(const zl_targets& t, int V, int64_t row, bool on, int lane, int32_t* ids,
+                                        int32_t (&mine)[ZL_TARGETS_MAX_K / 64]) {
   constexpr int PER = ZL_TARGETS_MAX_K / 64;
-  int32_t mine[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int e = lane + 64 * i;
     mine[i] = -1;
-    if (row < T && e < k) {
-      const int32_t id = t.ids[row * k + e];
+    if (on && e < t.k) {
+      const int32_t id = t.ids[row * t.k + e];
       if (id >= 0 && id < V) mine[i] = id;
     }
-    ids[wave][e] = mine[i];
+    ids[e] = mine[i];
   }
-  if (row < T && mask)
-    for (int64_t w = lane; w < ldm; w += 64) mask[row * ldm + w] = 0;
-  __threadfence_block();
+  __syncthreads();
+  int32_t once[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    once[i] = mine[i];
+    for (int f = 0; f < lane + 64 * i && once[i] >= 0; ++f)
+      if (ids[f] == once[i]) once[i] = -1;
+  }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int e = lane + 64 * i;
-    if (row >= T || e >= k) continue;
-    int32_t id = mine[i];
-    // the words of the mask are formed whole, by the first entry in each
-    uint32_t bits = 0;
-    bool first = true;
-    for (int f = 0; f < k && mine[i] >= 0; ++f) {
-      const int32_t o = ids[wave][f];
-      if (o < 0) continue;
-      if (f < e && o == mine[i]) id = -1;
-      if (o >> 5 == mine[i] >> 5) {
-        bits |= 1u << (o & 31);
-        first &= f >= e;
-      }
-    }
-    tid[row * (k + 1) + e] = id;
-    if (mask && mine[i] >= 0 && first) mask[row * ldm + (mine[i] >> 5)] = bits;
+    mine[i] = once[i];
+    ids[lane + 64 * i] = once[i];
   }
-  if (row < T && lane == 0) {
-    const int32_t y = t.labels ? t.labels[row] : -1;
-    tid[row * (k + 1) + k] = y >= 0 && y < V ? y : -1;
-  }
+  __syncthreads();
+}
+__device__ __forceinline__ int32_t row_label(const zl_targets& t, int V, int64_t row) {
+  const int32_t y = t.labels ? t.labels[row] : -1;
+  return y >= 0 && y < V ? y : -1;
 }
 
-// The logits that the targets name: a wave per entry, x and w read 16 bytes a lane.
-// Column of stats: the label's 3, id e's 4 + e.
+// x row . w row, 16 bytes a lane and load; every lane gets the sum.
 template <bool BF>
-__global__ void __launch_bounds__(256) head_named_kernel(int64_t n, int d, int k, const void* x, int64_t ldx,
-                                                         const void* w, int64_t ldw, const int32_t* tid, float* stats) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= n) return;
-  const int64_t row = at / (k + 1);
-  const int e = (int)(at - row * (k + 1));
-  const int32_t id = tid[at];
+__device__ __forceinline__ float row_dot(int d, const void* x, int64_t ox, const void* w, int64_t ow, int lane) {
   float s = 0.f;
-  if (id >= 0) {
-    for (int c = lane * 8; c < d; c += 512) {
-      float a[8], b[8];
-      ldv_act(x, BF ? BF16 : F32, row * ldx + c, a);
-      ldv_act(w, BF ? BF16 : F32, id * ldw + c, b);
+#pragma unroll 2
+  for (int c = lane * 8; c < d; c += 512) {
+    float a[8], b[8];
+    ldv_act(x, BF ? BF16 : F32, ox + c, a);
+    ldv_act(w, BF ? BF16 : F32, ow + c, b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += a[i] * b[i];
-    }
-    s = wave_sum(s);
+    for (int i = 0; i < 8; ++i) s += a[i] * b[i];
   }
-  if (lane == 0) stats[row * (4 + k) + (e == k ? 3 : 4 + e)] = s;
+  return wave_sum(s);
+}
+
+// What the targets name of every row: ids to tid [T, k + 1] (absent ones and repetitions
+// as -1, then the label), their logits to stats (the label's column 3, id e's 4 + e),
+// with a mask a bit per named column.  A block per `per` entries of a row, four of
+// them at a time; the row's first block writes tid and the mask.
+template <bool BF>
+__global__ void __launch_bounds__(256) head_named_kernel(int V, int d, zl_targets t, int per, const void* x, int64_t ldx,
+                                                         const void* w, int64_t ldw, int32_t* tid, float* stats,
+                                                         uint32_t* mask, int64_t ldm) {
+  __shared__ int32_t ids[4][ZL_TARGETS_MAX_K];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = t.k;
+  const int64_t row = blockIdx.x;
+  int32_t mine[ZL_TARGETS_MAX_K / 64];
+  const bool first = blockIdx.y == 0;
+  // cleared and set by one wave, whose stores stay in order
+  if (first && mask && wave == 0)
+    for (int64_t i = lane * 4; i < ldm; i += 256) *reinterpret_cast<uint4*>(mask + row * ldm + i) = make_uint4(0, 0, 0, 0);
+  row_ids(t, V, row, true, lane, ids[wave], mine);  // ends with a barrier
+  const int32_t y = row_label(t, V, row);
+  if (first && wave == 0) {
+#pragma unroll
+    for (int i = 0; i < ZL_TARGETS_MAX_K / 64; ++i) {
+      const int e = lane + 64 * i;
+      if (e >= k) continue;
+      tid[row * (k + 1) + e] = mine[i];
+      // a word of the mask is formed whole, by the first entry in it
+      uint32_t bits = 0;
+      bool lead = true;
+      for (int f = 0; f < k && mask && mine[i] >= 0; ++f) {
+        const int32_t o = ids[0][f];
+        if (o < 0 || o >> 5 != mine[i] >> 5) continue;
+        bits |= 1u << (o & 31);
+        lead &= f >= e;
+      }
+      if (mask && mine[i] >= 0 && lead) mask[row * ldm + (mine[i] >> 5)] = bits;
+    }
+    if (lane == 0) tid[row * (k + 1) + k] = y;
+  }
+  const int e1 = min(k + 1, ((int)blockIdx.y + 1) * per);
+  for (int e = blockIdx.y * per + wave; e < e1; e += 4) {
+    const int32_t id = e == k ? y : ids[wave][e];
+    const float z = id >= 0 ? row_dot<BF>(d, x, row * ldx, w, id * ldw, lane) : 0.f;
+    if (lane == 0) stats[row * (4 + k) + (e == k ? 3 : 4 + e)] = z;
+  }
 }
 
 // The teacher's distribution over a row's entries, a wave per row.
@@ -500,11 +543,12 @@ struct WaveTeacher {
 
 // Joins the partial sums of R rows, 256 / R strands of blocks each, then a wave per
 // row forms its losses.  PAIR: both log-sums; masked: the second leaves the
-// teacher's ids out.
-template <int R, bool PAIR>
-__global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int blocks, const float* part, zl_targets t, float a,
-                                                        float b, bool masked, const int32_t* tid, float* loss,
-                                                        float* stats) {
+// teacher's ids out.  Without a teacher the label's logit is formed here too.
+template <int R, bool PAIR, bool BF>
+__global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d, int blocks, const float* part,
+                                                        zl_targets t, float a, float b, bool masked, const void* x_,
+                                                        int64_t ldx, const void* w_, int64_t ldw, const int32_t* tid,
+                                                        float* loss, float* stats) {
   constexpr int S = 256 / R;
   __shared__ float4 red[S][R];
   const int r = threadIdx.x % R, st = threadIdx.x / R, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -546,7 +590,11 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int blocks, c
     }
     const int32_t* id = tid + row * (t.k + 1);
     float* out = stats + row * (4 + t.k);
-    const bool label = id[t.k] >= 0;
+    const int32_t yl = row_label(t, V, row);
+    const bool label = yl >= 0;
+    float zy = 0.f;
+    if (!t.ids && label) zy = row_dot<BF>(d, x_, row * ldx, w_, yl * ldw, lane);
+    else if (label) zy = out[3];
     float total = 0.f, lt = 0.f, other = 0.f, l1 = 0.f;
     bool on = false;
     if (t.ids) {
@@ -580,12 +628,13 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int blocks, c
     }
     l1 = PAIR ? p.log(1.f) : lt;
     if (lane == 0) {
-      if (label) total += a * (l1 - out[3]);
+      if (label) total += a * (l1 - zy);
       if (!label && !on) total = 0.f;
       loss[row] = total;
       out[0] = label ? l1 : 0.f;
       out[1] = on ? lt : 0.f;
       out[2] = on && masked ? other : 0.f;
+      out[3] = zy;
     }
   }
 }
@@ -594,24 +643,41 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int blocks, c
 __global__ void __launch_bounds__(1024) head_gmax_kernel(int64_t T, const float* dloss, float* gmax) {
   __shared__ float red[16];
   float m = 0.f;
-  for (int64_t i = threadIdx.x; i < T; i += 1024) m = fmaxf(m, dloss ? fabsf(dloss[i]) : 1.f);
+  for (int64_t i = threadIdx.x; i < T; i += 1024) m = fmaxf(m, fabsf(dloss[i]));
   m = block_max<1024>(m, red);
   if (threadIdx.x == 0) *gmax = m > 0.f && m < INFINITY ? m : 1.f;
 }
+constexpr int GMAX_ROWS = 4096;  // up to which every block of the next kernel looks for itself
 
-// Per row what dL/dz takes (GradEpi), and the named columns' values; a wave per row.
-__global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, zl_targets t, float a, float b, int mode,
-                                                        const float* stats, const float* dloss, const float* gmax,
-                                                        int32_t* tid, float* tval, float4* coef, int32_t* live) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+// Per row what dL/dz takes (GradEpi), the named columns (tid as in the forward) and
+// their values; a wave per row.
+__global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, int V, zl_targets t, float a, float b, int mode,
+                                                        const float* stats, const float* dloss, float* gmax, int32_t* tid,
+                                                        float* tval, float4* coef, int32_t* live) {
+  __shared__ float red[4];
+  __shared__ int32_t ids[4][ZL_TARGETS_MAX_K];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+  int32_t mine[ZL_TARGETS_MAX_K / 64];
+  if (t.ids) row_ids(t, V, row, row < T, lane, ids[wave], mine);
+  float most = 1.f;
+  if (dloss && T <= GMAX_ROWS) {
+    float m = 0.f;
+    for (int i = threadIdx.x; i < (int)T; i += 256) m = fmaxf(m, fabsf(dloss[i]));
+    m = block_max<256>(m, red);
+    most = m > 0.f && m < INFINITY ? m : 1.f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *gmax = most;
+  } else if (dloss) {
+    most = *gmax;
+  }
   if (row >= T) return;
+  const int32_t* id = ids[wave];
   const float* s = stats + row * (4 + t.k);
-  int32_t* id = tid + row * (t.k + 1);
+  int32_t* to = tid + row * (t.k + 1);
   float* val = tval + row * (t.k + 1);
   const float l1 = s[0], ls = s[1], lo = s[2];
-  const int y = id[t.k];
-  const float up = (dloss ? dloss[row] : 1.f) / *gmax;
+  const int32_t y = row_label(t, V, row);
+  const float up = dloss ? dloss[row] / most : 1.f;
   const float c1 = y >= 0 ? a * up : 0.f;
   float ct = 0.f, lt = ls, inv = 1.f;
   bool named = false, on = false;
@@ -628,12 +694,13 @@ __global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, zl_targets t,
 #pragma unroll
     for (int i = 0; i < WaveTeacher::PER; ++i) {
       const int e = lane + 64 * i;
-      if (e < t.k && id[e] >= 0) {
+      if (e < t.k) to[e] = mine[i];
+      if (e < t.k && mine[i] >= 0) {
         const float z = s[4 + e];
         float g = on ? f * (expf(z * inv - ls) - w.p[i]) : 0.f;
-        if (y >= 0) g += c1 * (id[e] == y ? expm1f(z - l1) : expf(z - l1));
+        if (y >= 0) g += c1 * (mine[i] == y ? expm1f(z - l1) : expf(z - l1));
         val[e] = g;
-        named |= id[e] == y;
+        named |= mine[i] == y;
       }
     }
   }
@@ -661,8 +728,8 @@ __global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, zl_targets t,
     coef[row] = c;
     live[row] = on || y >= 0;
   }
-  // an entry of the label that an id names too is that id's
-  if (named && lane == 0) id[t.k] = -2 - y;
+  // a label that an id names too is that id's entry
+  if (lane == 0) to[t.k] = named ? -1 : y;
 }
 
 // The named columns of the piece [v0, v0 + n) over what the product wrote.
@@ -748,7 +815,8 @@ HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool rest, bool ba
     GemmShape sh = {(int)T, V, d, true, true, false, 0, false, 0};
     p.large = plan_gemm(sh).large;
   }
-  const int width = p.large ? 128 : 64;  // columns of a wave tile
+  // columns of a wave tile
+  const int width = p.large ? 128 : dtype == F32 && f32_rows(T, true) == 32 ? 32 : 64;
   p.blocks = (V + width - 1) / width;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -823,14 +891,17 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   uint32_t* mask = masked ? reinterpret_cast<uint32_t*>(ws + p.mask) : nullptr;
   float wa, wb;
   loss_weights(t, wa, wb);
-  hipLaunchKernelGGL(head_targets_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, a.V, t, tid, mask, p.ldm);
-  const int64_t named = T * (t.k + 1);
-  if (bf)
-    hipLaunchKernelGGL((head_named_kernel<true>), dim3(grid(named, 4)), dim3(256), 0, s, named, a.d, t.k, a.x, a.ldx, a.w,
-                       a.ldw, tid, a.stats);
-  else
-    hipLaunchKernelGGL((head_named_kernel<false>), dim3(grid(named, 4)), dim3(256), 0, s, named, a.d, t.k, a.x, a.ldx, a.w,
-                       a.ldw, tid, a.stats);
+  if (soft) {
+    // four entries a block where rows are few, a row where they are many
+    const int per = T * (t.k + 1) <= 16384 ? 4 : t.k + 1;
+    const dim3 g((unsigned)T, grid(t.k + 1, per));
+    if (bf)
+      hipLaunchKernelGGL((head_named_kernel<true>), g, dim3(256), 0, s, a.V, a.d, t, per, a.x, a.ldx, a.w, a.ldw, tid,
+                         a.stats, mask, p.ldm);
+    else
+      hipLaunchKernelGGL((head_named_kernel<false>), g, dim3(256), 0, s, a.V, a.d, t, per, a.x, a.ldx, a.w, a.ldw, tid,
+                         a.stats, mask, p.ldm);
+  }
   // a masked sum is always the second of a pair
   const bool two = pair || masked;
   const GemmDesc g = head_gemm(T, a.V, a.d, a.x, a.ldx, true, a.w, a.ldw, true);
@@ -843,8 +914,12 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   auto rows = [&](auto rc, auto pc) {
     constexpr int R = decltype(rc)::value;
     constexpr bool P = decltype(pc)::value;
-    hipLaunchKernelGGL((head_rows_kernel<R, P>), dim3(grid(T, R)), dim3(256), 0, s, T, p.blocks, part, t, wa, wb, masked,
-                       tid, a.loss, a.stats);
+    if (bf)
+      hipLaunchKernelGGL((head_rows_kernel<R, P, true>), dim3(grid(T, R)), dim3(256), 0, s, T, a.V, a.d, p.blocks, part, t,
+                         wa, wb, masked, a.x, a.ldx, a.w, a.ldw, tid, a.loss, a.stats);
+    else
+      hipLaunchKernelGGL((head_rows_kernel<R, P, false>), dim3(grid(T, R)), dim3(256), 0, s, T, a.V, a.d, p.blocks, part, t,
+                         wa, wb, masked, a.x, a.ldx, a.w, a.ldw, tid, a.loss, a.stats);
   };
   using std::integral_constant;
   auto by_rows = [&](auto pc) {
@@ -857,9 +932,18 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Splits of an fp32 product's K: up to two blocks a CU, 128 of K each at least.
-static int f32_splits(int64_t M, int64_t N, int64_t K, size_t elems, int& ksplit) {
-  const int64_t tiles = ((M + ST - 1) / ST) * ((N + ST - 1) / ST);
+// Splits of a product's K; a part is a multiple of the k tile.
+template <bool AK, bool BKM>
+static int head_splits(int64_t M, int64_t N, int64_t K, bool bf, size_t elems, bool& large, int& ksplit) {
+  large = false;
+  if (bf) {
+    const GemmShape sh = {(int)M, (int)N, (int)K, AK, BKM, true, elems, false, 0};
+    const GemmPlan pl = plan_gemm(sh);
+    large = pl.large;
+    return split_k((int)K, pl.nz, KTile<AK, BKM>::BK, ksplit);
+  }
+  // up to two blocks a CU, 128 of K each at least
+  const int64_t tiles = ((M + f32_rows(M, AK) - 1) / f32_rows(M, AK)) * ((N + 127) / 128);
   int64_t nz = tiles >= 256 ? 1 : 512 / tiles;
   if (nz > K / 128) nz = K / 128;
   if (nz > (int64_t)(elems / (size_t)(M * N))) nz = (int64_t)(elems / (size_t)(M * N));
@@ -894,16 +978,24 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
   void* xc = ws + p.xc;
   float wa, wb;
   loss_weights(t, wa, wb);
-  hipLaunchKernelGGL(head_targets_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, a.V, t, tid, (uint32_t*)nullptr, (int64_t)0);
-  hipLaunchKernelGGL(head_gmax_kernel, dim3(1), dim3(1024), 0, s, T, a.dloss, gmax);
-  hipLaunchKernelGGL(head_coef_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, t, wa, wb, mode, a.stats, a.dloss, gmax,
+  if (a.dloss && T > GMAX_ROWS) hipLaunchKernelGGL(head_gmax_kernel, dim3(1), dim3(1024), 0, s, T, a.dloss, gmax);
+  hipLaunchKernelGGL(head_coef_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, a.V, t, wa, wb, mode, a.stats, a.dloss, gmax,
                      tid, tval, coef, live);
+  const float* most = a.dloss ? gmax : nullptr;
   if (a.dw)
     hipLaunchKernelGGL(head_clean_kernel, dim3(grid(T * (d / 8), 256)), dim3(256), 0, s, T, d, live, a.x, a.ldx, xc, dt);
   ZL_TRY(hipGetLastError());
+  auto finish = [&](int64_t rows, const float* in, int nz, float scale, const float* by, void* out, int64_t ldo, int type,
+                    int accumulate) {
+    hipLaunchKernelGGL(head_finish_kernel, dim3(grid(rows * (d / 8), 256)), dim3(256), 0, s, rows, d, in, nz, scale, by, out,
+                       ldo, type, accumulate);
+  };
   const size_t es = bf ? 2 : 4;
-  for (int v0 = 0; v0 < a.V; v0 += p.columns) {
-    const int n = a.V - v0 < p.columns ? a.V - v0 : p.columns;
+  // a piece of w is read with 32-bit offsets
+  const int64_t reach = (((int64_t)1 << 30) - 1) / a.ldw / 256 * 256;
+  const int columns = p.columns < reach ? p.columns : (int)reach;
+  for (int v0 = 0; v0 < a.V; v0 += columns) {
+    const int n = a.V - v0 < columns ? a.V - v0 : columns;
     const int n8 = (n + 7) / 8 * 8;
     const char* w = static_cast<const char*>(a.w) + (size_t)v0 * a.ldw * es;
     {
@@ -920,56 +1012,38 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
     const int64_t named = T * (t.k + 1);
     hipLaunchKernelGGL(head_put_kernel, dim3(grid(named, 256)), dim3(256), 0, s, named, t.k, v0, n, tid, tval, dz, p.ldz, dt);
     ZL_TRY(hipGetLastError());
+    // a product's tiles write where the result belongs; splits of K and, for dx, pieces
+    // of the vocabulary meet in fp32 first
+    const bool first = v0 == 0, last = v0 + n >= a.V;
     if (a.dx) {
       GemmDesc g = head_gemm(T, d, n8, dz, p.ldz, true, w, a.ldw, false);
       g.kb = n;
-      if (bf) {
-        g.part = split;
-        g.part_elems = p.split_elems;
-        EpiArgs e;
-        memset(&e, 0, sizeof(e));
-        e.kind = EPI_GRAD;
-        e.out = dxa;
-        e.ldo = d;
-        e.out_dtype = F32;
-        e.scale = 1.f;
-        e.accumulate = v0 > 0;
-        ZL_TRY(launch_gemm(g, e, BF16, s));
-      } else {
-        const int nz = f32_splits(T, d, n8, p.split_elems, g.ksplit);
-        OutEpi e = {dxa, d, F32, 1.f, nullptr, v0 > 0, 0};
-        if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, T * d};
-        ZL_TRY((run_head_f32<true, false>(g, e, s, nz)));
-        if (nz > 1)
-          hipLaunchKernelGGL(head_finish_kernel, dim3(grid(T * (d / 8), 256)), dim3(256), 0, s, T, d, split, nz, 1.f,
-                             (const float*)nullptr, dxa, (int64_t)d, (int)F32, (int)(v0 > 0));
-      }
+      bool large;
+      const int nz = head_splits<true, false>(T, d, n8, bf, p.split_elems, large, g.ksplit);
+      const bool whole = first && last;
+      OutEpi e = {dxa, d, F32, 1.f, nullptr, !first, 0};
+      if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, T * d};
+      else if (whole) e = {a.dx, a.lddx, dxt, a.scale, most, 0, 0};
+      if (bf) ZL_TRY((run_head<true, false>(g, e, large, s, nz)));
+      else ZL_TRY((run_head_f32<true, false>(g, e, s, nz)));
+      if (nz > 1 && whole)
+        finish(T, split, nz, a.scale, most, a.dx, a.lddx, dxt, 0);
+      else if (nz > 1)
+        finish(T, split, nz, 1.f, nullptr, dxa, d, F32, !first);
+      if (last && !whole) finish(T, dxa, 1, a.scale, most, a.dx, a.lddx, dxt, 0);
     }
     if (a.dw) {
       GemmDesc g = head_gemm(n, d, T, dz, p.ldz, false, xc, d, false);
       char* out = static_cast<char*>(a.dw) + (size_t)v0 * a.lddw * (dwt == BF16 ? 2 : 4);
-      int nz = 1;
-      bool large = false;
-      if (bf) {
-        GemmShape sh = {n, d, (int)T, false, false, true, p.split_elems, false, 0};
-        const GemmPlan pl = plan_gemm(sh);
-        large = pl.large;
-        nz = split_k((int)T, pl.nz, KTile<false, false>::BK, g.ksplit);
-      } else {
-        nz = f32_splits(n, d, T, p.split_elems, g.ksplit);
-      }
-      OutEpi e = {out, a.lddw, dwt, a.scale, gmax, a.accumulate, 0};
+      bool large;
+      const int nz = head_splits<false, false>(n, d, T, bf, p.split_elems, large, g.ksplit);
+      OutEpi e = {out, a.lddw, dwt, a.scale, most, a.accumulate, 0};
       if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, (int64_t)n * d};
       if (bf) ZL_TRY((run_head<false, false>(g, e, large, s, nz)));
       else ZL_TRY((run_head_f32<false, false>(g, e, s, nz)));
-      if (nz > 1)
-        hipLaunchKernelGGL(head_finish_kernel, dim3(grid((int64_t)n * (d / 8), 256)), dim3(256), 0, s, (int64_t)n, d, split,
-                           nz, a.scale, gmax, (void*)out, a.lddw, dwt, a.accumulate);
+      if (nz > 1) finish(n, split, nz, a.scale, most, out, a.lddw, dwt, a.accumulate);
     }
   }
-  if (a.dx)
-    hipLaunchKernelGGL(head_finish_kernel, dim3(grid(T * (d / 8), 256)), dim3(256), 0, s, T, d, dxa, 1, a.scale, gmax, a.dx,
-                       a.lddx, dxt, 0);
   return hipGetLastError();
 }
 

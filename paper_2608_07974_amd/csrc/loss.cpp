@@ -13,7 +13,7 @@ namespace {
 
 constexpr int64_t MAX_T = (int64_t)1 << 21;
 constexpr int MAX_V = 1 << 30;
-constexpr int64_t MAX_LD = (int64_t)1 << 22;  // of x and w: a tile's 32-bit offsets
+constexpr int64_t MAX_LD = (int64_t)1 << 21;  // of x and w: a tile's 32-bit offsets
 
 zl_status bad(const char* msg) { return set_error(ZL_ERR_INVALID_ARG, msg); }
 zl_status unsupported(const char* msg) { return set_error(ZL_ERR_UNSUPPORTED, msg); }
@@ -63,7 +63,7 @@ zl_status check_head(const zl_head_args* a, bool backward) {
   if (zl_status st = check_targets(a->targets, a->T)) return st;
   if (!mat_ok(a->x, a->ldx, a->d, a->T) || !mat_ok(a->w, a->ldw, a->d, a->T))
     return bad("x or w missing, not 16-byte aligned, or a bad row stride");
-  if (a->T && (a->ldx >= MAX_LD || a->ldw >= MAX_LD)) return unsupported("row strides of 2^22 and more");
+  if (a->T && (a->ldx >= MAX_LD || a->ldw >= MAX_LD)) return unsupported("row strides of 2^21 and more");
   if (a->T && (!a->stats || !by(a->stats, 4))) return bad("stats missing or misaligned");
   if (!backward) {
     if (a->T && (!a->loss || !by(a->loss, 4))) return bad("loss missing or misaligned");

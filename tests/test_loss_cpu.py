@@ -114,8 +114,8 @@ def test_head_loss_backward_refuses(kw):
 
 
 def test_head_loss_limits():
-    for kw in (dict(T=(1 << 21) + 1), dict(V=(1 << 30) + 1), dict(d=65544, ldx=65544, ldw=65544), dict(ldx=1 << 22),
-               dict(ldw=1 << 22), dict(targets=_t(k=257))):
+    for kw in (dict(T=(1 << 21) + 1), dict(V=(1 << 30) + 1), dict(d=65544, ldx=65544, ldw=65544), dict(ldx=1 << 21),
+               dict(ldw=1 << 21), dict(targets=_t(k=257))):
         _refused(UNS, zl.zl_head_loss, _head(**kw))
         _refused(UNS, zl.zl_head_loss_backward, _head(True, **kw))
     assert "accumulation" in _refused(UNS, zl.zl_head_loss_backward, _head(True, dw_dtype=zl.ZL_BF16))
