@@ -396,14 +396,23 @@ static hipError_t run_f32_tiles(const GemmDesc& g, const E& e, hipStream_t s, in
   hipLaunchKernelGGL((head_f32_kernel<BM, BN, WM, WN, AK, BKM, E>), dim3(nb, 1, nz), dim3(256), 0, s, g, e);
   return hipGetLastError();
 }
-// 32 rows of a tile where there are no more (of a product with K-major A: dw has a row
-// per column of the vocabulary).
-static int f32_rows(int64_t M, bool ak) { return ak && M <= 32 ? 32 : 128; }
+// Tiles by size: 32 rows where there are no more (of a product with K-major A: dw has a
+// row per column of the vocabulary); 64 x 64 where those of 128 x 128, with splits of 256 of
+// K at least where they may be, leave CUs idle (a matrix instruction takes 64 cycles: 64 of
+// K are 3.9 us in a tile of 128 x 128, 1 in one of 64 x 64; 4096 x 1000 x 512 60.7 and 53.8 us,
+// 128 x 50257 x 768 108 and 116); else 128 x 128.
+enum { F32_128, F32_64, F32_32 };
+static int f32_tile(int64_t M, int64_t N, int64_t split, bool ak) {
+  if (ak && M <= 32) return F32_32;
+  const int64_t parts = split >= 512 ? split / 256 : 1;
+  return ((M + 127) / 128) * ((N + 127) / 128) * parts <= 256 ? F32_64 : F32_128;
+}
 template <bool AK, bool BKM, typename E>
-static hipError_t run_head_f32(const GemmDesc& g, const E& e, hipStream_t s, int nz = 1) {
+static hipError_t run_head_f32(const GemmDesc& g, const E& e, int tile, hipStream_t s, int nz = 1) {
   if constexpr (AK) {
-    if (f32_rows(g.M, AK) == 32) return run_f32_tiles<32, 128, 1, 4, AK, BKM>(g, e, s, nz);
+    if (tile == F32_32) return run_f32_tiles<32, 128, 1, 4, AK, BKM>(g, e, s, nz);
   }
+  if (tile == F32_64) return run_f32_tiles<64, 64, 2, 2, AK, BKM>(g, e, s, nz);
   return run_f32_tiles<128, 128, 2, 2, AK, BKM>(g, e, s, nz);
 }
 
@@ -739,17 +748,24 @@ __global__ void __launch_bounds__(256) head_put_kernel(int64_t count, int k, int
   if (i >= count) return;
   const int32_t id = tid[i];
   if (id < v0 || id >= v0 + n) return;
-  st_act(dz, dtype, i / (k + 1) * ldz + (id - v0), tval[i]);
+  const int64_t row = i < 0x80000000ll ? (int64_t)((uint32_t)i / (uint32_t)(k + 1)) : i / (k + 1);
+  st_act(dz, dtype, row * ldz + (id - v0), tval[i]);
+}
+
+// Row and column of the i-th group of 8 among rows of `per` (a 64-bit division takes
+// longer than the group's memory).
+__device__ __forceinline__ int64_t split_groups(int64_t i, int per, int& c) {
+  const int64_t row = i < 0x80000000ll ? (int64_t)((uint32_t)i / (uint32_t)per) : i / per;
+  c = (int)(i - row * per) * 8;
+  return row;
 }
 
 // x with zeros in the rows that have no target (0 times NaN would spoil dw).
 __global__ void __launch_bounds__(256) head_clean_kernel(int64_t T, int d, const int32_t* live, const void* x,
                                                          int64_t ldx, void* xc, int dtype) {
-  const int per = d / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = i / per;
+  int c;
+  const int64_t row = split_groups((int64_t)blockIdx.x * 256 + threadIdx.x, d / 8, c);
   if (row >= T) return;
-  const int c = (int)(i - row * per) * 8;
   const bool on = live[row] != 0;
   if (dtype == BF16) {
     uint4 v = make_uint4(0, 0, 0, 0);
@@ -772,14 +788,13 @@ __global__ void __launch_bounds__(256) head_clean_kernel(int64_t T, int d, const
 __global__ void __launch_bounds__(256) head_finish_kernel(int64_t rows, int d, const float* in, int nz, float scale,
                                                           const float* gmax, void* out, int64_t ldo, int dtype,
                                                           int accumulate) {
-  const int per = d / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = i / per;
+  int c;
+  const int64_t row = split_groups((int64_t)blockIdx.x * 256 + threadIdx.x, d / 8, c);
   if (row >= rows) return;
-  const int c = (int)(i - row * per) * 8;
   const float f = gmax ? scale * *gmax : scale;
   float v[8], u[8];
   ldv_f32(in + row * d + c, v);
+#pragma unroll 4
   for (int z = 1; z < nz; ++z) {
     ldv_f32(in + z * rows * d + row * d + c, u);
 #pragma unroll
@@ -796,11 +811,11 @@ __global__ void __launch_bounds__(256) head_finish_kernel(int64_t rows, int d, c
 }
 
 __global__ void __launch_bounds__(256) head_zero_kernel(int64_t rows, int d, void* out, int64_t ldo, int dtype) {
-  const int per = d / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows * per) return;
+  int c;
+  const int64_t row = split_groups((int64_t)blockIdx.x * 256 + threadIdx.x, d / 8, c);
+  if (row >= rows) return;
   const float v[8] = {};
-  stv_act(out, dtype, i / per * ldo + i % per * 8, v);
+  stv_act(out, dtype, row * ldo + c, v);
 }
 
 // ------------------------------------------------------------------ launches
@@ -816,7 +831,7 @@ HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool rest, bool ba
     p.large = plan_gemm(sh).large;
   }
   // columns of a wave tile
-  const int width = p.large ? 128 : dtype == F32 && f32_rows(T, true) == 32 ? 32 : 64;
+  const int width = p.large ? 128 : dtype == F32 && f32_tile(T, V, 0, true) != F32_128 ? 32 : 64;
   p.blocks = (V + width - 1) / width;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -907,7 +922,7 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   const GemmDesc g = head_gemm(T, a.V, a.d, a.x, a.ldx, true, a.w, a.ldw, true);
   auto sums = [&](auto pc) -> hipError_t {
     const StatEpi<decltype(pc)::value> e = {soft ? LOG2E / t.temperature : LOG2E, part, T, mask, p.ldm};
-    return bf ? run_head<true, true>(g, e, p.large, s) : run_head_f32<true, true>(g, e, s);
+    return bf ? run_head<true, true>(g, e, p.large, s) : run_head_f32<true, true>(g, e, f32_tile(g.M, g.N, 0, true), s);
   };
   if (two) ZL_TRY(sums(std::true_type{}));
   else ZL_TRY(sums(std::false_type{}));
@@ -923,8 +938,8 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   };
   using std::integral_constant;
   auto by_rows = [&](auto pc) {
-    if (T >= 4096) rows(integral_constant<int, 32>{}, pc);
-    else if (T >= 64) rows(integral_constant<int, 4>{}, pc);
+    // two rows a wave; a block each where rows are few
+    if (T >= 512) rows(integral_constant<int, 8>{}, pc);
     else rows(integral_constant<int, 1>{}, pc);
   };
   if (two) by_rows(std::true_type{});
@@ -934,17 +949,18 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
 
 // Splits of a product's K; a part is a multiple of the k tile.
 template <bool AK, bool BKM>
-static int head_splits(int64_t M, int64_t N, int64_t K, bool bf, size_t elems, bool& large, int& ksplit) {
-  large = false;
+static int head_splits(int64_t M, int64_t N, int64_t K, bool bf, size_t elems, int& tile, int& ksplit) {
   if (bf) {
     const GemmShape sh = {(int)M, (int)N, (int)K, AK, BKM, true, elems, false, 0};
     const GemmPlan pl = plan_gemm(sh);
-    large = pl.large;
+    tile = pl.large;
     return split_k((int)K, pl.nz, KTile<AK, BKM>::BK, ksplit);
   }
-  // up to two blocks a CU, 128 of K each at least
-  const int64_t tiles = ((M + f32_rows(M, AK) - 1) / f32_rows(M, AK)) * ((N + 127) / 128);
-  int64_t nz = tiles >= 256 ? 1 : 512 / tiles;
+  // up to two blocks of 128 x 128 a CU, four of 64 x 64; 128 of K each at least
+  tile = f32_tile(M, N, K, AK);
+  const int64_t tiles = tile == F32_64 ? ((M + 63) / 64) * ((N + 63) / 64) : ((M + 127) / 128) * ((N + 127) / 128);
+  int64_t nz = (tile == F32_64 ? 1024 : 512) / tiles;
+  if (tile == F32_128 && tiles >= 256) nz = 1;
   if (nz > K / 128) nz = K / 128;
   if (nz > (int64_t)(elems / (size_t)(M * N))) nz = (int64_t)(elems / (size_t)(M * N));
   if (nz < 1) nz = 1;
@@ -1003,7 +1019,7 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
       GemmShape sh = {(int)T, n, d, true, true, false, 0, false, 0};
       auto grads = [&](auto mc) -> hipError_t {
         const GradEpi<decltype(mc)::value> e = {coef, soft ? 1.f / t.temperature : 1.f, dz, p.ldz, dt};
-        return bf ? run_head<true, true>(g, e, plan_gemm(sh).large, s) : run_head_f32<true, true>(g, e, s);
+        return bf ? run_head<true, true>(g, e, plan_gemm(sh).large, s) : run_head_f32<true, true>(g, e, f32_tile(g.M, g.N, 0, true), s);
       };
       if (mode == GRAD_ONE) ZL_TRY(grads(std::integral_constant<int, GRAD_ONE>{}));
       else if (mode == GRAD_TWO) ZL_TRY(grads(std::integral_constant<int, GRAD_TWO>{}));
@@ -1018,14 +1034,14 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
     if (a.dx) {
       GemmDesc g = head_gemm(T, d, n8, dz, p.ldz, true, w, a.ldw, false);
       g.kb = n;
-      bool large;
-      const int nz = head_splits<true, false>(T, d, n8, bf, p.split_elems, large, g.ksplit);
+      int tile;
+      const int nz = head_splits<true, false>(T, d, n8, bf, p.split_elems, tile, g.ksplit);
       const bool whole = first && last;
       OutEpi e = {dxa, d, F32, 1.f, nullptr, !first, 0};
       if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, T * d};
       else if (whole) e = {a.dx, a.lddx, dxt, a.scale, most, 0, 0};
-      if (bf) ZL_TRY((run_head<true, false>(g, e, large, s, nz)));
-      else ZL_TRY((run_head_f32<true, false>(g, e, s, nz)));
+      if (bf) ZL_TRY((run_head<true, false>(g, e, tile, s, nz)));
+      else ZL_TRY((run_head_f32<true, false>(g, e, tile, s, nz)));
       if (nz > 1 && whole)
         finish(T, split, nz, a.scale, most, a.dx, a.lddx, dxt, 0);
       else if (nz > 1)
@@ -1035,12 +1051,12 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
     if (a.dw) {
       GemmDesc g = head_gemm(n, d, T, dz, p.ldz, false, xc, d, false);
       char* out = static_cast<char*>(a.dw) + (size_t)v0 * a.lddw * (dwt == BF16 ? 2 : 4);
-      bool large;
-      const int nz = head_splits<false, false>(n, d, T, bf, p.split_elems, large, g.ksplit);
+      int tile;
+      const int nz = head_splits<false, false>(n, d, T, bf, p.split_elems, tile, g.ksplit);
       OutEpi e = {out, a.lddw, dwt, a.scale, most, a.accumulate, 0};
       if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, (int64_t)n * d};
-      if (bf) ZL_TRY((run_head<false, false>(g, e, large, s, nz)));
-      else ZL_TRY((run_head_f32<false, false>(g, e, s, nz)));
+      if (bf) ZL_TRY((run_head<false, false>(g, e, tile, s, nz)));
+      else ZL_TRY((run_head_f32<false, false>(g, e, tile, s, nz)));
       if (nz > 1) finish(n, split, nz, a.scale, most, out, a.lddw, dwt, a.accumulate);
     }
   }

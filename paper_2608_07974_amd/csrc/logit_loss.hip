@@ -435,17 +435,19 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
 }
 
 // --------------------------------------------------------------- top logits
-// 1. The row streams by once; the largest values of 1024 strands of it (a strand:
-//    half of every group of one thread) go to LDS.  The (k + 1)-th largest of
-//    them, cut to 16 bits, is a bound: at least k + 1 columns reach it, and with
-//    columns in no special order few more do.
-// 2. The row streams by again (mostly out of the caches): columns that reach the
-//    bound are listed, the others go into the rest's sum.
-// 3. The list is ordered by rank: keys are distinct (value, then lower column first).
-// Where the list overflows (many equal values), or there is a NaN, a radix search by 8 bits finds the
-// (k + 1)-th largest exactly and a last pass lists what is above it and, in order of
-// the columns, what equals it.
-constexpr int TT = 512, TOP_CAP = 1024;
+// The row streams by once, TOP_U groups a thread and round.
+//  1. Of the first round's columns the largest of 256 or 1024 strands go to LDS.  The
+//     (k + 1)-th largest of them, cut to 16 bits, is a bound: at least k + 1 columns reach
+//     it, and with columns in no special order few more do.
+//  2. Columns that reach the bound are listed in LDS, the others go into the rest's sum
+//     (relative to the bound, so that nothing overflows).  Between rounds a list of twice
+//     the length wanted is cut at its own (k + 1)-th largest, the new bound.
+//  3. The list is ordered by rank: keys are distinct (value, then lower column first).
+// Where the list overflows (many equal values, ascending rows), or there is a NaN, a
+// radix search by 8 bits finds the (k + 1)-th largest exactly and a last pass lists what
+// is above it and, in order of the columns, what equals it.
+// Two passes over memory for bound and list took 172 us of 2048 x 128256 bf16.
+constexpr int TOP_U = 8;
 
 // Order of floats as unsigned numbers; -0 as 0, every NaN above all numbers.
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -457,89 +459,195 @@ __device__ __forceinline__ float value_of(uint32_t o) {
   return __builtin_bit_cast(float, o == 0xffffffffu ? 0x7fc00000u : o >> 31 ? o & 0x7fffffffu : ~o);
 }
 
-template <bool BF>
-__global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, int64_t ldx, int k, float inv,
+// The largest number, down to bit `last`, that `want` of n keys reach (key lane + 64 i of a
+// lane in s[i], 0 past the n-th); one wave.
+template <int R>
+__device__ __forceinline__ uint32_t reached_by(uint32_t want, int last, uint32_t n, const uint32_t (&s)[R]) {
+  uint32_t b = 0;
+#pragma unroll 1
+  for (int bit = 31; bit >= last; --bit) {
+    const uint32_t c = b | (1u << bit);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (64u * i < n) m += __popcll(__ballot(s[i] >= c));
+    if (m >= want) b = c;
+    if (m == want) break;
+  }
+  return b;
+}
+
+// STRANDS: 256 up to k = 64, which shorten the search (four keys a lane), else 1024.
+template <bool BF, int NT, int STRANDS>
+__global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, int64_t ldx, int k, float inv,
                                                         int32_t* ids, float* values, float* rest) {
-  constexpr int W = Row<BF>::W;
-  __shared__ uint32_t strands[2 * TT];
-  __shared__ unsigned long long list[TOP_CAP];
-  __shared__ float red[TT / 64];
+  constexpr int W = Row<BF>::W, PER = STRANDS > NT ? STRANDS / NT : 1, JOIN = NT > STRANDS ? NT / STRANDS : 1;
+  constexpr int CAP = STRANDS == 256 ? 512 : 1024;
+  constexpr int MINE = (CAP + NT - 1) / NT;
+  static_assert(W % PER == 0, "whole strands a group");
+  __shared__ uint32_t strands[CAP];
+  __shared__ unsigned long long list[CAP];
+  __shared__ float red[NT / 64];
   __shared__ uint32_t bound_s, count_s, hist[256];
-  __shared__ int scan[TT / 64];
+  __shared__ int scan[NT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
   const Row<BF> z(x, row * ldx, V);
   const uint32_t want = (uint32_t)min(k + 1, V);
   const float c2 = inv * LOG2E;
 
-  float m0 = -INFINITY, m1 = -INFINITY;
-  z.template each<TT, 4>([&](int, float (&v)[W]) __attribute__((always_inline)) {
+  // groups z.full0 + tid + (at + u) NT; past the row: -inf
+  u32x4_t raw[TOP_U];
+  constexpr uint32_t NONE = BF ? 0xff80ff80u : 0xff800000u;
+  auto load = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < W / 2; ++e) {
-      m0 = fmaxf(m0, v[e]);
-      m1 = fmaxf(m1, v[W / 2 + e]);
+    for (int u = 0; u < TOP_U; ++u) {
+      const int g = z.full0 + tid + (at + u) * NT;
+      raw[u] = u32x4_t{NONE, NONE, NONE, NONE};
+      if (g < z.full1) raw[u] = z.load(g);
     }
-  });
-  strands[tid] = order_of(m0);
-  strands[TT + tid] = order_of(m1);
+  };
+  load(0);
+  {
+    float m[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) m[i] = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < TOP_U; ++u) {
+      float v[W];
+      z.get(raw[u], v);
+#pragma unroll
+      for (int e = 0; e < W; ++e) m[e / (W / PER)] = fmaxf(m[e / (W / PER)], v[e]);
+    }
+    if constexpr (JOIN > 1) {
+#pragma unroll
+      for (int o = 1; o < JOIN; o <<= 1) m[0] = fmaxf(m[0], __shfl_xor(m[0], o, 64));
+      if (lane % JOIN == 0) strands[tid / JOIN] = order_of(m[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) strands[tid + NT * i] = order_of(m[i]);
+    }
+  }
   if (tid == 0) count_s = 0;
   __syncthreads();
   if (wave == 0) {
-    // the largest bound of 16 bits that `want` strands reach
-    uint32_t s[2 * TT / 64];
+    uint32_t s[STRANDS / 64];
 #pragma unroll
-    for (int i = 0; i < 2 * TT / 64; ++i) s[i] = strands[i * 64 + lane];
-    uint32_t b = 0;
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t c = b | (1u << bit);
-      uint32_t n = 0;
-#pragma unroll
-      for (int i = 0; i < 2 * TT / 64; ++i) n += __popcll(__ballot(s[i] >= c));
-      if (n >= want) b = c;
-    }
-    if (lane == 0) bound_s = b;
+    for (int i = 0; i < STRANDS / 64; ++i) s[i] = strands[i * 64 + lane];
+    const uint32_t c = reached_by(want, 16, STRANDS, s);
+    if (lane == 0) bound_s = c;
   }
   __syncthreads();
   uint32_t bound = bound_s;
   float sum = 0.f;  // of exp((x - ref) c) below the bound
   float ref = value_of(bound);
-  const bool all = !(ref > -INFINITY && ref < INFINITY);  // no bound among numbers
+  const bool all = !(ref > -INFINITY && ref < INFINITY);  // no bound among numbers: list what there is
+  float least = all ? -INFINITY : ref;
   if (all) ref = 0.f;
-  z.template each<TT, 4>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
-    // a group below the bound, most of them, costs its maximum and its exponentials
-    // (NaN passes here and shows in the sum)
-    if (all || max_of(v) >= ref) {
+  auto enter = [&](int c, float v) __attribute__((always_inline)) {
+    const uint32_t at = atomicAdd(&count_s, 1u);
+    if (at < CAP) list[at] = (unsigned long long)order_of(v) << 32 | (0xffffffffu - (uint32_t)c);
+  };
+  // A group: the few columns that reach the bound leave it (a NaN too; one that the
+  // maximum hides shows in the sum), the rest is summed.  Kept short: unrolled per
+  // column, the listing made the kernel too long for the instruction cache (132 us).
+  auto take = [&](int g, u32x4_t r) __attribute__((always_inline)) {
+    float v[W];
+    z.get(r, v);
+    uint32_t hits = 0;
+    if (!(max_of(v) < least)) {
 #pragma unroll
-      for (int e = 0; e < W; ++e) {
-        const int c = W * g - z.pad + e;
-        const uint32_t o = order_of(v[e]);
-        if (o >= bound) {
-          if (c >= 0 && c < V) {
-            const uint32_t at = atomicAdd(&count_s, 1u);
-            if (at < TOP_CAP) list[at] = (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)c);
-          }
-        } else {
-          sum += __builtin_amdgcn_exp2f((v[e] - ref) * c2);
+      for (int e = 0; e < W; ++e)
+        if (!(v[e] < least)) {
+          hits |= 1u << e;
+          v[e] = -INFINITY;
         }
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < W; ++e) sum += __builtin_amdgcn_exp2f((v[e] - ref) * c2);
     }
-  });
-  const bool nan = block_max<TT>(sum == sum ? 0.f : 1.f, red) > 0.f;
+#pragma unroll
+    for (int e = 0; e < W; ++e) sum += __builtin_amdgcn_exp2f((v[e] - ref) * c2);
+    while (hits) {
+      const int e = __builtin_ctz(hits);
+      hits &= hits - 1;
+      const int q = BF ? e >> 1 : e;
+      const uint32_t lo = q & 1 ? r[1] : r[0], hi = q & 1 ? r[3] : r[2], d = q & 2 ? hi : lo;
+      enter(W * g - z.pad + e, __builtin_bit_cast(float, BF ? (e & 1 ? d & 0xffff0000u : d << 16) : d));
+    }
+  };
+  // cuts the list of n entries at its want-th largest; false where that is no number
+  auto tighten = [&](uint32_t n) -> bool {
+    if (wave == 0) {
+      uint32_t s[CAP / 64];
+#pragma unroll
+      for (int i = 0; i < CAP / 64; ++i) {
+        s[i] = 0;
+        if (64u * i < n) s[i] = (uint32_t)(i * 64 + lane) < n ? (uint32_t)(list[i * 64 + lane] >> 32) : 0;
+      }
+      const uint32_t c = reached_by(want, 0, n, s);
+      if (lane == 0) bound_s = c;
+    }
+    unsigned long long mine[MINE];
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) mine[i] = (uint32_t)(tid + NT * i) < n ? list[tid + NT * i] : 0;
+    __syncthreads();
+    const float to = value_of(bound_s);
+    if (all || !(to > -INFINITY && to < INFINITY)) return false;
+    bound = bound_s;
+    if (tid == 0) count_s = 0;
+    __syncthreads();
+    sum *= __builtin_amdgcn_exp2f((ref - to) * c2);
+    ref = least = to;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      if (mine[i] == 0) continue;
+      const uint32_t o = (uint32_t)(mine[i] >> 32);
+      if (o >= bound) list[atomicAdd(&count_s, 1u)] = mine[i];
+      else sum += __builtin_amdgcn_exp2f((value_of(o) - ref) * c2);
+    }
+    return true;
+  };
+  const int rounds = (z.full1 - z.full0 + TOP_U * NT - 1) / (TOP_U * NT);
+  bool fits = true;
+  for (int r = 0; r < rounds && fits; ++r) {
+#pragma unroll
+    for (int u = 0; u < TOP_U; ++u) {
+      const int g = z.full0 + tid + (r * TOP_U + u) * NT;
+      if (g < z.full1) take(g, raw[u]);
+    }
+    if (r + 1 < rounds) load((r + 1) * TOP_U);
+    __syncthreads();
+    const uint32_t n = count_s;
+    __syncthreads();
+    if (n > CAP) fits = false;
+    else if (n > 2 * want + 32 && r + 1 < rounds) fits = tighten(n);
+  }
+  if (tid < 2 && z.cut(tid) >= 0) {
+    const int c0 = W * z.cut(tid) - z.pad;
+#pragma unroll 1
+    for (int c = max(c0, 0); c < min(c0 + W, V); ++c) {
+      const float v = z.at(c);
+      if (!(v < least)) enter(c, v);
+      else sum += __builtin_amdgcn_exp2f((v - ref) * c2);
+    }
+  }
+  const bool nan = block_max<NT>(sum == sum ? 0.f : 1.f, red) > 0.f;
   __syncthreads();
   uint32_t n = count_s;
+  __syncthreads();
+  if (n > CAP || nan) fits = false;
+  else if (fits && n > want + 64 && tighten(n)) {
+    __syncthreads();
+    n = count_s;
+  }
   float ties = 0.f;  // columns equal to the bound that are not listed
-  if (n > TOP_CAP || nan) {
+  if (!fits) {
     // the want-th largest, 8 bits at a time: `above` columns are larger
     uint32_t key = 0, above = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
       __syncthreads();
-      if (tid < 256) hist[tid] = 0;
+      for (int i = tid; i < 256; i += NT) hist[i] = 0;
       __syncthreads();
       const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-      z.template each<TT, 1>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
+      z.template each<NT, 1>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
           const int c = W * g - z.pad + e;
@@ -569,7 +677,7 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
     const uint32_t need = want - above;
     uint32_t seen = 0;  // equal columns before this step's
     const int groups = z.groups();
-    for (int g0 = 0; g0 < groups; g0 += TT) {
+    for (int g0 = 0; g0 < groups; g0 += NT) {
       const int g = g0 + tid;
       float v[W];
 #pragma unroll
@@ -601,7 +709,7 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
       if (lane == 63) scan[wave] = before;
       __syncthreads();
       uint32_t rank = seen + (uint32_t)(before - mine), all = 0;
-      for (int w = 0; w < TT / 64; ++w) {
+      for (int w = 0; w < NT / 64; ++w) {
         if (w < wave) rank += (uint32_t)scan[w];
         all += (uint32_t)scan[w];
       }
@@ -620,9 +728,10 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
   }
   // ranks; what is listed beyond k goes back to the rest, in order
   const uint32_t kk = (uint32_t)k;
-  for (uint32_t i = tid; i < n; i += TT) {
+  for (uint32_t i = tid; i < n; i += NT) {
     const unsigned long long me = list[i];
     uint32_t r = 0;
+#pragma unroll 8
     for (uint32_t j = 0; j < n; ++j) r += list[j] > me;
     const float v = value_of((uint32_t)(me >> 32));
     if (r < kk) {
@@ -633,7 +742,7 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
     }
   }
   if (!rest) return;
-  sum = block_sum<TT>(sum, red);
+  sum = block_sum<NT>(sum, red);
   if (tid < 64) {
     const float top = n > kk ? __builtin_bit_cast(float, strands[0]) : -INFINITY;  // the rest's largest
     float t = 0.f;
@@ -652,12 +761,31 @@ __global__ void __launch_bounds__(TT) top_logits_kernel(int V, const void* x, in
 hipError_t launch_top_logits(int64_t T, int V, const void* x, int64_t ldx, int dtype, int k, float temperature,
                              int32_t* ids, float* values, float* rest, hipStream_t s) {
   if (T == 0) return hipSuccess;
-  const dim3 g((unsigned)T), b(TT);
+  const dim3 g((unsigned)T);
   const float inv = 1.f / temperature;
-  if (dtype == BF16)
-    hipLaunchKernelGGL((top_logits_kernel<true>), g, b, 0, s, V, x, ldx, k, inv, ids, values, rest);
-  else
-    hipLaunchKernelGGL((top_logits_kernel<false>), g, b, 0, s, V, x, ldx, k, inv, ids, values, rest);
+  auto run = [&](auto bf) {
+    constexpr bool BF = decltype(bf)::value;
+    auto go = [&](auto nt, auto strands) {
+      constexpr int NT = decltype(nt)::value, S = decltype(strands)::value;
+      hipLaunchKernelGGL((top_logits_kernel<BF, NT, S>), g, dim3(NT), 0, s, V, x, ldx, k, inv, ids, values, rest);
+    };
+    using std::integral_constant;
+    const integral_constant<int, 256> few{};
+    const integral_constant<int, 1024> many{};
+    // 16 waves a row where long rows are few, a wave where rows are short
+    if (T <= 512 && V >= 8192) {
+      if (k <= 64) go(many, few);
+      else go(many, many);
+    } else if (k > 64) {
+      go(few, many);
+    } else if (V <= 256 * Row<BF>::W) {
+      go(integral_constant<int, 64>{}, few);
+    } else {
+      go(few, few);
+    }
+  };
+  if (dtype == BF16) run(std::true_type{});
+  else run(std::false_type{});
   return hipGetLastError();
 }
 
