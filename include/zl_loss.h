@@ -77,7 +77,7 @@ zl_status zl_logit_loss_backward(int64_t T, int V, const void* z, int64_t ldz, i
 /* --------------------------------------------------- loss of a readout head
  * The same loss of z = x w^T, x [T, d], w [V, d] (both ZL_BF16 or both ZL_F32; d a
  * multiple of 8, at most 65536; rows 16-byte aligned, strides multiples of 8 below
- * 2^21).  z is held in fp32 accumulators and never stored: the forward keeps partial sums
+ * 2^21; the forward T V at most 2^36).  z is held in fp32 accumulators and never stored: the forward keeps partial sums
  * of 64 columns and more, the backward forms z again, `columns` of the vocabulary
  * at a time, and from it dL/dz in x's type, which it multiplies on.
  *

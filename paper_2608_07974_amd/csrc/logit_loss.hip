@@ -18,6 +18,16 @@ __device__ __forceinline__ void store16(void* p, u32x4_t v) {
   else *static_cast<u32x4_t*>(p) = v;
 }
 
+// The largest of a group, two columns an instruction (fmaxf first quiets every operand,
+// an instruction each).  With a NaN among them the result is any of them or NaN.
+template <int N>
+__device__ __forceinline__ float max_of_group(const float (&v)[N]) {
+  float m = fmaxf(v[0], v[1]);
+#pragma unroll
+  for (int k = 2; k < N; k += 2) asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(m), "v"(v[k]), "v"(v[k + 1]));
+  return m;
+}
+
 // ------------------------------------------------------------ rows of logits
 // Columns in groups of W = 8 (fp32: 4), 16 bytes aligned from the first full group on,
 // wherever the row starts: group g holds columns W g - pad .. W g - pad + W - 1 as far as
@@ -555,7 +565,7 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
     float v[W];
     z.get(r, v);
     uint32_t hits = 0;
-    if (!(max_of(v) < least)) {
+    if (!(max_of_group(v) < least)) {
 #pragma unroll
       for (int e = 0; e < W; ++e)
         if (!(v[e] < least)) {

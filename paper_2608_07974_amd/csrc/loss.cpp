@@ -66,6 +66,7 @@ zl_status check_head(const zl_head_args* a, bool backward) {
   if (a->T && (a->ldx >= MAX_LD || a->ldw >= MAX_LD)) return unsupported("row strides of 2^21 and more");
   if (a->T && (!a->stats || !by(a->stats, 4))) return bad("stats missing or misaligned");
   if (!backward) {
+    if (a->T * a->V > (int64_t)1 << 36) return unsupported("T V above 2^36: take the rows in parts");
     if (a->T && (!a->loss || !by(a->loss, 4))) return bad("loss missing or misaligned");
   } else {
     if (!by(a->dloss, 4)) return bad("misaligned dloss");

@@ -282,6 +282,30 @@ def test_logit_loss_masked_logits(dt, rest):
     assert not _np(dz)[6:].any() and not _np(loss)[6:].any() and not _np(stats)[6:].any()
 
 
+@pytest.mark.parametrize("alpha", [0.0, 1.0])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
+def test_alpha_at_its_ends(alpha, tau):
+    """One term has weight 0, also in rows that have no other."""
+    rng = _rng("alpha", int(alpha), int(tau))
+    zd = _dev(rng.standard_normal((12, 300)) * 3)
+    z = _np(zd)
+    y, ids, values, r = _targets(rng, z, 6, True, True, tau)
+    kw = dict(labels=_i32(y), teacher=_teacher(ids, values, r), alpha=alpha, temperature=tau)
+    loss, stats = _L().logit_loss(zd, **kw)
+    dz = _L().logit_loss_bwd(zd, stats, **kw)
+    ref, _, rdz = ol.loss(z, y, ids, values, r, alpha, tau)
+    log = (300 / 256 + 200) * (1 + _mag(z, values, r, tau)) * U
+    _near(_np(loss), ref, 2 * tau * tau * log)
+    _near(_np(dz), rdz, _spread(z, y, ids, values, r, alpha, tau) * 2 * log[:, None])
+    w = _dev(np.eye(300, 304))  # logits are x's columns
+    x = torch.zeros(12, 304, device="cuda")
+    x[:, :300] = zd
+    hl, hs = _L().head_loss(x, w, **kw)
+    dx, _ = _L().head_loss_bwd(x, w, hs, **kw)
+    _near(_np(hl), ref, 2 * tau * tau * log)
+    _near(_np(dx)[:, :300], rdz, _spread(z, y, ids, values, r, alpha, tau) * 2 * log[:, None])
+
+
 def test_teacher_that_weighs_nothing_is_none():
     z = _dev(np.ones((3, 20)))
     ids, values = np.array([[1, 2]] * 3), np.array([[-np.inf, -np.inf], [1.0, -np.inf], [-np.inf, -np.inf]])
@@ -493,6 +517,64 @@ def test_head_loss_is_the_loss_of_its_logits():
         want, ws = _L().logit_loss(_dev(z), **kw)
         _near(_np(loss), _np(want), 1e-5)  # two sums of 300 terms: 2 (300 / 256 + 200) (1 + 8) u * 2.5 < 6e-4 at most
         _near(_np(stats[:, :4]), _np(ws), 1e-5)
+
+
+# ------------------------------------------------------------ large offsets
+def test_rows_beyond_32_bit_offsets():
+    """The last rows of 5 GB of logits give what they give alone."""
+    L = _L()
+    T, V = 20001, 130000
+    z = torch.empty(T, V, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, T, 2000):
+        z[i: i + 2000] = torch.randn(min(2000, T - i), V, device="cuda") * 2
+    y = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
+    top = L.top_logits(z, 5)
+    kw = dict(labels=y, teacher=top)
+    loss, stats = L.logit_loss(z, **kw)
+    tail = slice(T - 3, T)
+    part = dict(labels=y[tail], teacher=L.TopLogits(*[t[tail].contiguous() for t in top]))
+    alone = z[tail].clone()
+    for a, b in zip(L.top_logits(alone, 5), top):
+        assert torch.allclose(a, b[tail], rtol=0, atol=1e-5)  # (rows few or many are summed in other orders)
+    l2, s2 = L.logit_loss(alone, **part)
+    # two orders of 130000 positive terms: (130000 / 256 + 120) u of the log-sum each
+    assert torch.allclose(l2, loss[tail], rtol=0, atol=1e-3)
+    want = L.logit_loss_bwd(alone, s2, **part).float()
+    got = L.logit_loss_bwd(z, stats, out=z, **kw)[tail].float()
+    assert torch.allclose(got, want, rtol=2.0 ** -7, atol=1e-6)
+
+
+def test_head_beyond_32_bit_offsets():
+    """A weight of 5 GB and its gradient; a weight whose rows lie 4 MB apart."""
+    L = _L()
+    T, V, d = 4, 300000, 8192
+    w = torch.empty(V, d, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, V, 50000):
+        w[i: i + 50000] = torch.randn(50000, d, device="cuda") / 40
+    x = torch.randn(T, d, device="cuda").bfloat16()
+    y = _i32([V - 1, 5, V - 2, 100])
+    z = torch.cat([x.float() @ w[i: i + 50000].float().t() for i in range(0, V, 50000)], 1)
+    loss, stats = L.head_loss(x, w, y)
+    want, ws = L.logit_loss(z, y)
+    # logits of spread 2 to 8000 u sum |x w|, 1e-3
+    assert torch.allclose(loss, want, rtol=0, atol=5e-3)
+    dx, dw = L.head_loss_bwd(x, w, stats, y, need_dw=True)
+    dz = L.logit_loss_bwd(z, ws, y)
+    for v in (0, 5, 100, 262143, 262144, V - 2, V - 1):
+        ref = dz[:, v] @ x.float()
+        assert (dw[v].float() - ref).norm() <= 2e-2 * ref.norm() + 1e-8, v
+    ref = sum(dz[:, i: i + 50000] @ w[i: i + 50000].float() for i in range(0, V, 50000))
+    assert (dx.float() - ref).norm() <= 2e-2 * ref.norm()
+    del w, dw, z, dz
+    far = torch.zeros(600, (1 << 21) - 8, dtype=torch.bfloat16, device="cuda")[:, :64]
+    near = torch.randn(600, 64, device="cuda").bfloat16()
+    far.copy_(near)
+    x = torch.randn(40, 64, device="cuda").bfloat16()
+    y = torch.randint(0, 600, (40,), device="cuda", dtype=torch.int32)
+    a, b = L.head_loss(x, far, y), L.head_loss(x, near, y)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    p, q = L.head_loss_bwd(x, far, a[1], y, need_dw=True), L.head_loss_bwd(x, near, b[1], y, need_dw=True, columns=256)
+    assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1])
 
 
 # ------------------------------------------------------- as a program uses them

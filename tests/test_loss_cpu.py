@@ -118,6 +118,7 @@ def test_head_loss_limits():
                dict(ldw=1 << 21), dict(targets=_t(k=257))):
         _refused(UNS, zl.zl_head_loss, _head(**kw))
         _refused(UNS, zl.zl_head_loss_backward, _head(True, **kw))
+    assert "2^36" in _refused(UNS, zl.zl_head_loss, _head(T=1 << 20, V=(1 << 16) + 1))
     assert "accumulation" in _refused(UNS, zl.zl_head_loss_backward, _head(True, dw_dtype=zl.ZL_BF16))
     wide = dict(T=1 << 18, d=4096, ldx=4096, ldw=4096, lddx=4096, lddw=4096)
     assert "2^30" in _refused(UNS, zl.zl_head_loss_backward, _head(True, **wide))
