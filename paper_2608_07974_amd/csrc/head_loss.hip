@@ -516,25 +516,35 @@ __global__ void __launch_bounds__(256) head_named_kernel(int V, int d, zl_target
 // The teacher's distribution over a row's entries, a wave per row.
 struct WaveTeacher {
   static constexpr int PER = ZL_TARGETS_MAX_K / 64;
+  int32_t id[PER];
   float t[PER], p[PER];
   bool on, rest;
   float L, r, u;
-  __device__ __forceinline__ WaveTeacher(const zl_targets& q, int64_t row, const int32_t* id, int lane) {
+  // the row's entries on their way: ids as cleaned, values
+  __device__ __forceinline__ void load(const zl_targets& q, int64_t row, const int32_t* ids, int lane) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = lane + 64 * i;
+      id[i] = -1;
+      t[i] = 0.f;
+      if (e < q.k) {
+        id[i] = ids[e];
+        t[i] = q.values[row * q.k + e];
+      }
+    }
+    u = q.rest ? q.rest[row] : -INFINITY;
+  }
+  __device__ __forceinline__ void form(const zl_targets& q) {
     const float inv = 1.f / q.temperature;
     bool any = false, bad = false;
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int e = lane + 64 * i;
-      t[i] = -INFINITY;
-      if (e < q.k && id[e] >= 0) {
-        any = true;
-        t[i] = q.values[row * q.k + e] * inv;
-        bad |= t[i] != t[i];
-        m = fmaxf(m, t[i]);
-      }
+      t[i] = id[i] >= 0 ? t[i] * inv : -INFINITY;
+      any |= id[i] >= 0;
+      bad |= t[i] != t[i];
+      m = fmaxf(m, t[i]);
     }
-    u = q.rest ? q.rest[row] : -INFINITY;
     m = fmaxf(wave_max(m), u);
     on = __ballot(any) != 0 && (m != -INFINITY || __ballot(bad) != 0 || u != u);
     const float ref = m == -INFINITY ? 0.f : m;
@@ -563,6 +573,20 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
   const int r = threadIdx.x % R, st = threadIdx.x / R, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row0 = (int64_t)blockIdx.x * R;
   const float inv = t.ids ? 1.f / t.temperature : 1.f, c2 = inv * LOG2E;
+  // what the first row of every wave takes is on its way before the sums are joined
+  WaveTeacher w;
+  int32_t yl = -1;
+  float zl[WaveTeacher::PER] = {}, zy = 0.f;
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+    yl = row_label(t, V, row);
+    if (!t.ids) return;
+    const float* from = stats + row * (4 + t.k);
+    zy = from[3];
+    w.load(t, row, tid + row * (t.k + 1), lane);
+#pragma unroll
+    for (int j = 0; j < WaveTeacher::PER; ++j) zl[j] = lane + 64 * j < t.k ? from[4 + lane + 64 * j] : 0.f;
+  };
+  if (wave < R && row0 + wave < T) fetch(row0 + wave);
   LogSum x, y;
   if (row0 + r < T) {
 #pragma unroll 4
@@ -597,30 +621,24 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
       p.merge(pm, ps, LOG2E);
       q.merge(qm, qs, c2);
     }
-    const int32_t* id = tid + row * (t.k + 1);
+    if (i != wave) fetch(row);
     float* out = stats + row * (4 + t.k);
-    const int32_t yl = row_label(t, V, row);
     const bool label = yl >= 0;
-    float zy = 0.f;
-    if (!t.ids && label) zy = row_dot<BF>(d, x_, row * ldx, w_, yl * ldw, lane);
-    else if (label) zy = out[3];
+    if (!t.ids) zy = label ? row_dot<BF>(d, x_, row * ldx, w_, yl * ldw, lane) : 0.f;
     float total = 0.f, lt = 0.f, other = 0.f, l1 = 0.f;
     bool on = false;
     if (t.ids) {
-      const WaveTeacher w(t, row, id, lane);
+      w.form(t);
       on = w.on;
-      float z[WaveTeacher::PER], kl = 0.f;
+      float kl = 0.f;
       LogSum n;
 #pragma unroll
       for (int j = 0; j < WaveTeacher::PER; ++j) {
-        const int e = lane + 64 * j;
-        z[j] = 0.f;
-        if (e < t.k && id[e] >= 0) {
-          z[j] = out[4 + e];
-          n.raise(z[j], c2);
-          n.s += n.m == -INFINITY ? 0.f : expf((z[j] - n.m) * inv);
+        if (w.id[j] >= 0) {
+          n.raise(zl[j], c2);
+          n.s += n.m == -INFINITY ? 0.f : expf((zl[j] - n.m) * inv);
         }
-        if (w.p[j] > 0.f || w.p[j] != w.p[j]) kl += w.p[j] * (w.t[j] - z[j] * inv);
+        if (w.p[j] > 0.f || w.p[j] != w.p[j]) kl += w.p[j] * (w.t[j] - zl[j] * inv);
       }
       if (masked) {
         other = q.log(inv);
@@ -691,7 +709,9 @@ __global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, int V, zl_tar
   float ct = 0.f, lt = ls, inv = 1.f;
   bool named = false, on = false;
   if (t.ids) {
-    const WaveTeacher w(t, row, id, lane);
+    WaveTeacher w;
+    w.load(t, row, id, lane);
+    w.form(t);
     inv = 1.f / t.temperature;
     on = w.on;
     const float f = on ? b * t.temperature * up : 0.f;

@@ -156,19 +156,26 @@ __device__ __forceinline__ RowTargets row_targets(const LogitLossArgs& a, int64_
                                                   typename NamesOf<NT>::type& names, bool both, float* red) {
   RowTargets q;
   const int tid = threadIdx.x, k = a.t.k, V = a.V;
+  // every load is on its way before the first barrier
   q.y = a.t.labels ? a.t.labels[row] : -1;
-  q.label = q.y >= 0 && q.y < V;
-  q.zy = q.label ? z.at(q.y) : 0.f;
-  q.teacher = q.rest = q.here = false;
-  q.L = q.r = q.zi = q.p = 0.f;
-  q.t = -INFINITY;
   q.id = -1;
+  float value = 0.f;
+  if (tid < k) {
+    q.id = a.t.ids[row * k + tid];
+    value = a.t.values[row * k + tid];
+  }
+  const float u = a.t.ids && a.t.rest ? a.t.rest[row] : -INFINITY;
+  q.label = q.y >= 0 && q.y < V;
+  q.here = q.id >= 0 && q.id < V;
+  q.zy = q.label ? z.at(q.y) : 0.f;
+  q.zi = q.here ? z.at(q.id) : 0.f;
+  q.teacher = q.rest = false;
+  q.L = q.r = q.p = 0.f;
+  q.t = -INFINITY;
   if (!a.t.ids && !(both && q.label)) return q;
   names.template clear<NT>();
   __syncthreads();
   if (tid < k) {
-    q.id = a.t.ids[row * k + tid];
-    q.here = q.id >= 0 && q.id < V;
     names.id[tid] = q.here ? q.id : -1;
     if (q.here) names.add(tid, q.id, z.group_of(q.id));
   }
@@ -190,22 +197,17 @@ __device__ __forceinline__ RowTargets row_targets(const LogitLossArgs& a, int64_
   if (twice) {
     names.id[tid] = -1;
     q.here = false;
+    q.zi = 0.f;
   }
   if (named) names.id[k] = -1;
   if (a.t.ids) {
-    const float inv = 1.f / a.t.temperature;
-    if (q.here) {
-      q.t = a.t.values[row * k + tid] * inv;
-      q.zi = z.at(q.id);
-    }
-    const float u = a.t.rest ? a.t.rest[row] : -INFINITY;
-    const bool any = block_max<NT>(q.here ? 1.f : 0.f, red) > 0.f;
-    const float bad = block_sum<NT>(q.here && q.t != q.t ? 1.f : 0.f, red);  // max drops a NaN
-    const float m = fmaxf(block_max<NT>(q.t, red), u);
-    q.teacher = any && (m != -INFINITY || bad > 0.f || u != u);
+    if (q.here) q.t = value * (1.f / a.t.temperature);
+    // -inf: no id; +inf: also a NaN, which a maximum would drop
+    const float top = block_max<NT>(q.here ? (q.t != q.t ? INFINITY : fmaxf(q.t, -3.402823466e38f)) : -INFINITY, red);
+    const float ref = fmaxf(top, u) == -INFINITY ? 0.f : fmaxf(top, u);
+    const float s = block_sum<NT>(q.here ? expf(q.t - ref) : 0.f, red) + expf(u - ref);
+    q.teacher = top != -INFINITY && s != 0.f;
     if (q.teacher) {
-      const float ref = m == -INFINITY ? 0.f : m;
-      const float s = block_sum<NT>(q.here ? expf(q.t - ref) : 0.f, red) + expf(u - ref);
       q.L = ref + logf(s);
       q.rest = u != -INFINITY;
       q.r = q.rest ? expf(u - q.L) : 0.f;
@@ -236,6 +238,14 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
   constexpr int W = Row<BF>::W;
   const int64_t row = blockIdx.x;
   const Row<BF> z(a.z, row * a.ldz, a.V);
+  float first = -INFINITY;
+  if ((int)threadIdx.x < z.groups()) {
+    const int g = threadIdx.x;
+    float v[W];
+    if (g >= z.full0 && g < z.full1) z.get(z.load(g), v);
+    else z.get_cut(g, v);
+    first = max_of(v);
+  }
   const RowTargets q = row_targets<NT, BF>(a, row, z, names, false, red);
   if (!q.label && !q.teacher) {
     if (threadIdx.x == 0) {
@@ -257,14 +267,6 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
     }
   };
   LogSum s1, st;  // of z, of z / tau (EXP_ONE: st alone, at 1 / tau)
-  float first = -INFINITY;
-  if ((int)threadIdx.x < z.groups()) {
-    const int g = threadIdx.x;
-    float v[W];
-    if (g >= z.full0 && g < z.full1) z.get(z.load(g), v);
-    else z.get_cut(g, v);
-    first = max_of(v);
-  }
   float ref = block_max<NT>(first, red);
   if (!(fabsf(ref) < INFINITY)) ref = 0.f;
   s1.m = st.m = ref;
@@ -379,14 +381,14 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
         if (c0 + k >= 0 && c0 + k < z.V) Elem<E>::store(out, c0 + k, v[k]);
     }
   };
+  const float4 s = *reinterpret_cast<const float4*>(a.stats + 4 * row);
+  const float up = a.scale * (a.dloss ? a.dloss[row] : 1.f);
   const RowTargets q = row_targets<NT, BF>(a, row, z, names, true, red);
   if (!q.label && !q.teacher) {
     const float none[W] = {};
     for (int g = threadIdx.x; g < z.groups(); g += NT) put(g, none);
     return;
   }
-  const float4 s = *reinterpret_cast<const float4*>(a.stats + 4 * row);
-  const float up = a.scale * (a.dloss ? a.dloss[row] : 1.f);
   const float tau = a.t.ids ? a.t.temperature : 1.f, inv = 1.f / tau;
   float c1 = q.label ? a.a * up : 0.f, l1 = s.x;
   const float f = q.teacher ? a.b * tau * up : 0.f;
