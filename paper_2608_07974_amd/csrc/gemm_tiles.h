@@ -73,13 +73,13 @@ struct SoftPart { float m, s, e; };
 // Grouped (GROUP_M row panels) order, then remapped so that the blocks the
 // dispatcher places on one XCD (round-robin over 8) take a contiguous range
 // of the grouped order and share A/B panels in that XCD's L2.
-__device__ inline void tile_coords(int b, int nbm, int nbn, int& tm, int& tn) {
-  const int nb = nbm * nbn;
-  if (nb >= 64) {
-    const int per = nb / 8, rem = nb % 8;
-    const int x = b % 8, idx = b / 8;
-    b = (x < rem ? x * (per + 1) : rem * (per + 1) + (x - rem) * per) + idx;
-  }
+// Block b of nb in that order: a contiguous range of them per XCD.
+__device__ inline int xcd_order(int b, int nb) {
+  const int per = nb / 8, rem = nb % 8;
+  const int x = b % 8, idx = b / 8;
+  return (x < rem ? x * (per + 1) : rem * (per + 1) + (x - rem) * per) + idx;
+}
+__device__ inline void grouped_coords(int b, int nbm, int nbn, int& tm, int& tn) {
 #ifndef GEMM_GROUP_M  // 4 measured best in the 8B update (2, 6, 8 and 16 slower)
 #define GEMM_GROUP_M 4
 #endif
@@ -90,6 +90,10 @@ __device__ inline void tile_coords(int b, int nbm, int nbn, int& tm, int& tn) {
   const int in_group = b % (GROUP_M * nbn);
   tm = first_m + in_group % gsz;
   tn = in_group / gsz;
+}
+__device__ inline void tile_coords(int b, int nbm, int nbn, int& tm, int& tn) {
+  const int nb = nbm * nbn;
+  grouped_coords(nb >= 64 ? xcd_order(b, nb) : b, nbm, nbn, tm, tn);
 }
 
 // Epilogue through LDS, one 32-row block of every wave tile at a time: the
@@ -865,12 +869,12 @@ __device__ inline void wait_vmcnt() {
 template <typename E> struct EpiTransposed { static constexpr bool value = false; };
 
 // NST-stage pipeline: the tile NST - 1 steps ahead is in flight while the
-// current one is multiplied; one barrier per BK-deep tile.  bl is the
-// block's index among the tiles of its problem.
+// current one is multiplied; one barrier per BK-deep tile.  (tm, tn): the
+// block's tile; kz: its split of K.
 template <int BM, int BN, int WM, int WN, int BK, int NST, int DS, bool AK, bool BKM, bool RA, bool RB, int MF,
           typename E>
-__device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const E& e, const int bl,
-                                              unsigned char* smem) {
+__device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const E& e, const int tm, const int tn,
+                                              const int kz, unsigned char* smem) {
   constexpr int NT = WM * WN * 64;
   constexpr int TM = BM / WM, TN = BN / WN;
   using M = Mma<MF>;
@@ -891,15 +895,12 @@ __device__ __forceinline__ void gemm_dma_body(const GemmDesc& g, const E& e, con
   static_assert(MF == 16 || NS % 2 == 0, "slice parity must repeat per tile");
   static_assert(MF == 32 || GEMM_IL, "16x16 fragments use the interleaved schedule");
 
-  const int nbm = (g.M + BM - 1) / BM, nbn = (g.N + BN - 1) / BN;
-  int tm, tn;
-  tile_coords(bl, nbm, nbn, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wm = wave / WN, wn = wave % WN;
 
   // split K: this block's range [kbeg, kbeg + ksplit) of the reduction
-  const int kz = blockIdx.z, kbeg = kz * g.ksplit;
+  const int kbeg = kz * g.ksplit;
   const int klen = min(g.K - kbeg, g.ksplit);
   const int ka = min(g.ka - kbeg, g.ksplit), kb = min(g.kb - kbeg, g.ksplit);
   const bf16_t* A = reinterpret_cast<const bf16_t*>(g.A) + (AK ? kbeg : (int64_t)kbeg * g.lda);
@@ -1108,10 +1109,14 @@ template <int BM, int BN, int WM, int WN, int BK, int NST, int DS, bool AK, bool
 __global__ void __launch_bounds__(WM * WN * 64)
 gemm_dma_kernel(GemmDesc g, EpiArgs e, GemmDesc g2, EpiArgs e2, int nb1) {
   extern __shared__ __align__(16) unsigned char smem[];
-  if (!PAIR || (int)blockIdx.x < nb1)
-    gemm_dma_body<BM, BN, WM, WN, BK, NST, DS, AK, BKM, RA, RB, MF>(g, e, blockIdx.x, smem);
-  else if constexpr (PAIR)
-    gemm_dma_body<BM, BN, WM, WN, BK, NST, DS, AK, BKM, RA, RB, MF>(g2, e2, blockIdx.x - nb1, smem);
+  int tm, tn;
+  if (!PAIR || (int)blockIdx.x < nb1) {
+    tile_coords(blockIdx.x, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN, tm, tn);
+    gemm_dma_body<BM, BN, WM, WN, BK, NST, DS, AK, BKM, RA, RB, MF>(g, e, tm, tn, blockIdx.z, smem);
+  } else if constexpr (PAIR) {
+    tile_coords(blockIdx.x - nb1, (g2.M + BM - 1) / BM, (g2.N + BN - 1) / BN, tm, tn);
+    gemm_dma_body<BM, BN, WM, WN, BK, NST, DS, AK, BKM, RA, RB, MF>(g2, e2, tm, tn, blockIdx.z, smem);
+  }
 }
 
 // ------------------------------------------------------------------ launch

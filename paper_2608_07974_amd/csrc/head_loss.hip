@@ -55,6 +55,12 @@ struct OutEpi {
   int accumulate;
   int64_t zstride;
 };
+// The epilogue of split z of K.
+template <typename E> __device__ __forceinline__ E split_part(const E& e, int) { return e; }
+__device__ __forceinline__ OutEpi split_part(OutEpi e, int z) {
+  e.out = static_cast<float*>(e.out) + z * e.zstride;
+  return e;
+}
 template <bool PAIR> struct EpiTransposed<StatEpi<PAIR>> { static constexpr bool value = true; };
 template <int MODE> struct EpiTransposed<GradEpi<MODE>> { static constexpr bool value = true; };
 template <> struct EpiTransposed<OutEpi> { static constexpr bool value = true; };
@@ -242,7 +248,7 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
         if (e.dtype == BF16) {
           rows.put(n - nb, make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)));
         } else if (m < g.M && n < g.N) {  // N is a multiple of 8: four columns are all there or none
-          float4* o = reinterpret_cast<float4*>(static_cast<float*>(e.out) + blockIdx.z * e.zstride + m * e.ldo + n);
+          float4* o = reinterpret_cast<float4*>(static_cast<float*>(e.out) + m * e.ldo + n);
           if (e.accumulate) {
             const float4 f = *o;
             v.x += f.x;
@@ -263,9 +269,20 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
 
 // ------------------------------------------------------------------ products
 template <int BM, int BN, int WM, int WN, int BK, int NST, bool AK, bool BKM, int MF, typename E>
-__global__ void __launch_bounds__(WM * WN * 64) head_gemm_kernel(GemmDesc g, E e) {
+__global__ void __launch_bounds__(WM * WN * 64) head_gemm_kernel(GemmDesc g, E e, int nz) {
   extern __shared__ __align__(16) unsigned char smem[];
-  gemm_dma_body<BM, BN, WM, WN, BK, NST, 1, AK, BKM, false, false, MF>(g, e, blockIdx.x, smem);
+  const int nbm = (g.M + BM - 1) / BM, nbn = (g.N + BN - 1) / BN;
+  int tm, tn, z = 0, at = blockIdx.x;
+  if (nz == 1) {
+    tile_coords(at, nbm, nbn, tm, tn);
+  } else {
+    // tiles of one split of K side by side on an XCD, which reads their operands once
+    // (dx of 4096 x 50257 x 768, 48 tiles in 5 splits: 298 us in the grid's order)
+    at = xcd_order(at, nbm * nbn * nz);
+    z = at / (nbm * nbn);
+    grouped_coords(at - z * nbm * nbn, nbm, nbn, tm, tn);
+  }
+  gemm_dma_body<BM, BN, WM, WN, BK, NST, 1, AK, BKM, false, false, MF>(g, split_part(e, z), tm, tn, z, smem);
 }
 
 template <int BM, int BN, int WM, int WN, bool AK, bool BKM, typename E>
@@ -280,7 +297,7 @@ static hipError_t run_head_tiles(const GemmDesc& g, const E& e, int nz, hipStrea
     if (err != hipSuccess) return err;
   }
   const int nb = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
-  hipLaunchKernelGGL(kern, dim3(nb, 1, nz), dim3(WM * WN * 64), lds, s, g, e);
+  hipLaunchKernelGGL(kern, dim3(nb * nz), dim3(WM * WN * 64), lds, s, g, e, nz);
   return hipGetLastError();
 }
 template <bool AK, bool BKM, typename E>
@@ -388,7 +405,7 @@ __global__ void __launch_bounds__(256) head_f32_kernel(GemmDesc g, E e) {
     }
   }
   __syncthreads();
-  store_tile<BM, BN, WM, WN, 32>(acc, reinterpret_cast<unsigned char*>(lds), g, e, m0, n0, wave, lane);
+  store_tile<BM, BN, WM, WN, 32>(acc, reinterpret_cast<unsigned char*>(lds), g, split_part(e, blockIdx.z), m0, n0, wave, lane);
 }
 template <int BM, int BN, int WM, int WN, bool AK, bool BKM, typename E>
 static hipError_t run_f32_tiles(const GemmDesc& g, const E& e, hipStream_t s, int nz) {
