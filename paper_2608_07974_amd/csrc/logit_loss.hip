@@ -453,7 +453,9 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
 //     it, and with columns in no special order few more do.
 //  2. Columns that reach the bound are listed in LDS, the others go into the rest's sum
 //     (relative to the bound, so that nothing overflows).  Between rounds a list of twice
-//     the length wanted is cut at its own (k + 1)-th largest, the new bound.
+//     the length wanted is cut at its own (k + 1)-th largest, the new bound.  What is cut
+//     off adds to the rest in units of 2^-40 of the bound's term (the rest holds that
+//     term): sums of integers, which do not depend on the order of the list.
 //  3. The list is ordered by rank: keys are distinct (value, then lower column first).
 // Where the list overflows (many equal values, ascending rows), or there is a NaN, a
 // radix search by 8 bits finds the (k + 1)-th largest exactly and a last pass lists what
@@ -501,6 +503,7 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
   __shared__ unsigned long long list[CAP];
   __shared__ float red[NT / 64];
   __shared__ uint32_t bound_s, count_s, hist[256];
+  __shared__ unsigned long long cut_s;  // terms cut off the list
   __shared__ int scan[NT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
@@ -540,7 +543,10 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
       for (int i = 0; i < PER; ++i) strands[tid + NT * i] = order_of(m[i]);
     }
   }
-  if (tid == 0) count_s = 0;
+  if (tid == 0) {
+    count_s = 0;
+    cut_s = 0;
+  }
   __syncthreads();
   if (wave == 0) {
     uint32_t s[STRANDS / 64];
@@ -604,17 +610,23 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
     const float to = value_of(bound_s);
     if (all || !(to > -INFINITY && to < INFINITY)) return false;
     bound = bound_s;
-    if (tid == 0) count_s = 0;
+    if (tid == 0) {
+      sum += (float)cut_s * 0x1p-40f;
+      count_s = 0;
+      cut_s = 0;
+    }
     __syncthreads();
     sum *= __builtin_amdgcn_exp2f((ref - to) * c2);
     ref = least = to;
+    unsigned long long cut = 0;
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
       if (mine[i] == 0) continue;
       const uint32_t o = (uint32_t)(mine[i] >> 32);
       if (o >= bound) list[atomicAdd(&count_s, 1u)] = mine[i];
-      else sum += __builtin_amdgcn_exp2f((value_of(o) - ref) * c2);
+      else cut += (unsigned long long)(__builtin_amdgcn_exp2f((value_of(o) - ref) * c2) * 0x1p40f);
     }
+    if (cut) atomicAdd(&cut_s, cut);
     return true;
   };
   const int rounds = (z.full1 - z.full0 + TOP_U * NT - 1) / (TOP_U * NT);
@@ -754,6 +766,7 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
     }
   }
   if (!rest) return;
+  if (fits && tid == 0) sum += (float)cut_s * 0x1p-40f;
   sum = block_sum<NT>(sum, red);
   if (tid < 64) {
     const float top = n > kk ? __builtin_bit_cast(float, strands[0]) : -INFINITY;  // the rest's largest

@@ -403,6 +403,23 @@ def test_top_logits_one_strand():
     _check_top(_dev(np.arange(30000, dtype=np.float64)[None]), 200)
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("k", [5, 64, 256])
+@pytest.mark.parametrize("T", [64, 600])
+def test_top_logits_repeatable(T, k, dt):
+    # rising rows, whose list is cut many times, and plain ones
+    L = _L()
+    g = torch.Generator(device="cuda").manual_seed(T + k)
+    z = torch.randn(T, 40003, generator=g, device="cuda")
+    z[::2] += torch.linspace(0, 8, 40003, device="cuda")
+    z = z.to(_dt(dt))
+    a = L.top_logits(z, k, temperature=2.0)
+    for _ in range(10):
+        b = L.top_logits(z, k, temperature=2.0)
+        assert torch.equal(a.ids, b.ids) and torch.equal(a.values, b.values)
+        assert torch.equal(a.rest, b.rest)
+
+
 def test_top_logits_without_rest():
     x = _dev(_rng("norest").standard_normal((3, 500)))
     a, b = _L().top_logits(x, 7, rest=False), _L().top_logits(x, 7)
