@@ -24,7 +24,7 @@ extern "C" {
 
 /* ------------------------------------------------------------- the targets
  * Row t has logits z (V of them) and adds
- *   loss = a CE + b tau^2 KL,   tau = temperature > 0,
+ *   loss = a CE + b tau^2 KL,   tau = temperature, 2^-60 to 2^60,
  * a = alpha, b = 1 - alpha with labels and a teacher, else 1 for the one there is.
  *
  * Label y:  CE = log sum_v exp(z_v) - z_y.  A label outside [0, V) is none.
@@ -48,7 +48,7 @@ typedef struct zl_targets {
   const float* rest;      /* [T] or NULL                                       */
   int k;                  /* 1 .. ZL_TARGETS_MAX_K with ids, else 0            */
   float alpha;            /* in [0, 1]                                         */
-  float temperature;      /* > 0                                               */
+  float temperature;      /* in [2^-60, 2^60]                                  */
 } zl_targets;
 
 /* -------------------------------------------------------------- top logits
@@ -56,7 +56,8 @@ typedef struct zl_targets {
  * alignment) the k largest: ids and values [T, k], in descending order, equal
  * ones by ascending column (-0 equals 0).  A NaN counts as larger than any
  * number.  rest [T] (or NULL): log of the sum of exp(x / temperature) over the
- * other columns; -inf where there are none.  1 <= k <= V, k <= 256. */
+ * other columns; -inf where there are none.  1 <= k <= V, k <= 256; temperature
+ * in [2^-60, 2^60]. */
 zl_status zl_top_logits(int64_t T, int V, const void* x, int64_t ldx, int dtype, int k, float temperature,
                         int32_t* ids, float* values, float* rest, void* stream);
 
@@ -77,9 +78,11 @@ zl_status zl_logit_loss_backward(int64_t T, int V, const void* z, int64_t ldz, i
 /* --------------------------------------------------- loss of a readout head
  * The same loss of z = x w^T, x [T, d], w [V, d] (both ZL_BF16 or both ZL_F32; d a
  * multiple of 8, at most 65536; rows 16-byte aligned, strides multiples of 8 below
- * 2^21; the forward T V at most 2^36).  z is held in fp32 accumulators and never stored: the forward keeps partial sums
- * of 64 columns and more, the backward forms z again, `columns` of the vocabulary
- * at a time, and from it dL/dz in x's type, which it multiplies on.
+ * 2^21; the forward T V at most 2^36).  z is held in fp32 accumulators and never
+ * stored: the forward keeps partial sums of 32 to 128 columns, the backward forms z
+ * again, `columns` of the vocabulary at a time, and from it dL/dz in x's type, which
+ * it multiplies on.  With ZL_BF16 log2(e) z and log2(e) z / tau have to be numbers of
+ * fp32 (|z| up to 2^127, which products of finite weights and inputs stay far below).
  *
  * stats [T, 4 + k], contiguous: as above, then z at the teacher's ids (0 where
  * absent).

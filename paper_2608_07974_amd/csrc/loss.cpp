@@ -25,6 +25,8 @@ zl_status done(hipError_t e, const char* what) {
 
 bool dtype_ok(int dt) { return dt == ZL_F32 || dt == ZL_BF16; }
 int dt_of(int dt) { return dt == ZL_BF16 ? BF16 : F32; }
+// log2(e) / tau and tau^2 have to be numbers of fp32: times a difference of 0 they are 0 then.
+bool temperature_ok(float tau) { return tau >= 0x1p-60f && tau <= 0x1p60f; }
 bool by(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 zl_status check_sizes(int64_t T, int V) {
@@ -48,8 +50,7 @@ zl_status check_targets(const zl_targets& t, int64_t T) {
   if (t.k > ZL_TARGETS_MAX_K) return unsupported("more than 256 ids per row");
   if (T && (soft != (t.values != nullptr) || (t.rest && !soft))) return bad("ids and values go together, rest with both");
   if (!(t.alpha >= 0.f && t.alpha <= 1.f)) return bad("alpha must be in [0, 1]");
-  if (!(t.temperature > 0.f) || !isfinite(t.temperature)) return bad("temperature must be > 0");
-  if (!(1.f / t.temperature > 0.f) || !isfinite(1.f / t.temperature)) return bad("temperature must have a finite inverse");
+  if (!temperature_ok(t.temperature)) return bad("temperature must be in [2^-60, 2^60]");
   if (!by(t.labels, 4) || !by(t.ids, 4) || !by(t.values, 4) || !by(t.rest, 4)) return bad("misaligned targets");
   return ZL_OK;
 }
@@ -99,7 +100,7 @@ zl_status zl_top_logits(int64_t T, int V, const void* x, int64_t ldx, int dtype,
   if (!dtype_ok(dtype)) return bad("bad dtype");
   if (k < 1 || k > V) return bad("k must be 1 .. V");
   if (k > TOP_MAX_K) return unsupported("k above 256");
-  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return bad("temperature must be > 0");
+  if (!temperature_ok(temperature)) return bad("temperature must be in [2^-60, 2^60]");
   if (!logits_ok(x, ldx, V, dtype, T)) return bad("logits missing, misaligned, or a row stride below V");
   if (T && (!ids || !values)) return bad("ids or values missing");
   if (!by(ids, 4) || !by(values, 4) || !by(rest, 4)) return bad("misaligned output");

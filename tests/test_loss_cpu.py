@@ -62,6 +62,17 @@ def test_targets_refused(kw):
     _refused(INV, zl.zl_head_loss_backward, _head(True, targets=t))
 
 
+@pytest.mark.parametrize("tau", [2.0 ** -61, 4e-39, 2.0 ** 61, 1e38])
+def test_temperatures_refused(tau):
+    # log2(e) / tau or tau^2 leaves fp32
+    t = _t(temperature=tau)
+    for said in (_refused(INV, zl.zl_top_logits, 4, 100, A, 100, zl.ZL_F32, 8, tau, A, A, A),
+                 _refused(INV, zl.zl_logit_loss, 4, 100, A, 100, zl.ZL_F32, t, A, A),
+                 _refused(INV, zl.zl_logit_loss_backward, 4, 100, A, 100, zl.ZL_F32, t, A, A, 1.0, A, 100),
+                 _refused(INV, zl.zl_head_loss, _head(targets=t)), _refused(INV, zl.zl_head_loss_backward, _head(True, targets=t))):
+        assert "temperature" in said
+
+
 @pytest.mark.parametrize("kw", [dict(T=-1), dict(V=0), dict(z=0), dict(z=A + 2), dict(ld=99), dict(dtype=7), dict(loss=0),
                                 dict(stats=0), dict(stats=A + 8), dict(loss=A + 2)])
 def test_logit_loss_refuses(kw):
