@@ -34,8 +34,7 @@ struct StatEpi {
 //   GRAD_ONE   ct exp(z / tau - lt)
 //   GRAD_TWO   c1 exp(z - l1) + ct exp(z / tau - lt)
 //   GRAD_SQUARE  the same at tau = 2, where with e = exp(z / 2 - lt) the first term is
-//     c1 exp(2 lt - l1) e^2 (c1 holds the product): one exponential for two, 16 of the
-//     44 cycles that a wave spends per element
+//     c1 exp(2 lt - l1) e^2 (c1 holds the product): one exponential for two
 enum { GRAD_ONE, GRAD_TWO, GRAD_SQUARE };
 template <int MODE>
 struct GradEpi {
@@ -75,7 +74,7 @@ __device__ __forceinline__ float across(float x, F&& f) {
 
 // bf16 results of MF rows of a wave's tile, four columns a lane, leave through LDS as
 // rows of 16 bytes a lane: straight from the accumulators a store would touch 16 or
-// 32 rows with 32 or 16 bytes each (dL/dz of 4096 x 50257 x 768: 419 us, 366 so).  The
+// 32 rows with 32 or 16 bytes each (dL/dz of 4096 x 50257 x 768: 437 us, 394 so).  The
 // region is the wave's own; its accesses to LDS stay in order.
 template <int TN, int MF>
 struct RowsOut {
@@ -268,6 +267,10 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
 }
 
 // ------------------------------------------------------------------ products
+// Bound by the matrix units: 4096 x 65536 at K 768 takes 395 us with sums (1040 TFLOP/s),
+// 500 with dL/dz, whose epilogue (6 us a tile of 256 x 256) hides behind nothing; at K 3200
+// 1231 and 1373 (1400 and 1250).  Blocks that stay and copy the next tile during the epilogue
+// gained 2 % at K 768 and lost 0.7 % at 4096.
 template <int BM, int BN, int WM, int WN, int BK, int NST, bool AK, bool BKM, int MF, typename E>
 __global__ void __launch_bounds__(WM * WN * 64) head_gemm_kernel(GemmDesc g, E e, int nz) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -277,7 +280,7 @@ __global__ void __launch_bounds__(WM * WN * 64) head_gemm_kernel(GemmDesc g, E e
     tile_coords(at, nbm, nbn, tm, tn);
   } else {
     // tiles of one split of K side by side on an XCD, which reads their operands once
-    // (dx of 4096 x 50257 x 768, 48 tiles in 5 splits: 298 us in the grid's order)
+    // (dx of 4096 x 50257 x 768, 48 tiles in 5 splits: 289 us, 298 in the grid's order)
     at = xcd_order(at, nbm * nbn * nz);
     z = at / (nbm * nbn);
     grouped_coords(at - z * nbm * nbn, nbm, nbn, tm, tn);
@@ -413,6 +416,8 @@ static hipError_t run_f32_tiles(const GemmDesc& g, const E& e, hipStream_t s, in
   hipLaunchKernelGGL((head_f32_kernel<BM, BN, WM, WN, AK, BKM, E>), dim3(nb, 1, nz), dim3(256), 0, s, g, e);
   return hipGetLastError();
 }
+// Bound by the matrix units: 4096 x 32000 x 1024 2105 us (128 TFLOP/s, the library's product
+// 139), one row 100 us (128256 x 1024, 5.2 TB/s).
 // Tiles by size: 32 rows where there are no more (of a product with K-major A: dw has a
 // row per column of the vocabulary); 64 x 64 where those of 128 x 128, with splits of 256 of
 // K at least where they may be, leave CUs idle (a matrix instruction takes 64 cycles: 64 of
