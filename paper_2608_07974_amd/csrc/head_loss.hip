@@ -1,9 +1,8 @@
 // Loss of a readout head z = x w^T without its logits (include/zl_loss.h).
 //
 // Forward: the product's tiles leave, per row and column block, the largest logit
-// and the sum of exponentials (the matrix unit's accumulators are the only place
-// where z exists); the few logits that the targets name are products of their own; a
-// kernel over the rows joins both.
+// and the sum of exponentials, and the logits of the teacher's ids (the matrix unit's
+// accumulators are the only place where z exists); a kernel over the rows joins them.
 // Backward, a piece of the vocabulary at a time: the product again, whose tiles
 // write dL/dz (bf16 or fp32); the named columns' values over it; two products from
 // there.
@@ -20,15 +19,29 @@ namespace zl {
 // row blocks, four consecutive columns at a time, so a row's sums need two steps
 // across lanes and its constants one load.
 
+// The teacher's distinct ids of every row, found again in the tiles: ids in ascending
+// order [T, k]; of every row and column block (a wave tile's columns) a span [T, ldb]: where
+// its ids begin (8 bits), the first one's column in the block (8), where they end (16; 0:
+// there are none); their logits [T, k], in that order.  k dot products
+// a row instead read k rows of w for each: 2117 x 1802 x 3824 bf16 with 60 ids took 150 us
+// for those.
+struct NamedCols {
+  const int32_t* order;
+  const uint32_t* span;  // null: no teacher
+  int64_t ldb;
+  float* z;
+  int k;
+};
 // Partial sums.  PAIR false: (max z, sum exp((z - max) c)).  PAIR true: those of
-// z at c = 1 over all columns and of z at c over the columns without a mask bit.
+// z at c = 1 over all columns and of z at c over all, or (other) the columns that the
+// teacher does not name.
 template <bool PAIR>
 struct StatEpi {
   float c2;               // log2(e) / tau
   float* part;            // [blocks, T, 2 or 4]
   int64_t T;
-  const uint32_t* mask;   // [T, ldm] or null
-  int64_t ldm;
+  NamedCols named;
+  bool other;
 };
 // dL/dz of the columns [0, N) of a piece, zeros up to the row stride:
 //   GRAD_ONE   ct exp(z / tau - lt)
@@ -72,6 +85,13 @@ __device__ __forceinline__ float across(float x, F&& f) {
   return x;
 }
 
+// A wave's own accesses to LDS stay in order; this keeps the compiler to it.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // bf16 results of MF rows of a wave's tile, four columns a lane, leave through LDS as
 // rows of 16 bytes a lane: straight from the accumulators a store would touch 16 or
 // 32 rows with 32 or 16 bytes each (dL/dz of 4096 x 50257 x 768: 437 us, 394 so).  The
@@ -89,18 +109,14 @@ struct RowsOut {
   // f(row, column, 8 values)
   template <typename F>
   __device__ __forceinline__ void flush(F&& f) {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    wave_sync();
     constexpr int LPR = TN / 8;
 #pragma unroll
     for (int it = 0; it < MF * LPR / 64; ++it) {
       const int r = it * (64 / LPR) + lane / LPR, c = lane % LPR * 8;
       f(r, c, *reinterpret_cast<const uint4*>(lds + r * LD + c));
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    wave_sync();
   }
 };
 
@@ -116,9 +132,16 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
   const int64_t block = nb / TN;
   auto fmax2 = [](float a, float b) { return fmaxf(a, b); };
   auto add2 = [](float a, float b) { return a + b; };
+  // on their way before the first sums
+  uint32_t span[FM];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int m = m0 + wm * TM + i * MF + (lane & (MF - 1));
+    span[i] = e.named.span && m < g.M ? e.named.span[m * e.named.ldb + block] : 0;
+  }
   static_for<0, FM>([&](auto ic) __attribute__((always_inline)) {
     constexpr int i = decltype(ic)::value;
-    const int m = m0 + wm * TM + i * MF + (lane & (MF - 1));
+    const int64_t m = m0 + wm * TM + i * MF + (lane & (MF - 1));
     float v[FN * NR];
 #pragma unroll
     for (int j = 0; j < FN; ++j)
@@ -138,23 +161,34 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
       for (int k = 0; k < FN * NR; ++k) s += __builtin_amdgcn_exp2f((v[k] - ref) * c2);
       s = across<MF>(s, add2);
     };
+    // a row's lanes look for the same column, one holds it
+    auto name = [&](bool out) __attribute__((always_inline)) {
+      const int end = span[i] >> 16, first = span[i] & 0xff;
+      for (int at = first; at < end; ++at) {
+        const int c = at == first ? (int)(span[i] >> 8 & 0xff) : e.named.order[m * e.named.k + at] - nb;
+        float z = 0.f;
+        bool here = false;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+            if (c == j * MF + Mma<MF>::row(lane, r)) {
+              z = v[j * NR + r];
+              here = true;
+              if (out) v[j * NR + r] = -INFINITY;
+            }
+        if (here) e.named.z[m * e.named.k + at] = z;
+      }
+    };
     float mx, s;
     if constexpr (!PAIR) {
       sums(e.c2, mx, s);
+      name(false);
       if (lane < MF && m < g.M) *reinterpret_cast<float2*>(e.part + (block * e.T + m) * 2) = make_float2(mx, s);
     } else {
       float mt, st;
       sums(LOG2E, mx, s);
-      if (e.mask && m < g.M) {
-        const uint32_t* w = e.mask + m * e.ldm + (nb >> 5);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const uint32_t bits = w[(j * MF) >> 5];
-#pragma unroll
-          for (int r = 0; r < NR; ++r)
-            if (bits >> ((j * MF & 31) + Mma<MF>::row(lane, r)) & 1) v[j * NR + r] = -INFINITY;
-        }
-      }
+      name(e.other);
       sums(e.c2, mt, st);
       if (lane < MF && m < g.M)
         *reinterpret_cast<float4*>(e.part + (block * e.T + m) * 4) = make_float4(mx, s, mt, st);
@@ -439,8 +473,8 @@ static hipError_t run_head_f32(const GemmDesc& g, const E& e, int tile, hipStrea
 }
 
 // --------------------------------------------------------------- target rows
-// The ids of a row, absent ones and repetitions as -1, into `ids` [256]: entries lane,
-// lane + 64, ... of every lane.  Whole waves, each a row of its own (or none).
+// The ids of a row, absent ones and repetitions as -1, into `ids` [256] (LDS of the wave's
+// own): entries lane, lane + 64, ... of every lane.
 __device__ __forceinline__ void row_ids(const zl_targets& t, int V, int64_t row, bool on, int lane, int32_t* ids,
                                         int32_t (&mine)[ZL_TARGETS_MAX_K / 64]) {
   constexpr int PER = ZL_TARGETS_MAX_K / 64;
@@ -454,21 +488,25 @@ __device__ __forceinline__ void row_ids(const zl_targets& t, int V, int64_t row,
     }
     ids[e] = mine[i];
   }
-  __syncthreads();
-  int32_t once[PER];
+  wave_sync();
+  bool twice[PER] = {};
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    once[i] = mine[i];
-    for (int f = 0; f < lane + 64 * i && once[i] >= 0; ++f)
-      if (ids[f] == once[i]) once[i] = -1;
+    const int e = lane + 64 * i;
+#pragma unroll 4
+    for (int f = 0; f < min(64 * (i + 1), t.k) && 64 * i < t.k; f += 4) {
+      const int4 o = *reinterpret_cast<const int4*>(ids + f);
+      twice[i] |= (o.x == mine[i] && f < e) || (o.y == mine[i] && f + 1 < e) || (o.z == mine[i] && f + 2 < e) ||
+                  (o.w == mine[i] && f + 3 < e);
+    }
   }
-  __syncthreads();
+  wave_sync();
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    mine[i] = once[i];
-    ids[lane + 64 * i] = once[i];
+    if (twice[i]) mine[i] = -1;
+    ids[lane + 64 * i] = mine[i];
   }
-  __syncthreads();
+  wave_sync();
 }
 __device__ __forceinline__ int32_t row_label(const zl_targets& t, int V, int64_t row) {
   const int32_t y = t.labels ? t.labels[row] : -1;
@@ -490,48 +528,58 @@ __device__ __forceinline__ float row_dot(int d, const void* x, int64_t ox, const
   return wave_sum(s);
 }
 
-// What the targets name of every row: ids to tid [T, k + 1] (absent ones and repetitions
-// as -1, then the label), their logits to stats (the label's column 3, id e's 4 + e),
-// with a mask a bit per named column.  A block per `per` entries of a row, four of
-// them at a time; the row's first block writes tid and the mask.
+// What the targets name of every row, two waves each.  The first: NamedCols' order and
+// spans, and the place of every entry in that order (slot [T, k], -1: absent or a
+// repetition); the second the label's logit (stats column 3).
 template <bool BF>
-__global__ void __launch_bounds__(256) head_named_kernel(int V, int d, zl_targets t, int per, const void* x, int64_t ldx,
-                                                         const void* w, int64_t ldw, int32_t* tid, float* stats,
-                                                         uint32_t* mask, int64_t ldm) {
-  __shared__ int32_t ids[4][ZL_TARGETS_MAX_K];
+__global__ void __launch_bounds__(128) head_named_kernel(int V, int d, zl_targets t, int width, const void* x, int64_t ldx,
+                                                         const void* w, int64_t ldw, float* stats, int32_t* slot,
+                                                         int32_t* order, uint32_t* span, int64_t ldb) {
+  constexpr int PER = ZL_TARGETS_MAX_K / 64;
+  __shared__ __align__(16) int32_t ids[ZL_TARGETS_MAX_K], sorted[ZL_TARGETS_MAX_K];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = t.k;
   const int64_t row = blockIdx.x;
-  int32_t mine[ZL_TARGETS_MAX_K / 64];
-  const bool first = blockIdx.y == 0;
-  // cleared and set by one wave, whose stores stay in order
-  if (first && mask && wave == 0)
-    for (int64_t i = lane * 4; i < ldm; i += 256) *reinterpret_cast<uint4*>(mask + row * ldm + i) = make_uint4(0, 0, 0, 0);
-  row_ids(t, V, row, true, lane, ids[wave], mine);  // ends with a barrier
-  const int32_t y = row_label(t, V, row);
-  if (first && wave == 0) {
+  span += row * ldb;
+  for (int64_t i = (int64_t)threadIdx.x * 4; i < ldb; i += 512)
+    *reinterpret_cast<uint4*>(span + i) = make_uint4(0, 0, 0, 0);
+  int n = 0;
+  if (wave == 0) {
+    int32_t mine[PER], at[PER];
+    row_ids(t, V, row, true, lane, ids, mine);
 #pragma unroll
-    for (int i = 0; i < ZL_TARGETS_MAX_K / 64; ++i) {
-      const int e = lane + 64 * i;
-      if (e >= k) continue;
-      tid[row * (k + 1) + e] = mine[i];
-      // a word of the mask is formed whole, by the first entry in it
-      uint32_t bits = 0;
-      bool lead = true;
-      for (int f = 0; f < k && mask && mine[i] >= 0; ++f) {
-        const int32_t o = ids[0][f];
-        if (o < 0 || o >> 5 != mine[i] >> 5) continue;
-        bits |= 1u << (o & 31);
-        lead &= f >= e;
+    for (int i = 0; i < PER; ++i) {
+      // how many distinct ids are smaller (-1 is the largest unsigned number)
+      at[i] = 0;
+#pragma unroll 4
+      for (int f = 0; f < k && 64 * i < k; f += 4) {
+        const uint4 o = *reinterpret_cast<const uint4*>(ids + f);
+        const uint32_t v = (uint32_t)mine[i];
+        at[i] += (o.x < v) + (o.y < v) + (o.z < v) + (o.w < v);
       }
-      if (mask && mine[i] >= 0 && lead) mask[row * ldm + (mine[i] >> 5)] = bits;
+      const bool on = mine[i] >= 0;
+      n += __popcll(__ballot(on));
+      if (on) {
+        sorted[at[i]] = mine[i];
+        order[row * k + at[i]] = mine[i];
+      }
+      if (lane + 64 * i < k) slot[row * k + lane + 64 * i] = on ? at[i] : -1;
     }
-    if (lane == 0) tid[row * (k + 1) + k] = y;
+  } else {
+    const int32_t y = row_label(t, V, row);
+    const float z = y >= 0 ? row_dot<BF>(d, x, row * ldx, w, y * ldw, lane) : 0.f;
+    if (lane == 0) stats[row * (4 + k) + 3] = z;
   }
-  const int e1 = min(k + 1, ((int)blockIdx.y + 1) * per);
-  for (int e = blockIdx.y * per + wave; e < e1; e += 4) {
-    const int32_t id = e == k ? y : ids[wave][e];
-    const float z = id >= 0 ? row_dot<BF>(d, x, row * ldx, w, id * ldw, lane) : 0.f;
-    if (lane == 0) stats[row * (4 + k) + (e == k ? 3 : 4 + e)] = z;
+  __syncthreads();  // the spans are cleared
+  if (wave == 0) {
+    uint16_t* ends = reinterpret_cast<uint16_t*>(span);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int r = lane + 64 * i;
+      if (r >= n) continue;
+      const int b = sorted[r] / width;
+      if (r == 0 || sorted[r - 1] / width != b) ends[2 * (int64_t)b] = (uint16_t)(r | sorted[r] % width << 8);
+      if (r == n - 1 || sorted[r + 1] / width != b) ends[2 * (int64_t)b + 1] = (uint16_t)(r + 1);
+    }
   }
 }
 
@@ -542,7 +590,7 @@ struct WaveTeacher {
   float t[PER], p[PER];
   bool on, rest;
   float L, r, u;
-  // the row's entries on their way: ids as cleaned, values
+  // the row's entries on their way: ids (only those below 0 are told apart), values
   __device__ __forceinline__ void load(const zl_targets& q, int64_t row, const int32_t* ids, int lane) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -584,12 +632,13 @@ struct WaveTeacher {
 
 // Joins the partial sums of R rows, 256 / R strands of blocks each, then a wave per
 // row forms its losses.  PAIR: both log-sums; masked: the second leaves the
-// teacher's ids out.  Without a teacher the label's logit is formed here too.
+// teacher's ids out; their logits go to the statistics in the ids' order.  Without a
+// teacher the label's logit is formed here too.
 template <int R, bool PAIR, bool BF>
 __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d, int blocks, const float* part,
                                                         zl_targets t, float a, float b, bool masked, const void* x_,
-                                                        int64_t ldx, const void* w_, int64_t ldw, const int32_t* tid,
-                                                        float* loss, float* stats) {
+                                                        int64_t ldx, const void* w_, int64_t ldw, const int32_t* slot,
+                                                        const float* named, float* loss, float* stats) {
   constexpr int S = 256 / R;
   __shared__ float4 red[S][R];
   const int r = threadIdx.x % R, st = threadIdx.x / R, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -602,11 +651,10 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
   auto fetch = [&](int64_t row) __attribute__((always_inline)) {
     yl = row_label(t, V, row);
     if (!t.ids) return;
-    const float* from = stats + row * (4 + t.k);
-    zy = from[3];
-    w.load(t, row, tid + row * (t.k + 1), lane);
+    zy = stats[row * (4 + t.k) + 3];
+    w.load(t, row, slot + row * t.k, lane);
 #pragma unroll
-    for (int j = 0; j < WaveTeacher::PER; ++j) zl[j] = lane + 64 * j < t.k ? from[4 + lane + 64 * j] : 0.f;
+    for (int j = 0; j < WaveTeacher::PER; ++j) zl[j] = w.id[j] >= 0 ? named[row * t.k + w.id[j]] : 0.f;
   };
   if (wave < R && row0 + wave < T) fetch(row0 + wave);
   LogSum x, y;
@@ -650,6 +698,9 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
     float total = 0.f, lt = 0.f, other = 0.f, l1 = 0.f;
     bool on = false;
     if (t.ids) {
+#pragma unroll
+      for (int j = 0; j < WaveTeacher::PER; ++j)
+        if (lane + 64 * j < t.k) out[4 + lane + 64 * j] = zl[j];
       w.form(t);
       on = w.on;
       float kl = 0.f;
@@ -863,7 +914,7 @@ __global__ void __launch_bounds__(256) head_zero_kernel(int64_t rows, int d, voi
 // ------------------------------------------------------------------ launches
 static unsigned grid(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
 
-HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool rest, bool backward, bool need_dx, bool need_dw,
+HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool backward, bool need_dx, bool need_dw,
                    int columns) {
   HeadPlan p;
   memset(&p, 0, sizeof(p));
@@ -873,19 +924,23 @@ HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool rest, bool ba
     p.large = plan_gemm(sh).large;
   }
   // columns of a wave tile
-  const int width = p.large ? 128 : dtype == F32 && f32_tile(T, V, 0, true) != F32_128 ? 32 : 64;
-  p.blocks = (V + width - 1) / width;
+  p.width = p.large ? 128 : dtype == F32 && f32_tile(T, V, 0, true) != F32_128 ? 32 : 64;
+  p.blocks = (V + p.width - 1) / p.width;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
     at += (bytes + 255) / 256 * 256;
     return o;
   };
-  p.tid = take(T * (k + 1) * 4);
+  p.tid = take(T * (k + 1) * 4);  // forward: slots
   if (!backward) {
     p.part = take((size_t)p.blocks * T * 16);
-    p.ldm = ((int64_t)V + 127) / 128 * 4;
-    if (rest) p.mask = take(T * p.ldm * 4);
+    p.ldb = ((int64_t)p.blocks + 3) / 4 * 4;
+    if (k) {
+      p.span = take(T * p.ldb * 4);
+      p.order = take(T * k * 4);
+      p.named = take(T * k * 4);
+    }
   } else {
     // a piece of dL/dz has at most 1 GiB
     const int64_t all = ((int64_t)V + 255) / 256 * 256;
@@ -941,29 +996,29 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   const zl_targets& t = a.targets;
   const bool bf = a.dtype == BF16, hard = t.labels != nullptr, soft = t.ids != nullptr, masked = soft && t.rest;
   const bool pair = hard && soft && (masked || t.temperature != 1.f);
-  const HeadPlan p = head_plan(T, a.V, a.d, bf ? BF16 : F32, t.k, masked, false, false, false, 0);
+  const HeadPlan p = head_plan(T, a.V, a.d, bf ? BF16 : F32, t.k, false, false, false, 0);
   char* ws = static_cast<char*>(a.workspace);
-  int32_t* tid = reinterpret_cast<int32_t*>(ws + p.tid);
+  int32_t* slot = reinterpret_cast<int32_t*>(ws + p.tid);
   float* part = reinterpret_cast<float*>(ws + p.part);
-  uint32_t* mask = masked ? reinterpret_cast<uint32_t*>(ws + p.mask) : nullptr;
+  uint32_t* span = soft ? reinterpret_cast<uint32_t*>(ws + p.span) : nullptr;
+  int32_t* order = reinterpret_cast<int32_t*>(ws + p.order);
+  float* named = reinterpret_cast<float*>(ws + p.named);
   float wa, wb;
   loss_weights(t, wa, wb);
   if (soft) {
-    // four entries a block where rows are few, a row where they are many
-    const int per = T * (t.k + 1) <= 16384 ? 4 : t.k + 1;
-    const dim3 g((unsigned)T, grid(t.k + 1, per));
+    const dim3 g((unsigned)T);
     if (bf)
-      hipLaunchKernelGGL((head_named_kernel<true>), g, dim3(256), 0, s, a.V, a.d, t, per, a.x, a.ldx, a.w, a.ldw, tid,
-                         a.stats, mask, p.ldm);
+      hipLaunchKernelGGL((head_named_kernel<true>), g, dim3(128), 0, s, a.V, a.d, t, p.width, a.x, a.ldx, a.w, a.ldw,
+                         a.stats, slot, order, span, p.ldb);
     else
-      hipLaunchKernelGGL((head_named_kernel<false>), g, dim3(256), 0, s, a.V, a.d, t, per, a.x, a.ldx, a.w, a.ldw, tid,
-                         a.stats, mask, p.ldm);
+      hipLaunchKernelGGL((head_named_kernel<false>), g, dim3(128), 0, s, a.V, a.d, t, p.width, a.x, a.ldx, a.w, a.ldw,
+                         a.stats, slot, order, span, p.ldb);
   }
   // a masked sum is always the second of a pair
   const bool two = pair || masked;
   const GemmDesc g = head_gemm(T, a.V, a.d, a.x, a.ldx, true, a.w, a.ldw, true);
   auto sums = [&](auto pc) -> hipError_t {
-    const StatEpi<decltype(pc)::value> e = {soft ? LOG2E / t.temperature : LOG2E, part, T, mask, p.ldm};
+    const StatEpi<decltype(pc)::value> e = {soft ? LOG2E / t.temperature : LOG2E, part, T, {order, span, p.ldb, named, t.k}, masked};
     return bf ? run_head<true, true>(g, e, p.large, s) : run_head_f32<true, true>(g, e, f32_tile(g.M, g.N, 0, true), s);
   };
   if (two) ZL_TRY(sums(std::true_type{}));
@@ -973,10 +1028,10 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
     constexpr bool P = decltype(pc)::value;
     if (bf)
       hipLaunchKernelGGL((head_rows_kernel<R, P, true>), dim3(grid(T, R)), dim3(256), 0, s, T, a.V, a.d, p.blocks, part, t,
-                         wa, wb, masked, a.x, a.ldx, a.w, a.ldw, tid, a.loss, a.stats);
+                         wa, wb, masked, a.x, a.ldx, a.w, a.ldw, slot, named, a.loss, a.stats);
     else
       hipLaunchKernelGGL((head_rows_kernel<R, P, false>), dim3(grid(T, R)), dim3(256), 0, s, T, a.V, a.d, p.blocks, part, t,
-                         wa, wb, masked, a.x, a.ldx, a.w, a.ldw, tid, a.loss, a.stats);
+                         wa, wb, masked, a.x, a.ldx, a.w, a.ldw, slot, named, a.loss, a.stats);
   };
   using std::integral_constant;
   auto by_rows = [&](auto pc) {
@@ -1023,7 +1078,7 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
   const bool hard = t.labels != nullptr, soft = t.ids != nullptr, rest = soft && t.rest;
   const bool two = hard && soft && (rest || t.temperature != 1.f);
   const int mode = !two ? GRAD_ONE : t.temperature == 2.f ? GRAD_SQUARE : GRAD_TWO;
-  const HeadPlan p = head_plan(T, a.V, d, dt, t.k, rest, true, a.dx != nullptr, a.dw != nullptr, a.columns);
+  const HeadPlan p = head_plan(T, a.V, d, dt, t.k, true, a.dx != nullptr, a.dw != nullptr, a.columns);
   char* ws = static_cast<char*>(a.workspace);
   int32_t* tid = reinterpret_cast<int32_t*>(ws + p.tid);
   float* tval = reinterpret_cast<float*>(ws + p.tval);

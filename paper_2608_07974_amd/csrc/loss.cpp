@@ -82,7 +82,7 @@ zl_status check_head(const zl_head_args* a, bool backward) {
   }
   if (a->T == 0) return ZL_OK;
   const zl_targets& t = a->targets;
-  const HeadPlan p = head_plan(a->T, a->V, a->d, dt_of(a->dtype), t.k, t.rest != nullptr, backward, a->dx != nullptr,
+  const HeadPlan p = head_plan(a->T, a->V, a->d, dt_of(a->dtype), t.k, backward, a->dx != nullptr,
                                a->dw != nullptr, a->columns);
   if (!a->workspace || a->workspace_bytes < p.bytes)
     return set_error(ZL_ERR_WORKSPACE, "head loss workspace missing or too small");
@@ -147,7 +147,7 @@ zl_status zl_head_loss_workspace(int64_t T, int V, int d, int dtype, int k, int 
   if (d < 8 || d % 8) return bad("d must be a positive multiple of 8");
   if (d > 65536) return unsupported("d above 65536");
   if (k > ZL_TARGETS_MAX_K) return unsupported("more than 256 ids per row");
-  *bytes = T ? head_plan(T, V, d, dt_of(dtype), k, has_rest != 0, backward != 0, need_dx != 0, need_dw != 0, columns).bytes : 0;
+  *bytes = T ? head_plan(T, V, d, dt_of(dtype), k, backward != 0, need_dx != 0, need_dw != 0, columns).bytes : 0;
   return ZL_OK;
 }
 

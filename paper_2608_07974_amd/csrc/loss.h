@@ -36,14 +36,14 @@ hipError_t launch_logit_loss(const LogitLossArgs& a, int dtype, bool backward, h
 // of the vocabulary that the backward goes through.
 struct HeadPlan {
   bool large;           // 256 x 256 tiles of the logits' product, else 128 x 128
-  int blocks;           // column blocks of the forward's partial sums
+  int width, blocks;    // column blocks of the forward's partial sums
   int columns;          // per piece
   int64_t ldz;          // row stride of dL/dz
-  int64_t ldm;          // words per row of the mask of named columns
-  size_t tid, tval, part, mask, gmax, coef, live, dz, dxa, xc, split, bytes;
+  int64_t ldb;          // blocks of a row as far as they have memory
+  size_t tid, tval, part, span, order, named, gmax, coef, live, dz, dxa, xc, split, bytes;
   size_t split_elems;
 };
-HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool rest, bool backward, bool need_dx, bool need_dw,
+HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool backward, bool need_dx, bool need_dw,
                    int columns);
 hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s);
 hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s);
