@@ -472,6 +472,111 @@ static hipError_t run_head_f32(const GemmDesc& g, const E& e, int tile, hipStrea
   return run_f32_tiles<128, 128, 2, 2, AK, BKM>(g, e, s, nz);
 }
 
+// Few tiles: 32 x 32 each, whose K four waves take in turns of 64 (fp32: 32), operands
+// straight into registers, the next turn's while one is multiplied; the first wave
+// adds the others' sums.  Both operands K-major.
+template <bool BF, typename E>
+__global__ void __launch_bounds__(256) head_small_kernel(GemmDesc g, E e) {
+  using el = typename std::conditional<BF, bf16_t, float>::type;
+  constexpr int W = 16 / sizeof(el), U = 4, TURN = 2 * W * U;
+  __shared__ __align__(16) float part[3][16][64];
+  static_assert(RowsOut<32, 32>::BYTES <= sizeof(part), "rows of the epilogue exceed LDS");
+  const int nbm = (g.M + 31) / 32, nbn = (g.N + 31) / 32;
+  int tm, tn;
+  tile_coords(blockIdx.x, nbm, nbn, tm, tn);
+  const int m0 = tm * 32, n0 = tn * 32;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lk = (lane >> 5) * W;
+  // rows past the end are others' once more; what they add is not stored
+  const el* a = static_cast<const el*>(g.A) + min(m0 + (lane & 31), g.M - 1) * g.lda + lk;
+  const el* b = static_cast<const el*>(g.B) + min(n0 + (lane & 31), g.N - 1) * g.ldb + lk;
+  Mma<32>::acc_t acc[1][1];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[0][0][r] = 0.f;
+  auto add = [&](uint4 x, uint4 w) __attribute__((always_inline)) {
+    if constexpr (BF) {
+      acc[0][0] = Mma<32>::run(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, x), acc[0][0]);
+    } else {
+      const float4 fx = __builtin_bit_cast(float4, x), fw = __builtin_bit_cast(float4, w);
+      acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(fw.x, fx.x, acc[0][0], 0, 0, 0);
+      acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(fw.y, fx.y, acc[0][0], 0, 0, 0);
+      acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(fw.z, fx.z, acc[0][0], 0, 0, 0);
+      acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(fw.w, fx.w, acc[0][0], 0, 0, 0);
+    }
+  };
+  // whole turns, two at a time: loads without conditions between them and into registers of
+  // their own, so that only the turn at hand is waited for
+  const int turns = g.K / TURN;
+  if (wave < turns) {
+    const int mine = (turns - wave + 3) / 4;
+    uint4 xa[U], wa[U], xb[U], wb[U];
+    auto load = [&](int i, uint4 (&x)[U], uint4 (&w)[U]) __attribute__((always_inline)) {
+      const int k = (wave + 4 * min(i, mine - 1)) * TURN;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        x[u] = *reinterpret_cast<const uint4*>(a + k + 2 * W * u);
+        w[u] = *reinterpret_cast<const uint4*>(b + k + 2 * W * u);
+      }
+      asm volatile("" ::: "memory");  // the loads stay in front of the products
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    load(0, xa, wa);
+    for (int i = 0; i + 1 < mine; i += 2) {
+      load(i + 1, xb, wb);
+#pragma unroll
+      for (int u = 0; u < U; ++u) add(xa[u], wa[u]);
+      load(i + 2, xa, wa);
+#pragma unroll
+      for (int u = 0; u < U; ++u) add(xb[u], wb[u]);
+    }
+    if (mine & 1)
+#pragma unroll
+      for (int u = 0; u < U; ++u) add(xa[u], wa[u]);
+  }
+  if (wave == turns % 4)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = turns * TURN + 2 * W * u;
+      uint4 x = make_uint4(0, 0, 0, 0), w = x;
+      if (k + lk < g.K) {  // K is a multiple of 8
+        x = *reinterpret_cast<const uint4*>(a + k);
+        w = *reinterpret_cast<const uint4*>(b + k);
+      }
+      add(x, w);
+    }
+  if (wave > 0)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) part[wave - 1][r][lane] = acc[0][0][r];
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[0][0][r] += part[w][r][lane];
+  wave_sync();
+  store_tile<32, 32, 1, 1, 32>(acc, reinterpret_cast<unsigned char*>(part), g, e, m0, n0, 0, lane);
+}
+// Up to 1024 of them, 512 in fp32 (larger tiles against these, forward: bf16 2 x 462 x 3368
+// 43.8 and 12.4 us, 345 x 2975 x 72 25.4 and 17.5, 112 x 12632 x 240 18.9 and 17.0 but
+// 214 x 12343 x 704 39.7 and 59.7; fp32 6 x 5639 x 528 25.2 and 14.7, 159 x 132 x 1520 47.9
+// and 20.5, 626 x 1585 x 440 27.9 and 29.9).
+static bool small_head(int64_t M, int64_t N, bool bf) {
+  return ((M + 31) / 32) * ((N + 31) / 32) <= (bf ? 1024 : 512);
+}
+template <typename E>
+static hipError_t run_head_small(const GemmDesc& g, const E& e, bool bf, hipStream_t s) {
+  const dim3 n(((g.M + 31) / 32) * ((g.N + 31) / 32));
+  if (bf) hipLaunchKernelGGL((head_small_kernel<true, E>), n, dim3(256), 0, s, g, e);
+  else hipLaunchKernelGGL((head_small_kernel<false, E>), n, dim3(256), 0, s, g, e);
+  return hipGetLastError();
+}
+// The product of x and w: sums or dL/dz.
+template <typename E>
+static hipError_t run_logits(const GemmDesc& g, const E& e, bool bf, bool large, hipStream_t s) {
+  if (small_head(g.M, g.N, bf)) return run_head_small(g, e, bf, s);
+  if (bf) return run_head<true, true>(g, e, large, s);
+  return run_head_f32<true, true>(g, e, f32_tile(g.M, g.N, 0, true), s);
+}
+
 // --------------------------------------------------------------- target rows
 // The ids of a row, absent ones and repetitions as -1, into `ids` [256] (LDS of the wave's
 // own): entries lane, lane + 64, ... of every lane.
@@ -865,15 +970,15 @@ __global__ void __launch_bounds__(256) head_clean_kernel(int64_t T, int d, const
     if (on) v = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(x) + row * ldx + c);
     *reinterpret_cast<uint4*>(static_cast<bf16_t*>(xc) + row * d + c) = v;
   } else {
-    float4 v[2] = {};
+    float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
     if (on) {
       const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + row * ldx + c);
-      v[0] = p[0];
-      v[1] = p[1];
+      lo = p[0];
+      hi = p[1];
     }
     float4* o = reinterpret_cast<float4*>(static_cast<float*>(xc) + row * d + c);
-    o[0] = v[0];
-    o[1] = v[1];
+    o[0] = lo;
+    o[1] = hi;
   }
 }
 
@@ -924,7 +1029,7 @@ HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool backward, boo
     p.large = plan_gemm(sh).large;
   }
   // columns of a wave tile
-  p.width = p.large ? 128 : dtype == F32 && f32_tile(T, V, 0, true) != F32_128 ? 32 : 64;
+  p.width = small_head(T, V, dtype == BF16) ? 32 : p.large ? 128 : dtype == F32 && f32_tile(T, V, 0, true) != F32_128 ? 32 : 64;
   p.blocks = (V + p.width - 1) / p.width;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -1019,7 +1124,7 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   const GemmDesc g = head_gemm(T, a.V, a.d, a.x, a.ldx, true, a.w, a.ldw, true);
   auto sums = [&](auto pc) -> hipError_t {
     const StatEpi<decltype(pc)::value> e = {soft ? LOG2E / t.temperature : LOG2E, part, T, {order, span, p.ldb, named, t.k}, masked};
-    return bf ? run_head<true, true>(g, e, p.large, s) : run_head_f32<true, true>(g, e, f32_tile(g.M, g.N, 0, true), s);
+    return run_logits(g, e, bf, p.large, s);
   };
   if (two) ZL_TRY(sums(std::true_type{}));
   else ZL_TRY(sums(std::false_type{}));
@@ -1116,7 +1221,7 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
       GemmShape sh = {(int)T, n, d, true, true, false, 0, false, 0};
       auto grads = [&](auto mc) -> hipError_t {
         const GradEpi<decltype(mc)::value> e = {coef, soft ? 1.f / t.temperature : 1.f, dz, p.ldz, dt};
-        return bf ? run_head<true, true>(g, e, plan_gemm(sh).large, s) : run_head_f32<true, true>(g, e, f32_tile(g.M, g.N, 0, true), s);
+        return run_logits(g, e, bf, bf && plan_gemm(sh).large, s);
       };
       if (mode == GRAD_ONE) ZL_TRY(grads(std::integral_constant<int, GRAD_ONE>{}));
       else if (mode == GRAD_TWO) ZL_TRY(grads(std::integral_constant<int, GRAD_TWO>{}));

@@ -498,6 +498,20 @@ def test_head_loss_large_tiles(hard, k, rest):
     _check_head(_head_case(1000, 16421, 72, k, rest, hard, 1.0 if not k else 2.0, BF), 1.0 if not k else 2.0, BF)
 
 
+@pytest.mark.parametrize("T,V,dt", [(300, 4209, BF), (3, 33001, BF), (130, 4209, F32), (1100, 4001, F32), (20, 17001, F32)])
+@pytest.mark.parametrize("hard,k,rest,tau", [(1, 0, 0, 1.0), (0, 33, 0, 1.0), (0, 200, 1, 2.0), (1, 9, 0, 2.0)])
+def test_head_loss_more_tiles(T, V, dt, hard, k, rest, tau):
+    """Sizes beyond the smallest tiles, of every tile in between, strided operands."""
+    _check_head(_head_case(T, V, 40, k, rest, hard, tau, dt, pad=8), tau, dt)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("d", [8, 56, 64, 72, 256, 264, 1000])
+def test_head_loss_few_tiles_any_width(d, dt):
+    """A sum over d split over the waves, parts of it empty or cut."""
+    _check_head(_head_case(34, 70, d, 5, True, 1, 2.0, dt, pad=8), 2.0, dt)
+
+
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_head_loss_many_rows_few_columns(dt):
     """Few tiles of a long sum: the weight's gradient is split over the rows."""
