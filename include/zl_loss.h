@@ -78,11 +78,11 @@ zl_status zl_logit_loss_backward(int64_t T, int V, const void* z, int64_t ldz, i
 /* --------------------------------------------------- loss of a readout head
  * The same loss of z = x w^T, x [T, d], w [V, d] (both ZL_BF16 or both ZL_F32; d a
  * multiple of 8, at most 65536; rows 16-byte aligned, strides multiples of 8 below
- * 2^21; the forward T V at most 2^36).  z is held in fp32 accumulators and never
- * stored: the forward keeps partial sums of 32 to 128 columns, the backward forms z
- * again, `columns` of the vocabulary at a time, and from it dL/dz in x's type, which
- * it multiplies on.  With ZL_BF16 log2(e) z and log2(e) z / tau have to be numbers of
- * fp32 (|z| up to 2^127, which products of finite weights and inputs stay far below).
+ * 2^21; the forward T V at most 2^36, the backward T d below 2^35).  z is held in fp32
+ * accumulators and never stored: the forward keeps partial sums of 32 to 128 columns,
+ * the backward forms z again, `columns` of the vocabulary at a time, and from it dL/dz
+ * in x's type, which it multiplies on.  With ZL_BF16 log2(e) z and log2(e) z / tau have
+ * to be numbers of fp32 (|z| up to 2^127).
  *
  * stats [T, 4 + k], contiguous: as above, then z at the teacher's ids (0 where
  * absent).
@@ -113,7 +113,8 @@ typedef struct zl_head_args {
   void* dx;
   int64_t lddx;
   int dx_dtype;
-  void* dw;               /* with it T d < 2^30 (ZL_ERR_UNSUPPORTED above)     */
+  void* dw;               /* with it T d < 2^30, V d < 2^35
+                             (ZL_ERR_UNSUPPORTED above)                        */
   int64_t lddw;
   int dw_dtype;
   int accumulate;

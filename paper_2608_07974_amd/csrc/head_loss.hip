@@ -456,11 +456,14 @@ static hipError_t run_f32_tiles(const GemmDesc& g, const E& e, hipStream_t s, in
 // row per column of the vocabulary); 64 x 64 where those of 128 x 128, with splits of 256 of
 // K at least where they may be, leave CUs idle (a matrix instruction takes 64 cycles: 64 of
 // K are 3.9 us in a tile of 128 x 128, 1 in one of 64 x 64; 4096 x 1000 x 512 60.7 and 53.8 us,
-// 128 x 50257 x 768 108 and 116); else 128 x 128.
+// 128 x 50257 x 768 108 and 116) or would be a tenth emptier (192 x 97946 x 200 103 and 95,
+// dx of 264 x 10870 x 1552 from 265 for all to 249); else 128 x 128.
 enum { F32_128, F32_64, F32_32 };
 static int f32_tile(int64_t M, int64_t N, int64_t split, bool ak) {
   if (ak && M <= 32) return F32_32;
   const int64_t parts = split >= 512 ? split / 256 : 1;
+  const int64_t wide = ((M + 127) / 128) * ((N + 127) / 128) * 4, narrow = ((M + 63) / 64) * ((N + 63) / 64);
+  if (narrow * 10 <= wide * 9 && narrow < 1 << 23) return F32_64;  // (2^31 threads)
   return ((M + 127) / 128) * ((N + 127) / 128) * parts <= 256 ? F32_64 : F32_128;
 }
 template <bool AK, bool BKM, typename E>

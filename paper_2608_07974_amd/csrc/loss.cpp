@@ -13,6 +13,7 @@ namespace {
 
 constexpr int64_t MAX_T = (int64_t)1 << 21;
 constexpr int MAX_V = 1 << 30;
+constexpr int64_t MAX_ELEMS = (int64_t)1 << 35;  // of a matrix that a thread per eight goes over
 constexpr int64_t MAX_LD = (int64_t)1 << 21;  // of x and w: a tile's 32-bit offsets
 
 zl_status bad(const char* msg) { return set_error(ZL_ERR_INVALID_ARG, msg); }
@@ -71,12 +72,14 @@ zl_status check_head(const zl_head_args* a, bool backward) {
     if (a->T && (!a->loss || !by(a->loss, 4))) return bad("loss missing or misaligned");
   } else {
     if (!by(a->dloss, 4)) return bad("misaligned dloss");
+    if (a->T * a->d >= MAX_ELEMS) return unsupported("T d >= 2^35: take the rows in parts");
     if (a->columns < 0) return bad("columns must be >= 0");
     if (!a->dx && !a->dw) return bad("dx, dw or both must be there");
     if (a->dx && (!dtype_ok(a->dx_dtype) || !mat_ok(a->dx, a->lddx, a->d, 1))) return bad("dx: bad dtype, alignment or row stride");
     if (a->dw) {
       if (!dtype_ok(a->dw_dtype) || !mat_ok(a->dw, a->lddw, a->d, 1)) return bad("dw: bad dtype, alignment or row stride");
       if (a->accumulate && a->dw_dtype != ZL_F32) return unsupported("accumulation into a bf16 dw");
+      if ((int64_t)a->V * a->d >= MAX_ELEMS) return unsupported("dw of V d >= 2^35");
       if ((a->T + 64) * a->d >= (int64_t)1 << 30) return unsupported("dw of T d >= 2^30: take the rows in parts, with accumulate");
     }
   }

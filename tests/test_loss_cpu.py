@@ -135,6 +135,15 @@ def test_head_loss_limits():
     assert "2^30" in _refused(UNS, zl.zl_head_loss_backward, _head(True, **wide))
 
 
+def test_head_loss_backward_beyond_a_launch():
+    # a thread per eight elements: 2^32 of them are one launch too many
+    rows = dict(T=1 << 21, d=16384, ldx=16384, ldw=16384, lddx=16384, lddw=16384)
+    assert "2^35" in _refused(UNS, zl.zl_head_loss_backward, _head(True, **rows, dw=0))
+    wide = dict(V=1 << 30, d=64, ldx=64, ldw=64, lddx=64, lddw=64)
+    assert "2^35" in _refused(UNS, zl.zl_head_loss_backward, _head(True, **wide))
+    assert "2^35" in _refused(UNS, zl.zl_head_loss_backward, _head(True, **wide, T=0))
+
+
 def test_head_loss_workspace():
     for back in (False, True):
         fn = zl.zl_head_loss_backward if back else zl.zl_head_loss
