@@ -503,7 +503,7 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
   __shared__ unsigned long long list[CAP];
   __shared__ float red[NT / 64];
   __shared__ uint32_t bound_s, count_s, hist[256];
-  __shared__ unsigned long long cut_s;  // terms cut off the list
+  __shared__ unsigned long long cut_s[NT / 64];  // terms cut off the list, by wave
   __shared__ int scan[NT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
@@ -543,10 +543,8 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
       for (int i = 0; i < PER; ++i) strands[tid + NT * i] = order_of(m[i]);
     }
   }
-  if (tid == 0) {
-    count_s = 0;
-    cut_s = 0;
-  }
+  if (tid == 0) count_s = 0;
+  if (tid < NT / 64) cut_s[tid] = 0;
   __syncthreads();
   if (wave == 0) {
     uint32_t s[STRANDS / 64];
@@ -591,6 +589,12 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
       enter(W * g - z.pad + e, __builtin_bit_cast(float, BF ? (e & 1 ? d & 0xffff0000u : d << 16) : d));
     }
   };
+  auto cut_off = [&]() -> float {
+    unsigned long long c = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) c += cut_s[w];
+    return (float)c * 0x1p-40f;
+  };
   // cuts the list of n entries at its want-th largest; false where that is no number
   auto tighten = [&](uint32_t n) -> bool {
     if (wave == 0) {
@@ -611,9 +615,8 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
     if (all || !(to > -INFINITY && to < INFINITY)) return false;
     bound = bound_s;
     if (tid == 0) {
-      sum += (float)cut_s * 0x1p-40f;
+      sum += cut_off();
       count_s = 0;
-      cut_s = 0;
     }
     __syncthreads();
     sum *= __builtin_amdgcn_exp2f((ref - to) * c2);
@@ -626,7 +629,9 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
       if (o >= bound) list[atomicAdd(&count_s, 1u)] = mine[i];
       else cut += (unsigned long long)(__builtin_amdgcn_exp2f((value_of(o) - ref) * c2) * 0x1p40f);
     }
-    if (cut) atomicAdd(&cut_s, cut);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) cut += __shfl_xor(cut, o, 64);
+    if (lane == 0) cut_s[wave] = cut;
     return true;
   };
   const int rounds = (z.full1 - z.full0 + TOP_U * NT - 1) / (TOP_U * NT);
@@ -766,7 +771,7 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
     }
   }
   if (!rest) return;
-  if (fits && tid == 0) sum += (float)cut_s * 0x1p-40f;
+  if (fits && tid == 0) sum += cut_off();
   sum = block_sum<NT>(sum, red);
   if (tid < 64) {
     const float top = n > kk ? __builtin_bit_cast(float, strands[0]) : -INFINITY;  // the rest's largest
