@@ -227,7 +227,7 @@ enum { EXP_ONE, EXP_TWO, EXP_SQUARE };
 // Log-sums of z (unless EXP_ONE) and of z / tau; REST: the latter without the teacher's
 // ids.  The sums are taken relative to the largest of the row's first columns: no
 // running maximum (8 instead of 10 cycles of the vector units per element, which come
-// near the memory's time; 4096 x 128256 bf16, labels and 64 ids at tau 2: 177 us, 5.9 TB/s).
+// near the memory's time; 4096 x 128256 bf16, labels and 64 ids at tau 2: 175 us, 6.0 TB/s).
 // Where that reference is so far off that a sum overflows, or that of the columns beside
 // the teacher's nearly vanishes, the row goes by once more with running maxima.
 template <bool BF, int NT, int MODE, bool REST, bool STREAM>
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
 // Off the named columns c1 exp(z - l1) + ct exp(z / tau - lt): the softmax itself, or with
 // a rest what is left of it once the teacher's share of the rest is taken off.  The
 // named columns' values are formed first and put in as those come by, so that each
-// element is written once (4096 x 128256 bf16, as above: 381 us, 5.5 TB/s).  Differences are taken before the scaling by log2(e), which
+// element is written once (4096 x 128256 bf16, as above: 380 us, 5.5 TB/s).  Differences are taken before the scaling by log2(e), which
 // would overflow in a row of the type's lowest values.
 template <bool STREAM>
 __device__ __forceinline__ void store_group(bf16_t* p, const float (&v)[8]) {
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
 // Where the list overflows (many equal values, ascending rows), or there is a NaN, a
 // radix search by 8 bits finds the (k + 1)-th largest exactly and a last pass lists what
 // is above it and, in order of the columns, what equals it.
-// 2048 x 128256 bf16, k 64: 120 us, 4.4 TB/s; two passes over memory for bound and list 172.
+// 2048 x 128256 bf16, k 64: 122 us, 4.3 TB/s; two passes over memory for bound and list 172.
 constexpr int TOP_U = 8;
 
 // Order of floats as unsigned numbers; -0 as 0, every NaN above all numbers.
