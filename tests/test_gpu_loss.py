@@ -536,6 +536,26 @@ def test_head_loss_rows_without_targets_may_hold_anything(dt):
     assert not bool(dx[::3].any())
 
 
+@pytest.mark.parametrize("T,V,dt", [(300, 4209, BF), (1000, 16421, BF), (130, 4209, F32), (1100, 4001, F32), (20, 17001, F32)])
+def test_head_loss_rows_without_targets_in_every_tile(T, V, dt):
+    L = _L()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, 40, generator=g, device="cuda").to(_dt(dt))
+    w = (torch.randn(V, 40, generator=g, device="cuda") / 3).to(_dt(dt))
+    y = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    top = L.top_logits(x.float() @ w.float().t(), 7, temperature=2.0)
+    y[::3] = -100
+    top.ids[::3] = -1
+    kw = dict(labels=y, teacher=top, temperature=2.0)
+    bad = x.clone()
+    bad[::3] = float("nan")
+    bad[3] = float("inf")
+    (a, sa), (b, sb) = L.head_loss(x, w, **kw), L.head_loss(bad, w, **kw)
+    assert torch.equal(a, b) and torch.equal(sa, sb)
+    p, q = L.head_loss_bwd(x, w, sa, need_dw=True, **kw), L.head_loss_bwd(bad, w, sb, need_dw=True, **kw)
+    assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1]) and not bool(q[0][::3].any())
+
+
 def test_head_loss_is_the_loss_of_its_logits():
     """The two operators agree on logits that fp32 holds exactly."""
     rng = _rng("same")
@@ -612,6 +632,22 @@ def test_head_beyond_32_bit_offsets():
     p = L.head_loss_bwd(x, far, a[1], y, need_dw=True)
     for m, n in zip(p, q):
         assert torch.allclose(m.float(), n.float(), rtol=2.0 ** -7, atol=1e-3)
+
+
+@pytest.mark.parametrize("T,dt", [(300, BF), (1000, BF), (130, F32), (20, F32)])
+def test_head_of_rows_far_apart(T, dt):
+    """A weight whose rows lie 4 or 8 MB apart, in every tile; the same sums as one of close rows."""
+    L = _L()
+    V = 4209 if T > 20 else 3001
+    far = torch.empty(V, (1 << 21) - 8, dtype=_dt(dt), device="cuda")[:, :64]
+    near = (torch.randn(V, 64, device="cuda") / 4).to(_dt(dt))
+    far.copy_(near)
+    x = torch.randn(T, 64, device="cuda").to(_dt(dt))
+    y = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
+    a, b = L.head_loss(x, far, y), L.head_loss(x, near, y)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    p, q = (L.head_loss_bwd(x, m, a[1], y, need_dw=True, columns=256) for m in (far, near))
+    assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1])
 
 
 # ------------------------------------------------------- as a program uses them
