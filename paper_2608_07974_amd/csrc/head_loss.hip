@@ -1199,6 +1199,12 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
   void* xc = ws + p.xc;
   float wa, wb;
   loss_weights(t, wa, wb);
+  // The labels' weight (the teacher's, where that is all but alone) is taken out of dL/dz and
+  // into the scale, as the largest |dloss| is: a sure label's entry is then -1, not a number
+  // that is rounded alike in every row.
+  const float weight = wa > 0x1p-20f * wb * t.temperature ? wa : wb * t.temperature, scale = a.scale * weight;
+  wa /= weight;
+  wb /= weight;
   if (a.dloss && T > GMAX_ROWS) hipLaunchKernelGGL(head_gmax_kernel, dim3(1), dim3(1024), 0, s, T, a.dloss, gmax);
   hipLaunchKernelGGL(head_coef_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, a.V, t, wa, wb, mode, a.stats, a.dloss, gmax,
                      tid, tval, coef, live);
@@ -1244,25 +1250,25 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
       const bool whole = first && last;
       OutEpi e = {dxa, d, F32, 1.f, nullptr, !first, 0};
       if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, T * d};
-      else if (whole) e = {a.dx, a.lddx, dxt, a.scale, most, 0, 0};
+      else if (whole) e = {a.dx, a.lddx, dxt, scale, most, 0, 0};
       if (bf) ZL_TRY((run_head<true, false>(g, e, tile, s, nz)));
       else ZL_TRY((run_head_f32<true, false>(g, e, tile, s, nz)));
       if (nz > 1 && whole)
-        finish(T, split, nz, a.scale, most, a.dx, a.lddx, dxt, 0);
+        finish(T, split, nz, scale, most, a.dx, a.lddx, dxt, 0);
       else if (nz > 1)
         finish(T, split, nz, 1.f, nullptr, dxa, d, F32, !first);
-      if (last && !whole) finish(T, dxa, 1, a.scale, most, a.dx, a.lddx, dxt, 0);
+      if (last && !whole) finish(T, dxa, 1, scale, most, a.dx, a.lddx, dxt, 0);
     }
     if (a.dw) {
       GemmDesc g = head_gemm(n, d, T, dz, p.ldz, false, xc, d, false);
       char* out = static_cast<char*>(a.dw) + (size_t)v0 * a.lddw * (dwt == BF16 ? 2 : 4);
       int tile;
       const int nz = head_splits<false, false>(n, d, T, bf, p.split_elems, tile, g.ksplit);
-      OutEpi e = {out, a.lddw, dwt, a.scale, most, a.accumulate, 0};
+      OutEpi e = {out, a.lddw, dwt, scale, most, a.accumulate, 0};
       if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, (int64_t)n * d};
       if (bf) ZL_TRY((run_head<false, false>(g, e, tile, s, nz)));
       else ZL_TRY((run_head_f32<false, false>(g, e, tile, s, nz)));
-      if (nz > 1) finish(n, split, nz, a.scale, most, out, a.lddw, dwt, a.accumulate);
+      if (nz > 1) finish(n, split, nz, scale, most, out, a.lddw, dwt, a.accumulate);
     }
   }
   return hipGetLastError();

@@ -556,6 +556,23 @@ def test_head_loss_rows_without_targets_in_every_tile(T, V, dt):
     assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1]) and not bool(q[0][::3].any())
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_head_loss_weights_do_not_round(dt):
+    """A label's weight is no part of the bf16 operand: with no teacher in any row alpha only
+    scales the result."""
+    L = _L()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, w = torch.randn(70, 64, generator=g, device="cuda").to(_dt(dt)), torch.randn(130, 64, generator=g, device="cuda").to(_dt(dt))
+    y = torch.randint(0, 130, (70,), generator=g, device="cuda", dtype=torch.int32)
+    none = L.TopLogits(torch.full((70, 3), -1, dtype=torch.int32, device="cuda"), torch.zeros(70, 3, device="cuda"))
+    out = []
+    for kw, scale in ((dict(teacher=none, alpha=0.3), 1.0), (dict(), 0.3)):
+        dx, dw = torch.empty(70, 64, device="cuda"), torch.empty(130, 64, device="cuda")
+        _, stats = L.head_loss(x, w, y, **kw)
+        out.append(L.head_loss_bwd(x, w, stats, y, dx=dx, dw=dw, scale=scale, **kw))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
 def test_head_loss_is_the_loss_of_its_logits():
     """The two operators agree on logits that fp32 holds exactly."""
     rng = _rng("same")
