@@ -560,9 +560,13 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
   const bool all = !(ref > -INFINITY && ref < INFINITY);  // no bound among numbers: list what there is
   float least = all ? -INFINITY : ref;
   if (all) ref = 0.f;
-  auto enter = [&](int c, float v) __attribute__((always_inline)) {
+  // Entries beyond the list are counted only; the row is searched again then.
+  auto append = [&](unsigned long long key) __attribute__((always_inline)) {
     const uint32_t at = atomicAdd(&count_s, 1u);
-    if (at < CAP) list[at] = (unsigned long long)order_of(v) << 32 | (0xffffffffu - (uint32_t)c);
+    if (at < CAP) list[at] = key;
+  };
+  auto enter = [&](int c, float v) __attribute__((always_inline)) {
+    append((unsigned long long)order_of(v) << 32 | (0xffffffffu - (uint32_t)c));
   };
   // A group: the few columns that reach the bound leave it (a NaN too; one that the
   // maximum hides shows in the sum), the rest is summed.  Kept short: unrolled per
@@ -626,7 +630,8 @@ __global__ void __launch_bounds__(NT) top_logits_kernel(int V, const void* x, in
     for (int i = 0; i < MINE; ++i) {
       if (mine[i] == 0) continue;
       const uint32_t o = (uint32_t)(mine[i] >> 32);
-      if (o >= bound) list[atomicAdd(&count_s, 1u)] = mine[i];
+      // (waves ahead of this one enter the next round's columns meanwhile)
+      if (o >= bound) append(mine[i]);
       else cut += (unsigned long long)(__builtin_amdgcn_exp2f((value_of(o) - ref) * c2) * 0x1p40f);
     }
 #pragma unroll

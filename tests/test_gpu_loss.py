@@ -420,6 +420,48 @@ def test_top_logits_repeatable(T, k, dt):
         assert torch.equal(a.rest, b.rest)
 
 
+def _check_top_rows(x, k, rows, tau=2.0):
+    """Some rows of a batch whose size decides the kernel's form."""
+    got = _L().top_logits(x, k, temperature=tau)
+    ids, values, rest = ol.top_logits(_np(x[rows]), k, tau)
+    assert np.array_equal(got.ids[rows].cpu().numpy(), ids)
+    assert np.array_equal(_np(got.values[rows]), values)
+    _near(_np(got.rest[rows]), rest, (x.shape[1] / 512 + 160) * U + 4 * U * np.abs(rest), what="rest")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("k", [5, 150, 256])
+@pytest.mark.parametrize("T,V,step", [(600, 70001, 8192), (4, 300001, 32768), (600, 1000, 100)])
+def test_top_logits_of_ties_that_grow(T, V, step, k, dt):
+    """Equal columns nearly fill the list in the first round and more come in every later one
+    (step: columns of a round of fp32; a round of bf16 has twice as many)."""
+    rng = _rng("grow", T, V, k, dt)
+    x = _dev(np.zeros((T, V)), dt, 3, 1)
+    x.copy_(torch.randn(T, V, generator=torch.Generator(device="cuda").manual_seed(k), device="cuda"))
+    step *= 2 if dt == BF else 1
+    cap = 512 if k <= 64 else 1024
+    rows = [0, 1, T // 2, T - 1]
+    for r, fill in zip(rows, (0.8, 0.9, 0.97, 0.99)):
+        x[r, torch.from_numpy(rng.permutation(step)[: int(cap * fill)] % V).cuda()] = 9.0
+        for at in range(step, V, step):
+            n = min(V - at, step)
+            x[r, at + torch.from_numpy(rng.permutation(n)[: 100]).cuda()] = 9.0
+    _check_top_rows(x, k, rows)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("k", [5, 64, 256])
+@pytest.mark.parametrize("skip", [0, 3])
+def test_top_logits_of_many_rows(skip, k, dt):
+    """Rows of many rounds whose list is cut between them, in the form for many rows."""
+    T, V = 600, 40003
+    x = torch.full((T, V + 5), float("nan"), dtype=_dt(dt), device="cuda")[:, skip: skip + V]
+    z = torch.randn(T, V, generator=torch.Generator(device="cuda").manual_seed(k + skip), device="cuda")
+    z[::2] += torch.linspace(0, 8, V, device="cuda")
+    x.copy_(z)
+    _check_top_rows(x, k, [0, 1, 2, 3, 298, 299, 598, 599])
+
+
 def test_top_logits_without_rest():
     x = _dev(_rng("norest").standard_normal((3, 500)))
     a, b = _L().top_logits(x, 7, rest=False), _L().top_logits(x, 7)
