@@ -228,8 +228,9 @@ enum { EXP_ONE, EXP_TWO, EXP_SQUARE };
 // ids.  The sums are taken relative to the largest of the row's first columns: no
 // running maximum (8 instead of 10 cycles of the vector units per element, which come
 // near the memory's time; 4096 x 128256 bf16, labels and 64 ids at tau 2: 175 us, 6.0 TB/s).
-// Where that reference is so far off that a sum overflows, or that of the columns beside
-// the teacher's nearly vanishes, the row goes by once more with running maxima.
+// Where that reference is so far off that either sum overflows or nearly vanishes (first
+// columns at -inf: 0, which no column need be near; the columns beside the teacher's), the
+// row goes by once more with running maxima.
 template <bool BF, int NT, int MODE, bool REST, bool STREAM>
 __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
   __shared__ typename NamesOf<NT>::type names;
@@ -296,7 +297,8 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
   });
   st.s = block_sum<NT>(st.s, red);
   if constexpr (TWO) s1.s = block_sum<NT>(s1.s, red);
-  if (!(st.s < INFINITY && st.s > 1e-18f && (!TWO || s1.s < INFINITY))) {
+  auto fits = [](float s) { return s > 1e-18f && s < INFINITY; };
+  if (!fits(st.s) || (TWO && !fits(s1.s))) {
     s1 = st = LogSum();
     z.template each<NT, 1>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
       if constexpr (TWO) {

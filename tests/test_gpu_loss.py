@@ -282,6 +282,36 @@ def test_logit_loss_masked_logits(dt, rest):
     assert not _np(dz)[6:].any() and not _np(loss)[6:].any() and not _np(stats)[6:].any()
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("tau", [2.0, 4.0, 10.0, 0.5])
+@pytest.mark.parametrize("T,V,head", [(6, 8192, 2048), (6, 30000, 16384), (2100, 4000, 1024), (6, 1500, 512)])
+def test_logit_loss_of_a_masked_head(T, V, head, tau, rest, dt):
+    """A row's first columns, as many as a block looks at for a reference, are all at -inf and
+    the others far from 0, where exp(z) or its square leaves fp32 and exp(z / tau) does not."""
+    rng = _rng("masked head", T, V, int(tau * 2), rest, dt)
+    far = np.array([-90.0, -100.0, -130.0, -200.0, -700.0, 120.0])
+    z = rng.standard_normal((6, V)) + far[:, None]
+    z[:, :head] = -np.inf
+    zd = torch.zeros(T, V, dtype=_dt(dt), device="cuda")
+    zd[:6] = _dev(z, dt)
+    z = _np(zd[:6])
+    y = rng.integers(head, V, T)
+    ids = rng.permuted(np.tile(np.arange(head, V), (T, 1)), axis=1)[:, :5]
+    ids[1, 2] = y[1]
+    values = rng.standard_normal((T, 5)).astype(np.float32).astype(np.float64)
+    r = rng.standard_normal(T).astype(np.float32).astype(np.float64) if rest else None
+    kw = dict(labels=_i32(y), teacher=_teacher(ids, values, r), alpha=0.3, temperature=tau)
+    loss, stats = _L().logit_loss(zd, **kw)
+    dz = _L().logit_loss_bwd(zd, stats, **kw)
+    six = (z, y[:6], ids[:6], values[:6], r[:6] if rest else None, 0.3, tau)
+    ref, rs, rdz = ol.loss(*six)
+    log = (V / 256 + 200) * (1 + _mag(z, values[:6], six[4], tau)) * U
+    _near(_np(loss[:6]), ref, (0.3 + 0.7 * tau * tau) * 2 * log, what="loss")
+    _near(_np(stats[:6]), rs, log[:, None], what="stats")
+    _near(_np(dz[:6]), rdz, _spread(*six) * 2 * log[:, None], dt, "dz")
+
+
 @pytest.mark.parametrize("alpha", [0.0, 1.0])
 @pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
 def test_alpha_at_its_ends(alpha, tau):
