@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
     ct = lt == -INFINITY ? 0.f : f * (expf(s.z - s.y) - q.r);
   }
   if (q.here) {
-    float g = f * (expf(q.zi * inv - s.y) - q.p);
+    float g = q.teacher ? f * (expf(q.zi * inv - s.y) - q.p) : 0.f;  // (0 times what may overflow)
     if (q.label) g += c1 * (q.id == q.y ? expm1f(q.zi - s.x) : expf(q.zi - s.x));
     names.val[threadIdx.x] = g;
   }

@@ -350,6 +350,39 @@ def test_teacher_that_weighs_nothing_is_none():
         assert not _np(dz)[0].any()
 
 
+@pytest.mark.parametrize("tau", [0.1, 1.0, 2.0, 3.0])
+@pytest.mark.parametrize("rest", [False, True])
+def test_teacher_that_weighs_nothing_beside_labels(rest, tau):
+    """The labels' loss alone, also where the ids' logits are such that exp(z / tau) of them
+    leaves fp32, the label's among them."""
+    V, k, T = 300, 3, 7
+    rng = _rng("nothing", rest, int(tau * 10))
+    z = rng.standard_normal((T, V)) * 3
+    ids = np.tile(np.array([4, 90, 299]), (T, 1))
+    z[1:, 4] = [9.0, 50.0, 100.0, 700.0, 100.0, 100.0]
+    z[2:, 90] = 120.0
+    y = np.array([1, 4, 4, 90, 2, 4, -1])
+    values, r = np.full((T, k), -np.inf), np.full(T, -np.inf) if rest else None
+    values[5] = [1.0, 2.0, -np.inf]  # one row has a teacher
+    kw = dict(labels=_i32(y), teacher=_teacher(ids, values, r), alpha=0.3, temperature=tau)
+    zd = _dev(z)
+    z = _np(zd)
+    ref, rs, rdz = ol.loss(z, y, ids, values, r, 0.3, tau)
+    log = (V / 256 + 200) * (1 + _mag(z, np.nan_to_num(values, neginf=0.0), r, tau)) * U
+    tol = _spread(z, y, ids, values, r, 0.3, tau) * 2 * log[:, None]
+    loss, stats = _L().logit_loss(zd, **kw)
+    _near(_np(loss), ref, (0.3 + 0.7 * tau * tau) * 2 * log, what="loss")
+    _near(_np(stats), rs, log[:, None], what="stats")
+    _near(_np(_L().logit_loss_bwd(zd, stats, **kw)), rdz, tol, what="dz")
+    # the head of the same logits: each is one product with 1 and zeros
+    w, x = torch.eye(V, 304, device="cuda"), torch.zeros(T, 304, device="cuda")
+    x[:, :V] = zd
+    loss, stats = _L().head_loss(x, w, **kw)
+    _near(_np(loss), ref, (0.3 + 0.7 * tau * tau) * 2 * log, what="head's loss")
+    dx, _ = _L().head_loss_bwd(x, w, stats, **kw)
+    _near(_np(dx)[:, :V], rdz, tol, what="dx")
+
+
 def test_nan_is_seen():
     """A NaN in a row that counts reaches its loss."""
     z = np.zeros((2, 300))
