@@ -74,7 +74,7 @@ zl_status check_head(const zl_head_args* a, bool backward) {
     if (!by(a->dloss, 4)) return bad("misaligned dloss");
     if (a->T * a->d >= MAX_ELEMS) return unsupported("T d >= 2^35: take the rows in parts");
     if (a->columns < 0) return bad("columns must be >= 0");
-    if (!a->dx && !a->dw) return bad("dx, dw or both must be there");
+    if (a->T && !a->dx && !a->dw) return bad("dx, dw or both must be there");
     if (a->dx && (!dtype_ok(a->dx_dtype) || !mat_ok(a->dx, a->lddx, a->d, 1))) return bad("dx: bad dtype, alignment or row stride");
     if (a->dw) {
       if (!dtype_ok(a->dw_dtype) || !mat_ok(a->dw, a->lddw, a->d, 1)) return bad("dw: bad dtype, alignment or row stride");

@@ -412,6 +412,20 @@ def test_empty_batch():
     assert not bool(dw.any())
 
 
+def test_empty_batch_of_a_frozen_head():
+    """An empty dx has no address, and there is no dw."""
+    L = _L()
+    x, w = torch.ones(3, 16, device="cuda"), torch.ones(50, 16, device="cuda")
+    y = _i32([1, 2, 3])
+    _, stats = L.head_loss(x, w, y)
+    for empty in (torch.empty(0, 16, device="cuda"), x[0:0]):
+        dx, dw = L.head_loss_bwd(empty, w, stats[0:0], y[0:0])
+        assert dx.shape == (0, 16) and dw is None
+    top = L.TopLogits(_i32([[1, 2]] * 3), _f32([[1.0, 2.0]] * 3))
+    _, stats = L.head_loss(x[0:0], w, None, L.TopLogits(top.ids[0:0], top.values[0:0]))
+    assert L.head_loss_bwd(x[0:0], w, stats, None, L.TopLogits(top.ids[0:0], top.values[0:0]))[0].shape == (0, 16)
+
+
 # --------------------------------------------------------------- top logits
 def _check_top(x, k, tau=1.0):
     got = _L().top_logits(x, k, temperature=tau)

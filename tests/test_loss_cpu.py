@@ -124,6 +124,16 @@ def test_head_loss_backward_refuses(kw):
     _refused(INV, zl.zl_head_loss_backward, _head(True, **kw))
 
 
+@pytest.mark.parametrize("kw", [dict(dx=0, dw=0), dict(dx=0, dw=0, x=0, stats=0, dloss=0, workspace=0, workspace_bytes=0),
+                                dict(dx=0, dw=0, targets=_t(labels=0, ids=0, values=0, rest=0, k=0))])
+def test_head_loss_backward_of_nothing_is_not_invalid(kw):
+    """No rows, no dw: nothing to do, as of empty tensors, which have no addresses."""
+    try:
+        zl.zl_head_loss_backward(_head(True, T=0, accumulate=0, **kw))
+    except zl.ZlError as e:
+        assert e.status == zl.ZL_ERR_HIP, e  # (a machine without a GPU)
+
+
 def test_head_loss_limits():
     for kw in (dict(T=(1 << 21) + 1), dict(V=(1 << 30) + 1), dict(d=65544, ldx=65544, ldw=65544), dict(ldx=1 << 21),
                dict(ldw=1 << 21), dict(targets=_t(k=257))):
