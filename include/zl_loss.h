@@ -91,7 +91,7 @@ zl_status zl_logit_loss_backward(int64_t T, int V, const void* z, int64_t ldz, i
  * accumulate: fp32 dw only); either may be NULL (both with T = 0).  A row of x without label and
  * teacher adds nothing to dw, also if it is infinite or NaN.  With ZL_BF16 dL/dz
  * is rounded to bf16 as an operand of both products, after division by the
- * largest |dloss| and by a (without labels b tau), so that rows of equal weight
+ * largest |dloss| of rows with a target and by a (without labels b tau), so that rows of equal weight
  * round as with weight 1; sums are fp32. */
 typedef struct zl_head_args {
   int64_t T;

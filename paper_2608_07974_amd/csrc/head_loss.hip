@@ -847,15 +847,31 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
   }
 }
 
-// The largest |dloss| (0 and what is not finite count as 1).
-__global__ void __launch_bounds__(1024) head_gmax_kernel(int64_t T, const float* dloss, float* gmax) {
-  __shared__ float red[16];
-  float m = 0.f;
-  for (int64_t i = threadIdx.x; i < T; i += 1024) m = fmaxf(m, fabsf(dloss[i]));
-  m = block_max<1024>(m, red);
-  if (threadIdx.x == 0) *gmax = m > 0.f && m < INFINITY ? m : 1.f;
+// The largest |dloss| of rows with a target (0 and what is not finite count as 1): with a
+// label, or a log-sum of z / tau, which rows without a teacher have not.  (One that is 0 by
+// chance is passed over: the largest is a scale, no more.)
+__device__ __forceinline__ float row_weight(const zl_targets& t, int V, const float* stats, const float* dloss,
+                                            int64_t row) {
+  const float w = fabsf(dloss[row]);
+  bool on = row_label(t, V, row) >= 0;
+  if (t.ids) on |= stats[row * (4 + t.k) + 1] != 0.f;
+  return on ? w : 0.f;
 }
-constexpr int GMAX_ROWS = 4096;  // up to which every block of the next kernel looks for itself
+// Its share of the rows each, GMAX_PARTS at most (one block of 1024 threads: 10 us for 16384
+// rows, whose statistics are a cache line each).
+constexpr int GMAX_PARTS = 64;
+__global__ void __launch_bounds__(256) head_gmax_kernel(int64_t T, int V, zl_targets t, const float* stats,
+                                                        const float* dloss, float* part) {
+  __shared__ float red[4];
+  float m = 0.f;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < T; i += (int64_t)gridDim.x * 256)
+    m = fmaxf(m, row_weight(t, V, stats, dloss, i));
+  m = block_max<256>(m, red);
+  if (threadIdx.x == 0) part[blockIdx.x] = m;
+}
+// Up to so many rows every block of the next kernel looks for itself: a launch less.
+__host__ __device__ inline bool gmax_by_block(int64_t T, const zl_targets& t) { return T <= (t.ids ? 1024 : 4096); }
+__host__ __device__ inline int gmax_parts(int64_t T) { return (int)(T < 256 * GMAX_PARTS ? (T + 255) / 256 : GMAX_PARTS); }
 
 // Per row what dL/dz takes (GradEpi), the named columns (tid as in the forward) and
 // their values; a wave per row.
@@ -869,14 +885,15 @@ __global__ void __launch_bounds__(256) head_coef_kernel(int64_t T, int V, zl_tar
   int32_t mine[ZL_TARGETS_MAX_K / 64];
   if (t.ids) row_ids(t, V, row, row < T, lane, ids[wave], mine);
   float most = 1.f;
-  if (dloss && T <= GMAX_ROWS) {
+  if (dloss) {
     float m = 0.f;
-    for (int i = threadIdx.x; i < (int)T; i += 256) m = fmaxf(m, fabsf(dloss[i]));
+    if (gmax_by_block(T, t))
+      for (int i = threadIdx.x; i < (int)T; i += 256) m = fmaxf(m, row_weight(t, V, stats, dloss, i));
+    else if ((int)threadIdx.x < gmax_parts(T))
+      m = gmax[1 + threadIdx.x];
     m = block_max<256>(m, red);
     most = m > 0.f && m < INFINITY ? m : 1.f;
     if (blockIdx.x == 0 && threadIdx.x == 0) *gmax = most;
-  } else if (dloss) {
-    most = *gmax;
   }
   if (row >= T) return;
   const int32_t* id = ids[wave];
@@ -1060,7 +1077,7 @@ HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool backward, boo
     p.columns = (int)c;
     p.ldz = c;
     p.tval = take(T * (k + 1) * 4);
-    p.gmax = take(4);
+    p.gmax = take((1 + GMAX_PARTS) * 4);  // and of parts of the rows
     p.coef = take(T * 16);
     p.live = take(T * 4);
     p.dz = take(T * p.ldz * es);
@@ -1205,7 +1222,8 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
   const float weight = wa > 0x1p-20f * wb * t.temperature ? wa : wb * t.temperature, scale = a.scale * weight;
   wa /= weight;
   wb /= weight;
-  if (a.dloss && T > GMAX_ROWS) hipLaunchKernelGGL(head_gmax_kernel, dim3(1), dim3(1024), 0, s, T, a.dloss, gmax);
+  if (a.dloss && !gmax_by_block(T, t))
+    hipLaunchKernelGGL(head_gmax_kernel, dim3(gmax_parts(T)), dim3(256), 0, s, T, a.V, t, a.stats, a.dloss, gmax + 1);
   hipLaunchKernelGGL(head_coef_kernel, dim3(grid(T, 4)), dim3(256), 0, s, T, a.V, t, wa, wb, mode, a.stats, a.dloss, gmax,
                      tid, tval, coef, live);
   const float* most = a.dloss ? gmax : nullptr;

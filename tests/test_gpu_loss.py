@@ -692,6 +692,35 @@ def test_head_loss_weights_do_not_round(dt):
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("T,V,k", [(70, 130, 0), (70, 130, 3), (1500, 130, 3), (5000, 130, 0), (5000, 130, 3)])
+@pytest.mark.parametrize("big", [3e38, float("inf"), float("nan")])
+def test_head_loss_weights_of_rows_without_targets(T, V, k, big, dt):
+    """They may be anything: the other rows' gradients are what they are beside weights of 0."""
+    L = _L()
+    g = torch.Generator(device="cuda").manual_seed(T + k)
+    x = torch.randn(T, 64, generator=g, device="cuda").to(_dt(dt))
+    w = (torch.randn(V, 64, generator=g, device="cuda") / 4).to(_dt(dt))
+    y = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    y[1::2] = -1
+    kw = dict(labels=y)
+    if k:
+        top = L.top_logits(x.float() @ w.float().t(), k)
+        top.ids[::3] = -1
+        kw.update(teacher=top)
+    dead = torch.zeros(T, dtype=torch.bool, device="cuda")
+    dead[1::2] = True
+    if k:
+        dead[1::2] = top.ids[1::2, 0] < 0
+    dloss = (torch.rand(T, generator=g, device="cuda") + 0.5) / T
+    dloss[dead] = 0.0
+    _, stats = L.head_loss(x, w, **kw)
+    want = L.head_loss_bwd(x, w, stats, dloss=dloss, need_dw=True, **kw)
+    assert bool(want[0].any())
+    got = L.head_loss_bwd(x, w, stats, dloss=torch.where(dead, big, dloss), need_dw=True, **kw)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_head_loss_is_the_loss_of_its_logits():
     """The two operators agree on logits that fp32 holds exactly."""
     rng = _rng("same")
