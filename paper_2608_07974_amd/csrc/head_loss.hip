@@ -56,7 +56,8 @@ struct GradEpi {
   int64_t ldz;
   int dtype;
 };
-// out = (accumulate ? out : 0) + scale * *gmax * C, or fp32 partials of split z.
+// out = (accumulate ? out : 0) + scale * *gmax * C, or fp32 partials of split z.  Rows that
+// are not live add 0 (dx: where w is infinite or NaN, C is NaN though dL/dz is 0).
 struct OutEpi {
   void* out;
   int64_t ldo;
@@ -65,6 +66,7 @@ struct OutEpi {
   const float* gmax;      // or null
   int accumulate;
   int64_t zstride;
+  const int32_t* live;    // [M] or null
 };
 // The epilogue of split z of K.
 template <typename E> __device__ __forceinline__ E split_part(const E& e, int) { return e; }
@@ -267,12 +269,14 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
   static_for<0, FM>([&](auto ic) __attribute__((always_inline)) {
     constexpr int i = decltype(ic)::value;
     const int64_t m = m0 + wm * TM + i * MF + (lane & (MF - 1));
+    const bool on = !e.live || (m < g.M && e.live[m] != 0);
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r0 = 0; r0 < NR; r0 += 4) {
         const int n = nb + j * MF + Mma<MF>::row(lane, r0);
-        float4 v = make_float4(acc[i][j][r0], acc[i][j][r0 + 1], acc[i][j][r0 + 2], acc[i][j][r0 + 3]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (on) v = make_float4(acc[i][j][r0], acc[i][j][r0 + 1], acc[i][j][r0 + 2], acc[i][j][r0 + 3]);
         v.x *= scale;
         v.y *= scale;
         v.z *= scale;
@@ -1266,9 +1270,9 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
       int tile;
       const int nz = head_splits<true, false>(T, d, n8, bf, p.split_elems, tile, g.ksplit);
       const bool whole = first && last;
-      OutEpi e = {dxa, d, F32, 1.f, nullptr, !first, 0};
-      if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, T * d};
-      else if (whole) e = {a.dx, a.lddx, dxt, scale, most, 0, 0};
+      OutEpi e = {dxa, d, F32, 1.f, nullptr, !first, 0, live};
+      if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, T * d, live};
+      else if (whole) e = {a.dx, a.lddx, dxt, scale, most, 0, 0, live};
       if (bf) ZL_TRY((run_head<true, false>(g, e, tile, s, nz)));
       else ZL_TRY((run_head_f32<true, false>(g, e, tile, s, nz)));
       if (nz > 1 && whole)
@@ -1282,8 +1286,8 @@ hipError_t launch_head_loss_bwd(const zl_head_args& a, hipStream_t s) {
       char* out = static_cast<char*>(a.dw) + (size_t)v0 * a.lddw * (dwt == BF16 ? 2 : 4);
       int tile;
       const int nz = head_splits<false, false>(n, d, T, bf, p.split_elems, tile, g.ksplit);
-      OutEpi e = {out, a.lddw, dwt, scale, most, a.accumulate, 0};
-      if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, (int64_t)n * d};
+      OutEpi e = {out, a.lddw, dwt, scale, most, a.accumulate, 0, nullptr};
+      if (nz > 1) e = {split, d, F32, 1.f, nullptr, 0, (int64_t)n * d, nullptr};
       if (bf) ZL_TRY((run_head<false, false>(g, e, tile, s, nz)));
       else ZL_TRY((run_head_f32<false, false>(g, e, tile, s, nz)));
       if (nz > 1) finish(n, split, nz, scale, most, out, a.lddw, dwt, a.accumulate);

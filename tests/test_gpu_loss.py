@@ -676,6 +676,34 @@ def test_head_loss_rows_without_targets_in_every_tile(T, V, dt):
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("gdt", [BF, F32])
+@pytest.mark.parametrize("T,V,d,columns", [(5, 40, 24, 0), (300, 4209, 40, 0), (300, 4209, 40, 1024), (40, 30000, 64, 0),
+                                           (1000, 16421, 72, 0)])
+def test_head_loss_rows_without_targets_of_a_broken_head(T, V, d, columns, gdt, dt):
+    """Their dx is 0 also where it is the weight that is infinite or NaN, and they add nothing to
+    dw, in one piece or several, with and without splits of the sum."""
+    L = _L()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, d, generator=g, device="cuda").to(_dt(dt))
+    w = (torch.randn(V, d, generator=g, device="cuda") / 4).to(_dt(dt))
+    w[V // 2] = float("inf")
+    w[V - 1, 3] = float("nan")
+    y = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    some = y.clone()
+    some[T // 2] = 3
+    for labels in (y, some):
+        loss, stats = L.head_loss(x, w, labels)
+        dx, dw = torch.full((T, d), 7.0, dtype=_dt(gdt), device="cuda"), torch.full((V, d), 7.0, dtype=_dt(gdt), device="cuda")
+        L.head_loss_bwd(x, w, stats, labels, dx=dx, dw=dw, columns=columns)
+        dead = labels < 0
+        assert not bool(loss[dead].any()) and not bool(dx[dead].any())
+        if labels is y:
+            assert not bool(dw.any())
+        else:
+            assert bool(torch.isnan(loss[T // 2])) and bool(torch.isnan(dx[T // 2]).any())
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
 def test_head_loss_weights_do_not_round(dt):
     """A label's weight is no part of the bf16 operand: with no teacher in any row alpha only
     scales the result."""
