@@ -25,7 +25,8 @@ extern "C" {
 /* ------------------------------------------------------------- the targets
  * Row t has logits z (V of them) and adds
  *   loss = a CE + b tau^2 KL,   tau = temperature, 2^-60 to 2^60,
- * a = alpha, b = 1 - alpha with labels and a teacher, else 1 for the one there is.
+ * a = alpha, b = 1 - alpha with labels and a teacher, else 1 for the one there is.  A term
+ * of weight 0 adds nothing, also where it is infinite.
  *
  * Label y:  CE = log sum_v exp(z_v) - z_y.  A label outside [0, V) is none.
  *

@@ -834,13 +834,13 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
       lt = q.log(inv);
       kl = wave_sum(kl) + lt - w.L;
       if (masked && w.r != 0.f) kl += w.r * (w.u - other);
-      if (on) total = b * t.temperature * t.temperature * kl;
+      if (on && b != 0.f) total = b * t.temperature * t.temperature * kl;  // (a term of weight 0 may be infinite)
     } else {
       lt = q.log(inv);
     }
     l1 = PAIR ? p.log(1.f) : lt;
     if (lane == 0) {
-      if (label) total += a * (l1 - zy);
+      if (label && a != 0.f) total += a * (l1 - zy);
       if (!label && !on) total = 0.f;
       loss[row] = total;
       out[0] = label ? l1 : 0.f;

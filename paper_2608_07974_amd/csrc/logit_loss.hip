@@ -340,8 +340,9 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
   }
   if (threadIdx.x == 0) {
     const float tau = a.t.temperature;
-    float loss = q.label ? a.a * (l1 - q.zy) : 0.f;
-    if (q.teacher) loss += a.b * tau * tau * kl;
+    // (a term of weight 0 may be infinite)
+    float loss = q.label && a.a != 0.f ? a.a * (l1 - q.zy) : 0.f;
+    if (q.teacher && a.b != 0.f) loss += a.b * tau * tau * kl;
     a.loss[row] = loss;
     *reinterpret_cast<float4*>(a.stats + 4 * row) =
         make_float4(q.label ? l1 : 0.f, q.teacher ? lt : 0.f, REST && q.teacher ? other : 0.f, q.zy);

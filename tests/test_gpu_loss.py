@@ -336,6 +336,37 @@ def test_alpha_at_its_ends(alpha, tau):
     _near(_np(dx)[:, :300], rdz, _spread(z, y, ids, values, r, alpha, tau) * 2 * log[:, None])
 
 
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
+def test_a_term_of_weight_0_may_be_infinite(tau):
+    """alpha 1 beside a teacher whose divergence is infinite (its rest has no column, or an id is
+    masked), alpha 0 beside a masked label."""
+    z = np.array([[1.0, -2.0, 0.5], [1.0, -2.0, -np.inf], [1.0, 0.0, -1.0]])
+    zd = _dev(z)
+    ids, values, rest = np.array([[0, 1, 2]] * 3), np.ones((3, 3)), np.array([0.0, -np.inf, -np.inf])
+    none = np.full((3, 3), -1)
+    y = np.array([1, 0, 2])
+    kw = dict(teacher=_teacher(ids, values, rest), alpha=1.0, temperature=tau)
+    loss, stats = _L().logit_loss(zd, _i32(y), **kw)
+    want = ol.loss(z, y, none, values, None, 1.0)
+    _near(_np(loss), want[0], 1e-5)  # (3 columns of magnitude 2: a few u)
+    _near(_np(_L().logit_loss_bwd(zd, stats, _i32(y), **kw)), want[2], 1e-5)
+    y[:] = 2
+    kw = dict(teacher=_teacher(ids[:, :2], values[:, :2], None), alpha=0.0, temperature=tau)
+    loss, stats = _L().logit_loss(zd, _i32(y), **kw)
+    want = ol.loss(z, None, ids[:, :2], values[:, :2], None, tau=tau)
+    _near(_np(loss), want[0], 1e-4)  # (tau^2 times that)
+    _near(_np(_L().logit_loss_bwd(zd, stats, _i32(y), **kw)), want[2], 1e-4)
+    x, w = torch.ones(2, 8, device="cuda"), torch.zeros(3, 8, device="cuda")
+    w[:, 0] = zd[0]
+    x[:, 1:] = 0.0
+    kw = dict(teacher=_teacher(ids[:2], values[:2], np.zeros(2)), alpha=1.0, temperature=tau)
+    loss, stats = _L().head_loss(x, w, _i32(y[:2]), **kw)
+    want = ol.loss(np.stack([z[0]] * 2), y[:2])
+    _near(_np(loss), want[0], 1e-5)
+    dx, _ = _L().head_loss_bwd(x, w, stats, _i32(y[:2]), **kw)
+    _near(_np(dx), want[2] @ _np(w), 1e-4)
+
+
 def test_teacher_that_weighs_nothing_is_none():
     z = _dev(np.ones((3, 20)))
     ids, values = np.array([[1, 2]] * 3), np.array([[-np.inf, -np.inf], [1.0, -np.inf], [-np.inf, -np.inf]])
