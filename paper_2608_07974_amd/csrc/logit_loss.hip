@@ -63,22 +63,45 @@ struct Row {
       else v[k] = __builtin_bit_cast(float, (uint32_t)r[k]);
     }
   }
-  // a cut group, -inf outside the row
-  __device__ __forceinline__ void get_cut(int g, float (&v)[W]) const {
+  // a cut group, -inf outside the row and in column y
+  __device__ __forceinline__ void get_cut(int g, float (&v)[W], int y = -1) const {
 #pragma unroll
     for (int k = 0; k < W; ++k) {
       const int c = W * g - pad + k;
-      v[k] = c >= 0 && c < V ? at(c) : -INFINITY;
+      v[k] = c >= 0 && c < V && c != y ? at(c) : -INFINITY;
     }
   }
-  // f(group, values) for this thread's groups, U loads in flight
-  template <int NT, int U, bool STREAM = false, typename F>
-  __device__ __forceinline__ void each(F&& f) const {
-    int g = full0 + (int)threadIdx.x;
+  // -inf in column y of its group
+  __device__ __forceinline__ void drop(u32x4_t& r, int y) const {
+    const int e = (y + pad) & (W - 1);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (BF) {
+        if (e >> 1 == w) r[w] = e & 1 ? (r[w] & 0xffffu) | 0xff800000u : (r[w] & 0xffff0000u) | 0xff80u;
+      } else {
+        if (e == w) r[w] = 0xff800000u;
+      }
+    }
+  }
+  // f(group, values) for this thread's groups, U loads in flight; DROP: column y (-1: none)
+  // as -inf, found with a comparison per U groups
+  template <int NT, int U, bool STREAM = false, bool DROP = false, typename F>
+  __device__ __forceinline__ void each(F&& f, int y = -1) const {
+    int g = full0 + (int)threadIdx.x, gy = -1;
+    if constexpr (DROP) {
+      if (y >= 0 && ((group_of(y) - g) & (NT - 1)) == 0) gy = group_of(y);
+    }
     for (; g + (U - 1) * NT < full1; g += U * NT) {
       u32x4_t r[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) r[u] = load<STREAM>(g + u * NT);
+      if constexpr (DROP) {
+        if ((uint32_t)(gy - g) <= (U - 1) * NT) {
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (g + u * NT == gy) drop(r[u], y);
+        }
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         float v[W];
@@ -87,15 +110,19 @@ struct Row {
       }
     }
     for (; g < full1; g += NT) {
+      u32x4_t r = load<STREAM>(g);
+      if constexpr (DROP) {
+        if (g == gy) drop(r, y);
+      }
       float v[W];
-      get(load<STREAM>(g), v);
+      get(r, v);
       f(g, v);
     }
     if (threadIdx.x < 2) {
       const int c = cut((int)threadIdx.x);
       if (c >= 0) {
         float v[W];
-        get_cut(c, v);
+        get_cut(c, v, y);
         f(c, v);
       }
     }
@@ -225,7 +252,7 @@ enum { EXP_ONE, EXP_TWO, EXP_SQUARE };
 
 // ---------------------------------------------------------------- forward
 // Log-sums of z (unless EXP_ONE) and of z / tau; REST: the latter without the teacher's
-// ids.  The sums are taken relative to the largest of the row's first columns: no
+// ids; all without the label, which joins them at the end (label_term).  The sums are taken relative to the largest of the row's first columns: no
 // running maximum (8 instead of 10 cycles of the vector units per element, which come
 // near the memory's time; 4096 x 128256 bf16, labels and 64 ids at tau 2: 175 us, 6.0 TB/s).
 // Where that reference is so far off that either sum overflows or nearly vanishes (first
@@ -239,14 +266,9 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
   constexpr int W = Row<BF>::W;
   const int64_t row = blockIdx.x;
   const Row<BF> z(a.z, row * a.ldz, a.V);
-  float first = -INFINITY;
-  if ((int)threadIdx.x < z.groups()) {
-    const int g = threadIdx.x;
-    float v[W];
-    if (g >= z.full0 && g < z.full1) z.get(z.load(g), v);
-    else z.get_cut(g, v);
-    first = max_of(v);
-  }
+  u32x4_t first = {};
+  const int g0 = threadIdx.x;
+  if (g0 >= z.full0 && g0 < z.full1) first = z.load(g0);
   const RowTargets q = row_targets<NT, BF>(a, row, z, names, false, red);
   if (!q.label && !q.teacher) {
     if (threadIdx.x == 0) {
@@ -267,11 +289,24 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
       }
     }
   };
+  // The label's column is left out of both sums, and out of their reference.
+  const int y = q.label ? q.y : -1;
   LogSum s1, st;  // of z, of z / tau (EXP_ONE: st alone, at 1 / tau)
-  float ref = block_max<NT>(first, red);
+  float ref = -INFINITY;
+  if (g0 < z.groups()) {
+    float v[W];
+    if (g0 >= z.full0 && g0 < z.full1) {
+      if (y >= 0 && z.group_of(y) == g0) z.drop(first, y);
+      z.get(first, v);
+    } else {
+      z.get_cut(g0, v, y);
+    }
+    ref = max_of(v);
+  }
+  ref = block_max<NT>(ref, red);
   if (!(fabsf(ref) < INFINITY)) ref = 0.f;
   s1.m = st.m = ref;
-  z.template each<NT, 4, STREAM>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
+  z.template each<NT, 4, STREAM, true>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
     if constexpr (MODE == EXP_TWO) {
 #pragma unroll
       for (int k = 0; k < W; ++k) s1.s += __builtin_amdgcn_exp2f((v[k] - ref) * LOG2E);
@@ -294,13 +329,13 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
       st.s += p;
       if constexpr (MODE == EXP_SQUARE) s1.s = __builtin_fmaf(p, p, s1.s);
     }
-  });
+  }, y);
   st.s = block_sum<NT>(st.s, red);
   if constexpr (TWO) s1.s = block_sum<NT>(s1.s, red);
   auto fits = [](float s) { return s > 1e-18f && s < INFINITY; };
   if (!fits(st.s) || (TWO && !fits(s1.s))) {
     s1 = st = LogSum();
-    z.template each<NT, 1>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
+    z.template each<NT, 1, false, true>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
       if constexpr (TWO) {
         s1.raise(max_of(v), LOG2E);
         const float r = s1.ref();
@@ -314,9 +349,17 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
       const float r = st.ref();
 #pragma unroll
       for (int k = 0; k < W; ++k) st.s += __builtin_amdgcn_exp2f((v[k] - r) * c2);
-    });
+    }, y);
     st = block_logsum<NT>(st, c2, red);
     if constexpr (TWO) s1 = block_logsum<NT>(s1, LOG2E, red);
+  }
+  const LabelTerm ce = label_term(TWO ? s1 : st, q.zy);
+  if (q.label && q.teacher) {
+    // the label's share of the teacher's log-sum, unless the teacher names it and has a rest
+    bool named = false;
+    if constexpr (REST)
+      for (int e = names.first(z.group_of(q.y)); e >= 0; e = names.next[e]) named |= names.id[e] == q.y;
+    if (!named) st.merge(q.zy, q.zy == -INFINITY ? 0.f : 1.f, c2);
   }
   float other = 0.f, lt = 0.f;
   if constexpr (REST) {
@@ -331,21 +374,20 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
     n = block_logsum<NT>(n, c2, red);
     st.merge(n.m, n.s, c2);
   }
-  lt = st.log(inv);
-  const float l1 = TWO ? s1.log(1.f) : lt;  // (EXP_ONE: tau = 1 where there are labels)
   float kl = 0.f;
   if (a.t.ids) {
+    lt = st.log(inv);
     kl = block_sum<NT>(q.p > 0.f || q.p != q.p ? q.p * (q.t - q.zi * inv) : 0.f, red) + lt - q.L;
     if (REST && q.r != 0.f) kl += q.r * (a.t.rest[row] - other);
   }
   if (threadIdx.x == 0) {
     const float tau = a.t.temperature;
     // (a term of weight 0 may be infinite)
-    float loss = q.label && a.a != 0.f ? a.a * (l1 - q.zy) : 0.f;
+    float loss = q.label && a.a != 0.f ? a.a * ce.loss : 0.f;
     if (q.teacher && a.b != 0.f) loss += a.b * tau * tau * kl;
     a.loss[row] = loss;
     *reinterpret_cast<float4*>(a.stats + 4 * row) =
-        make_float4(q.label ? l1 : 0.f, q.teacher ? lt : 0.f, REST && q.teacher ? other : 0.f, q.zy);
+        make_float4(q.label ? ce.logsum : 0.f, q.teacher ? lt : 0.f, REST && q.teacher ? other : 0.f, q.zy);
   }
 }
 
@@ -353,7 +395,11 @@ __global__ void __launch_bounds__(NT) logit_loss_kernel(LogitLossArgs a) {
 // Off the named columns c1 exp(z - l1) + ct exp(z / tau - lt): the softmax itself, or with
 // a rest what is left of it once the teacher's share of the rest is taken off.  The
 // named columns' values are formed first and put in as those come by, so that each
-// element is written once (4096 x 128256 bf16, as above: 380 us, 5.5 TB/s).  Differences are taken before the scaling by log2(e), which
+// element is written once (4096 x 128256 bf16, as above: 380 us, 5.5 TB/s).
+// A sure label's q - 1 (q above 0.88) is the sum of the others' -q, taken on the way and
+// stored by the wave that ends last: as expm1(z - l1) it would have the steps of z, not its
+// own digits (all rows sure 385 us; bf16 16384 x 1000 17.4 against 13.9).  Others lose up to
+// 3 bits of it, and no time.  Differences are taken before the scaling by log2(e), which
 // would overflow in a row of the type's lowest values.
 template <bool STREAM>
 __device__ __forceinline__ void store_group(bf16_t* p, const float (&v)[8]) {
@@ -370,18 +416,20 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
   constexpr int W = Row<BF>::W;
   __shared__ typename NamesOf<NT>::type names;
   __shared__ float red[NT / 64];
+  __shared__ int ended;
   const int64_t row = blockIdx.x;
   const Row<BF> z(a.z, row * a.ldz, a.V);
   E* out = static_cast<E*>(a.dz) + row * a.lddz;
   const bool vec = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(z.p)) & 15) == 0;
-  auto put = [&](int g, const float (&v)[W]) __attribute__((always_inline)) {
+  // but for column `last` of group `glast`
+  auto put = [&](int g, const float (&v)[W], int glast = -1, int last = -1) __attribute__((always_inline)) {
     const int c0 = W * g - z.pad;
-    if (vec && c0 >= 0 && c0 + W <= z.V) {
+    if (vec && c0 >= 0 && c0 + W <= z.V && g != glast) {
       store_group<STREAM>(out + c0, v);
     } else {
 #pragma unroll
       for (int k = 0; k < W; ++k)
-        if (c0 + k >= 0 && c0 + k < z.V) Elem<E>::store(out, c0 + k, v[k]);
+        if (c0 + k >= 0 && c0 + k < z.V && c0 + k != last) Elem<E>::store(out, c0 + k, v[k]);
     }
   };
   const float4 s = *reinterpret_cast<const float4*>(a.stats + 4 * row);
@@ -400,15 +448,26 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
     lt = s.z;
     ct = lt == -INFINITY ? 0.f : f * (expf(s.z - s.y) - q.r);
   }
+  const float alpha = c1;
+  const bool sure = q.label && alpha != 0.f && s.x - q.zy < 0.125f;
+  float others = 0.f;  // exp(z - l1) of this thread's id
   if (q.here) {
     float g = q.teacher ? f * (expf(q.zi * inv - s.y) - q.p) : 0.f;  // (0 times what may overflow)
-    if (q.label) g += c1 * (q.id == q.y ? expm1f(q.zi - s.x) : expf(q.zi - s.x));
+    if (q.label && q.id != q.y) {
+      others = expf(q.zi - s.x);
+      g += c1 * others;
+    } else if (q.label && !sure) {
+      g += c1 * expm1f(q.zi - s.x);
+    }
     names.val[threadIdx.x] = g;
   }
-  if (threadIdx.x == 0 && q.label) {
-    float g = c1 * expm1f(q.zy - s.x);
-    if (ct != 0.f) g += ct * expf(q.zy * inv - lt);
-    names.val[a.t.k] = g;
+  if (threadIdx.x == 0) {
+    ended = 0;
+    if (q.label) {
+      float g = sure ? 0.f : c1 * expm1f(q.zy - s.x);
+      if (ct != 0.f) g += ct * expf(q.zy * inv - lt);
+      names.val[a.t.k] = g;
+    }
   }
   __syncthreads();
   if constexpr (MODE == EXP_ONE) {
@@ -421,32 +480,67 @@ __global__ void __launch_bounds__(NT) logit_loss_bwd_kernel(LogitLossArgs a) {
   // a term that is not there vanishes also where its exponential would overflow
   if (ct == 0.f && (MODE != EXP_SQUARE || c1 == 0.f)) lt = INFINITY;
   if (c1 == 0.f) l1 = INFINITY;
-  z.template each<NT, 4, STREAM>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
-    float o[W];
+  float sum = 0.f;  // of unnamed columns' exp(z - l1), as the mode has them
+  const int gy = sure ? z.group_of(q.y) : -1;
+  auto pass = [&](auto of_sure) __attribute__((always_inline)) {
+    constexpr bool SURE = decltype(of_sure)::value;
+    z.template each<NT, 4, STREAM>([&](int g, float (&v)[W]) __attribute__((always_inline)) {
+      const bool named = names.maybe(g);
+      // f(column in the group, entry) of the named ones
+      auto each_named = [&](auto&& f) __attribute__((always_inline)) {
+        for (int e = names.first(g); e >= 0; e = names.next[e]) {
+          const int c = names.id[e];
+          if (c >= 0 && z.group_of(c) == g) f(c - (W * g - z.pad), e);
+        }
+      };
+      if (SURE && named)
+        each_named([&](int c, int) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], inv, -lt) * LOG2E);
-      if constexpr (MODE == EXP_ONE) {
-        o[k] = ct * p;
-      } else if constexpr (MODE == EXP_SQUARE) {
-        o[k] = p * __builtin_fmaf(p, c1, ct);
-      } else {
-        const float p1 = __builtin_amdgcn_exp2f((v[k] - l1) * LOG2E);
-        o[k] = __builtin_fmaf(c1, p1, ct * p);
-      }
-    }
-    if (names.maybe(g)) {
-      for (int e = names.first(g); e >= 0; e = names.next[e]) {
-        const int c = names.id[e];
-        if (c >= 0 && z.group_of(c) == g) {
-          const float w = names.val[e];
+          for (int k = 0; k < W; ++k) v[k] = k == c ? -INFINITY : v[k];
+        });
+      float o[W];
 #pragma unroll
-          for (int k = 0; k < W; ++k) o[k] = W * g - z.pad + k == c ? w : o[k];
+      for (int k = 0; k < W; ++k) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], inv, -lt) * LOG2E);
+        if constexpr (MODE == EXP_ONE) {
+          o[k] = ct * p;
+          if constexpr (SURE) sum += p;
+        } else if constexpr (MODE == EXP_SQUARE) {
+          o[k] = p * __builtin_fmaf(p, c1, ct);
+          if constexpr (SURE) sum = __builtin_fmaf(p, p, sum);
+        } else {
+          const float p1 = __builtin_amdgcn_exp2f((v[k] - l1) * LOG2E);
+          o[k] = __builtin_fmaf(c1, p1, ct * p);
+          if constexpr (SURE) sum += p1;
         }
       }
-    }
-    put(g, o);
-  });
+      if (named)
+        each_named([&](int c, int e) __attribute__((always_inline)) {
+          const float w = names.val[e];
+#pragma unroll
+          for (int k = 0; k < W; ++k) o[k] = k == c ? w : o[k];
+        });
+      if constexpr (SURE) put(g, o, gy, q.y);
+      else put(g, o);
+    });
+  };
+  if (!sure) {
+    pass(std::false_type{});
+    return;
+  }
+  pass(std::true_type{});
+  // EXP_SQUARE: c1 holds the factor between the terms and exp(z - l1)
+  sum = wave_sum(MODE == EXP_SQUARE ? __builtin_fmaf(sum, c1, others * alpha) : (sum + others) * alpha);
+  if ((threadIdx.x & 63) != 0) return;
+  red[threadIdx.x >> 6] = sum;
+  if (__hip_atomic_fetch_add(&ended, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_WORKGROUP) != NT / 64 - 1) return;
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) sum += red[w];
+  float base = 0.f;
+  for (int e = names.first(gy); e >= 0; e = names.next[e])
+    if (names.id[e] == q.y) base = names.val[e];
+  Elem<E>::store(out, q.y, base - sum);
 }
 
 // --------------------------------------------------------------- top logits

@@ -80,4 +80,21 @@ __device__ __forceinline__ LogSum block_logsum(LogSum a, float c2, float* red) {
   return r;
 }
 
+// Of a label's logit and the log-sum of the row's other columns (tau 1): CE, which is
+// softplus(others - zy), and the log-sum of all.  From a log-sum of all columns CE would be a
+// difference: of a sure label 0, or a step of the logits' magnitude (40 against 50000 columns at
+// 16: 3.8e-6 where 1.9e-6 is right).
+struct LabelTerm {
+  float loss, logsum;
+};
+__device__ __forceinline__ LabelTerm label_term(const LogSum& others, float zy) {
+  const float ls = __builtin_amdgcn_logf(others.s) * LN2;  // (1 step of 2^-23, as the reciprocal)
+  const float x = (others.m - zy) + ls, lo = others.m + ls;
+  const float y = __builtin_amdgcn_exp2f(-fabsf(x) * LOG2E), u = 1.f + y;
+  // log(1 + y): the quotient mends u's rounding; a NaN stays
+  float t = u == 1.f ? y : __builtin_amdgcn_logf(u) * LN2 * (y * __builtin_amdgcn_rcpf(u - 1.f));
+  if (zy == INFINITY) t = NAN;
+  return {fmaxf(x, 0.f) + t, zy == -INFINITY ? lo : (x > 0.f ? lo : zy) + t};
+}
+
 }  // namespace zl

@@ -312,6 +312,64 @@ def test_logit_loss_of_a_masked_head(T, V, head, tau, rest, dt):
     _near(_np(dz[:6]), rdz, _spread(*six) * 2 * log[:, None], dt, "dz")
 
 
+def _label_parts(z, y):
+    """CE and 1 - q_y of every row from what the other columns weigh beside the label: both
+    to 64 bits of their own, however sure the label."""
+    x = np.array([ol.lse(np.delete(z[t], y[t])) - z[t, y[t]] for t in range(len(y))])
+    ce = np.logaddexp(0, x)
+    return ce, np.where(np.isfinite(x), np.exp(np.where(np.isfinite(x), x, 0) - ce), 0.0)
+
+
+def _sure_rows(rng, V, rows=9):
+    """Logits of magnitude 20 to 200 whose label stands 5 to 50 above the others, or below them."""
+    z = rng.standard_normal((rows, V))
+    y = rng.integers(0, V, rows)
+    y[0], y[1] = 0, V - 1
+    at = np.array([20.0, 40.0, 100.0, 200.0, -50.0, 60.0, 30.0, -120.0, 24.0])
+    gap = np.array([12.0, 24.0, 20.0, 30.0, 16.0, 50.0, -8.0, 18.0, 5.0])
+    z += (at - gap)[:, None]
+    z[np.arange(rows), y] = at
+    return z, y
+
+
+# the teacher's part of the loss has weight 0, its sums are formed all the same
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("soft,rest,tau", [(0, 0, 1.0), (1, 0, 1.0), (1, 1, 1.0), (1, 0, 2.0), (1, 1, 2.0), (1, 1, 3.0),
+                                           (1, 0, 0.5)])
+@pytest.mark.parametrize("T,V", [(9, 300), (9, 50001), (2100, 3000), (9, 2)])
+def test_logit_loss_of_sure_labels(T, V, soft, rest, tau, dt):
+    """CE and the label's gradient have the digits of what the other columns weigh: their terms'
+    exponents (2 a + 4 u at distance a), their sum, the distance to the label."""
+    rng = _rng("sure", T, V, soft, rest, int(tau * 2), dt)
+    z9, y9 = _sure_rows(rng, V)
+    zd, y = torch.zeros(T, V, dtype=_dt(dt), device="cuda"), np.full(T, -1)
+    zd[:9], y[:9] = _dev(z9, dt), y9
+    z = _np(zd[:9])
+    kw = dict(labels=_i32(y), alpha=1.0, temperature=tau)
+    k = min(3, V)
+    if soft:
+        ids = rng.permuted(np.tile(np.arange(V), (9, 1)), axis=1)[:, :k]
+        ids[2, 1], ids[3, 0] = y9[2], y9[3]
+        ids[4] = -1
+        ids = np.concatenate([ids, np.full((T - 9, k), -1)])
+        kw["teacher"] = _teacher(ids, rng.standard_normal((T, k)), rng.standard_normal(T) if rest else None)
+    ce, off = _label_parts(z, y9)
+    gap = np.abs(z[np.arange(9), y9] - np.array([np.delete(z[t], y9[t]).max() for t in range(9)]))
+    tol = (V / 256 + 200 + 4 * gap) * U
+    loss, stats = _L().logit_loss(zd, **kw)
+    _near(_np(loss)[:9], ce, tol * ce, what="loss")
+    g = rng.uniform(0.5, 1.5, T).astype(np.float32).astype(np.float64)
+    dz = _L().logit_loss_bwd(zd, stats, dloss=_f32(g), **kw)
+    same = zd.clone()
+    assert torch.equal(_L().logit_loss_bwd(same, stats, dloss=_f32(g), out=same, **kw), dz)
+    dz = _np(dz)[:9]
+    q = np.exp(z - np.array([ol.lse(r) for r in z])[:, None])
+    q[np.arange(9), y9] = -off
+    # q carries the log-sum's rounding
+    rel = 2 * (tol + (V / 256 + 200) * U + 4 * U * np.abs(z).max(1))[:, None]
+    _near(dz, g[:9, None] * q, rel * g[:9, None] * np.abs(q), dt, "dz")
+
+
 @pytest.mark.parametrize("alpha", [0.0, 1.0])
 @pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
 def test_alpha_at_its_ends(alpha, tau):
