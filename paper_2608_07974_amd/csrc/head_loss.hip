@@ -31,9 +31,11 @@ struct NamedCols {
   float* z;
   int k;
 };
-// Partial sums.  PAIR false: (max z, sum exp((z - max) c)).  PAIR true: those of
-// z at c = 1 over all columns and of z at c over all, or (other) the columns that the
-// teacher does not name.
+// Partial sums.  PAIR false: (max z, sum exp((z - max) c)) over all columns but the label.
+// PAIR true: those of z at c = 1 over all but the label, and of z at c over all, or (other)
+// the columns that the teacher does not name.  The label's logit leaves from the tile that
+// holds it, so that it is the one that the row's other logits were formed with (a dot product
+// of its own differs in its last bits, and CE may be below 0 then).
 template <bool PAIR>
 struct StatEpi {
   float c2;               // log2(e) / tau
@@ -41,6 +43,8 @@ struct StatEpi {
   int64_t T;
   NamedCols named;
   bool other;
+  const int32_t* labels;  // or null
+  float* stats;           // [T, 4 + named.k], the label's logit in column 3
 };
 // dL/dz of the columns [0, N) of a piece, zeros up to the row stride:
 //   GRAD_ONE   ct exp(z / tau - lt)
@@ -135,10 +139,13 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
   auto add2 = [](float a, float b) { return a + b; };
   // on their way before the first sums
   uint32_t span[FM];
+  int label[FM];  // its column in the block; outside [0, TN): not here
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     const int m = m0 + wm * TM + i * MF + (lane & (MF - 1));
     span[i] = e.named.span && m < g.M ? e.named.span[m * e.named.ldb + block] : 0;
+    const int y = e.labels && m < g.M ? e.labels[m] : -1;
+    label[i] = y >= nb && y < g.N ? y - nb : -1;
   }
   static_for<0, FM>([&](auto ic) __attribute__((always_inline)) {
     constexpr int i = decltype(ic)::value;
@@ -163,6 +170,21 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
       s = across<MF>(s, add2);
     };
     // a row's lanes look for the same column, one holds it
+    float zy = 0.f;
+    auto label_out = [&](bool out) __attribute__((always_inline)) {
+      if ((unsigned)label[i] >= (unsigned)TN) return;
+      bool here = false;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+          if (label[i] == j * MF + Mma<MF>::row(lane, r)) {
+            if (out) zy = v[j * NR + r];
+            v[j * NR + r] = out ? -INFINITY : zy;
+            here = true;
+          }
+      if (out && here) e.stats[m * (4 + e.named.k) + 3] = zy;
+    };
     auto name = [&](bool out) __attribute__((always_inline)) {
       const int end = span[i] >> 16, first = span[i] & 0xff;
       for (int at = first; at < end; ++at) {
@@ -182,13 +204,16 @@ __device__ __forceinline__ void store_tile(const typename Mma<MF>::acc_t (&acc)[
       }
     };
     float mx, s;
+    label_out(true);
     if constexpr (!PAIR) {
       sums(e.c2, mx, s);
+      if (span[i] >> 16) label_out(false);
       name(false);
       if (lane < MF && m < g.M) *reinterpret_cast<float2*>(e.part + (block * e.T + m) * 2) = make_float2(mx, s);
     } else {
       float mt, st;
       sums(LOG2E, mx, s);
+      label_out(false);
       name(e.other);
       sums(e.c2, mt, st);
       if (lane < MF && m < g.M)
@@ -625,73 +650,46 @@ __device__ __forceinline__ int32_t row_label(const zl_targets& t, int V, int64_t
   return y >= 0 && y < V ? y : -1;
 }
 
-// x row . w row, 16 bytes a lane and load; every lane gets the sum.
-template <bool BF>
-__device__ __forceinline__ float row_dot(int d, const void* x, int64_t ox, const void* w, int64_t ow, int lane) {
-  float s = 0.f;
-#pragma unroll 2
-  for (int c = lane * 8; c < d; c += 512) {
-    float a[8], b[8];
-    ldv_act(x, BF ? BF16 : F32, ox + c, a);
-    ldv_act(w, BF ? BF16 : F32, ow + c, b);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += a[i] * b[i];
-  }
-  return wave_sum(s);
-}
-
-// What the targets name of every row, two waves each.  The first: NamedCols' order and
-// spans, and the place of every entry in that order (slot [T, k], -1: absent or a
-// repetition); the second the label's logit (stats column 3).
-template <bool BF>
-__global__ void __launch_bounds__(128) head_named_kernel(int V, int d, zl_targets t, int width, const void* x, int64_t ldx,
-                                                         const void* w, int64_t ldw, float* stats, int32_t* slot,
-                                                         int32_t* order, uint32_t* span, int64_t ldb) {
+// What the teacher names of every row, a wave each: NamedCols' order and spans, and the place
+// of every entry in that order (slot [T, k], -1: absent or a repetition).
+__global__ void __launch_bounds__(64) head_named_kernel(int V, zl_targets t, int width, int32_t* slot, int32_t* order,
+                                                        uint32_t* span, int64_t ldb) {
   constexpr int PER = ZL_TARGETS_MAX_K / 64;
   __shared__ __align__(16) int32_t ids[ZL_TARGETS_MAX_K], sorted[ZL_TARGETS_MAX_K];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = t.k;
+  const int lane = threadIdx.x, k = t.k;
   const int64_t row = blockIdx.x;
   span += row * ldb;
-  for (int64_t i = (int64_t)threadIdx.x * 4; i < ldb; i += 512)
-    *reinterpret_cast<uint4*>(span + i) = make_uint4(0, 0, 0, 0);
+  for (int64_t i = (int64_t)lane * 4; i < ldb; i += 256) *reinterpret_cast<uint4*>(span + i) = make_uint4(0, 0, 0, 0);
   int n = 0;
-  if (wave == 0) {
-    int32_t mine[PER], at[PER];
-    row_ids(t, V, row, true, lane, ids, mine);
+  int32_t mine[PER], at[PER];
+  row_ids(t, V, row, true, lane, ids, mine);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      // how many distinct ids are smaller (-1 is the largest unsigned number)
-      at[i] = 0;
+  for (int i = 0; i < PER; ++i) {
+    // how many distinct ids are smaller (-1 is the largest unsigned number)
+    at[i] = 0;
 #pragma unroll 4
-      for (int f = 0; f < k && 64 * i < k; f += 4) {
-        const uint4 o = *reinterpret_cast<const uint4*>(ids + f);
-        const uint32_t v = (uint32_t)mine[i];
-        at[i] += (o.x < v) + (o.y < v) + (o.z < v) + (o.w < v);
-      }
-      const bool on = mine[i] >= 0;
-      n += __popcll(__ballot(on));
-      if (on) {
-        sorted[at[i]] = mine[i];
-        order[row * k + at[i]] = mine[i];
-      }
-      if (lane + 64 * i < k) slot[row * k + lane + 64 * i] = on ? at[i] : -1;
+    for (int f = 0; f < k && 64 * i < k; f += 4) {
+      const uint4 o = *reinterpret_cast<const uint4*>(ids + f);
+      const uint32_t v = (uint32_t)mine[i];
+      at[i] += (o.x < v) + (o.y < v) + (o.z < v) + (o.w < v);
     }
-  } else {
-    const int32_t y = row_label(t, V, row);
-    const float z = y >= 0 ? row_dot<BF>(d, x, row * ldx, w, y * ldw, lane) : 0.f;
-    if (lane == 0) stats[row * (4 + k) + 3] = z;
+    const bool on = mine[i] >= 0;
+    n += __popcll(__ballot(on));
+    if (on) {
+      sorted[at[i]] = mine[i];
+      order[row * k + at[i]] = mine[i];
+    }
+    if (lane + 64 * i < k) slot[row * k + lane + 64 * i] = on ? at[i] : -1;
   }
   __syncthreads();  // the spans are cleared
-  if (wave == 0) {
-    uint16_t* ends = reinterpret_cast<uint16_t*>(span);
+  uint16_t* ends = reinterpret_cast<uint16_t*>(span);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int r = lane + 64 * i;
-      if (r >= n) continue;
-      const int b = sorted[r] / width;
-      if (r == 0 || sorted[r - 1] / width != b) ends[2 * (int64_t)b] = (uint16_t)(r | sorted[r] % width << 8);
-      if (r == n - 1 || sorted[r + 1] / width != b) ends[2 * (int64_t)b + 1] = (uint16_t)(r + 1);
-    }
+  for (int i = 0; i < PER; ++i) {
+    const int r = lane + 64 * i;
+    if (r >= n) continue;
+    const int b = sorted[r] / width;
+    if (r == 0 || sorted[r - 1] / width != b) ends[2 * (int64_t)b] = (uint16_t)(r | sorted[r] % width << 8);
+    if (r == n - 1 || sorted[r + 1] / width != b) ends[2 * (int64_t)b + 1] = (uint16_t)(r + 1);
   }
 }
 
@@ -744,12 +742,11 @@ struct WaveTeacher {
 
 // Joins the partial sums of R rows, 256 / R strands of blocks each, then a wave per
 // row forms its losses.  PAIR: both log-sums; masked: the second leaves the
-// teacher's ids out; their logits go to the statistics in the ids' order.  Without a
-// teacher the label's logit is formed here too.
-template <int R, bool PAIR, bool BF>
-__global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d, int blocks, const float* part,
-                                                        zl_targets t, float a, float b, bool masked, const void* x_,
-                                                        int64_t ldx, const void* w_, int64_t ldw, const int32_t* slot,
+// teacher's ids out; their logits go to the statistics in the ids' order.  The label joins
+// the first of a pair, or the only one, here (label_term).
+template <int R, bool PAIR>
+__global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int blocks, const float* part, zl_targets t,
+                                                        float a, float b, bool masked, const int32_t* slot,
                                                         const float* named, float* loss, float* stats) {
   constexpr int S = 256 / R;
   __shared__ float4 red[S][R];
@@ -762,8 +759,8 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
   float zl[WaveTeacher::PER] = {}, zy = 0.f;
   auto fetch = [&](int64_t row) __attribute__((always_inline)) {
     yl = row_label(t, V, row);
+    zy = yl >= 0 ? stats[row * (4 + t.k) + 3] : 0.f;
     if (!t.ids) return;
-    zy = stats[row * (4 + t.k) + 3];
     w.load(t, row, slot + row * t.k, lane);
 #pragma unroll
     for (int j = 0; j < WaveTeacher::PER; ++j) zl[j] = w.id[j] >= 0 ? named[row * t.k + w.id[j]] : 0.f;
@@ -806,8 +803,8 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
     if (i != wave) fetch(row);
     float* out = stats + row * (4 + t.k);
     const bool label = yl >= 0;
-    if (!t.ids) zy = label ? row_dot<BF>(d, x_, row * ldx, w_, yl * ldw, lane) : 0.f;
-    float total = 0.f, lt = 0.f, other = 0.f, l1 = 0.f;
+    const LabelTerm ce = label_term(PAIR ? p : q, zy);
+    float total = 0.f, lt = 0.f, other = 0.f;
     bool on = false;
     if (t.ids) {
 #pragma unroll
@@ -815,6 +812,7 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
         if (lane + 64 * j < t.k) out[4 + lane + 64 * j] = zl[j];
       w.form(t);
       on = w.on;
+      if (!PAIR && label) q.merge(zy, zy == -INFINITY ? 0.f : 1.f, c2);
       float kl = 0.f;
       LogSum n;
 #pragma unroll
@@ -835,15 +833,12 @@ __global__ void __launch_bounds__(256) head_rows_kernel(int64_t T, int V, int d,
       kl = wave_sum(kl) + lt - w.L;
       if (masked && w.r != 0.f) kl += w.r * (w.u - other);
       if (on && b != 0.f) total = b * t.temperature * t.temperature * kl;  // (a term of weight 0 may be infinite)
-    } else {
-      lt = q.log(inv);
     }
-    l1 = PAIR ? p.log(1.f) : lt;
     if (lane == 0) {
-      if (label && a != 0.f) total += a * (l1 - zy);
+      if (label && a != 0.f) total += a * ce.loss;
       if (!label && !on) total = 0.f;
       loss[row] = total;
-      out[0] = label ? l1 : 0.f;
+      out[0] = label ? ce.logsum : 0.f;
       out[1] = on ? lt : 0.f;
       out[2] = on && masked ? other : 0.f;
       out[3] = zy;
@@ -1134,20 +1129,14 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   float* named = reinterpret_cast<float*>(ws + p.named);
   float wa, wb;
   loss_weights(t, wa, wb);
-  if (soft) {
-    const dim3 g((unsigned)T);
-    if (bf)
-      hipLaunchKernelGGL((head_named_kernel<true>), g, dim3(128), 0, s, a.V, a.d, t, p.width, a.x, a.ldx, a.w, a.ldw,
-                         a.stats, slot, order, span, p.ldb);
-    else
-      hipLaunchKernelGGL((head_named_kernel<false>), g, dim3(128), 0, s, a.V, a.d, t, p.width, a.x, a.ldx, a.w, a.ldw,
-                         a.stats, slot, order, span, p.ldb);
-  }
+  if (soft)
+    hipLaunchKernelGGL(head_named_kernel, dim3((unsigned)T), dim3(64), 0, s, a.V, t, p.width, slot, order, span, p.ldb);
   // a masked sum is always the second of a pair
   const bool two = pair || masked;
   const GemmDesc g = head_gemm(T, a.V, a.d, a.x, a.ldx, true, a.w, a.ldw, true);
   auto sums = [&](auto pc) -> hipError_t {
-    const StatEpi<decltype(pc)::value> e = {soft ? LOG2E / t.temperature : LOG2E, part, T, {order, span, p.ldb, named, t.k}, masked};
+    const StatEpi<decltype(pc)::value> e = {soft ? LOG2E / t.temperature : LOG2E, part, T, {order, span, p.ldb, named, t.k},
+                                                 masked, t.labels, a.stats};
     return run_logits(g, e, bf, p.large, s);
   };
   if (two) ZL_TRY(sums(std::true_type{}));
@@ -1155,12 +1144,8 @@ hipError_t launch_head_loss(const zl_head_args& a, hipStream_t s) {
   auto rows = [&](auto rc, auto pc) {
     constexpr int R = decltype(rc)::value;
     constexpr bool P = decltype(pc)::value;
-    if (bf)
-      hipLaunchKernelGGL((head_rows_kernel<R, P, true>), dim3(grid(T, R)), dim3(256), 0, s, T, a.V, a.d, p.blocks, part, t,
-                         wa, wb, masked, a.x, a.ldx, a.w, a.ldw, slot, named, a.loss, a.stats);
-    else
-      hipLaunchKernelGGL((head_rows_kernel<R, P, false>), dim3(grid(T, R)), dim3(256), 0, s, T, a.V, a.d, p.blocks, part, t,
-                         wa, wb, masked, a.x, a.ldx, a.w, a.ldw, slot, named, a.loss, a.stats);
+    hipLaunchKernelGGL((head_rows_kernel<R, P>), dim3(grid(T, R)), dim3(256), 0, s, T, a.V, p.blocks, part, t, wa, wb, masked,
+                       slot, named, a.loss, a.stats);
   };
   using std::integral_constant;
   auto by_rows = [&](auto pc) {

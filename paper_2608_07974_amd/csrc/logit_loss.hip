@@ -252,8 +252,8 @@ enum { EXP_ONE, EXP_TWO, EXP_SQUARE };
 
 // ---------------------------------------------------------------- forward
 // Log-sums of z (unless EXP_ONE) and of z / tau; REST: the latter without the teacher's
-// ids; all without the label, which joins them at the end (label_term).  The sums are taken relative to the largest of the row's first columns: no
-// running maximum (8 instead of 10 cycles of the vector units per element, which come
+// ids; all without the label, which joins them at the end (label_term).  The sums are taken
+// relative to the largest of the row's first columns: no running maximum (8 instead of 10 cycles of the vector units per element, which come
 // near the memory's time; 4096 x 128256 bf16, labels and 64 ids at tau 2: 175 us, 6.0 TB/s).
 // Where that reference is so far off that either sum overflows or nearly vanishes (first
 // columns at -inf: 0, which no column need be near; the columns beside the teacher's), the

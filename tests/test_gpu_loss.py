@@ -764,6 +764,40 @@ def test_head_loss_rows_without_targets_in_every_tile(T, V, dt):
     assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1]) and not bool(q[0][::3].any())
 
 
+@pytest.mark.parametrize("T,V,dt", [(9, 300, BF), (9, 300, F32), (300, 4209, BF), (9, 40000, BF), (1000, 16421, BF), (130, 4209, F32),
+                                    (1100, 4001, F32), (20, 17001, F32)])
+@pytest.mark.parametrize("soft,rest,tau", [(0, 0, 1.0), (1, 0, 1.0), (1, 1, 1.0), (1, 0, 2.0), (1, 1, 3.0)])
+def test_head_loss_of_sure_labels(T, V, dt, soft, rest, tau):
+    """As of logits, whose sums are exact here: multiples of 1 / 64 below 256, of which three
+    products are not 0."""
+    rng = _rng("sure head", T, V, dt, soft, rest, int(tau))
+    at = np.array([20.0, 40.0, 100.0, 180.0, -50.0, 60.0, 30.0, -120.0, 24.0])
+    gap = np.array([12.0, 24.0, 20.0, 30.0, 16.0, 50.0, -8.0, 18.0, 5.0])
+    y9 = rng.permutation(V)[:9]
+    y9[0], y9[1] = 0, V - 1
+    w = np.zeros((V, 16))
+    w[:, 0], w[:, 1] = 1.0, np.clip(np.round(rng.standard_normal(V) * 64), -255, 255) / 64
+    w[y9, 2 + np.arange(9)] = gap
+    x = np.zeros((T, 16))
+    r = np.arange(T) % 9
+    x[:, 0], x[:, 1], x[np.arange(T), 2 + r] = (at - gap)[r], 1.0, 1.0
+    y = y9[r]
+    z = x[:9] @ w.T
+    kw = dict(labels=_i32(y), alpha=1.0, temperature=tau)
+    if soft:
+        ids = rng.permuted(np.tile(np.arange(V), (T, 1)), axis=1)[:, :3] if T < 99 else rng.integers(0, V, (T, 3))
+        ids[2::9, 1], ids[3::9, 0] = y9[2], y9[3]
+        ids[4::9] = -1
+        kw["teacher"] = _teacher(ids, rng.standard_normal((T, 3)), rng.standard_normal(T) if rest else None)
+    loss, stats = _L().head_loss(_dev(x, dt), _dev(w, dt), **kw)
+    ce, _ = _label_parts(z, y9)
+    far = np.abs(z[np.arange(9), y9] - np.array([np.delete(z[t], y9[t]).max() for t in range(9)]))
+    _near(_np(loss), ce[r], ((V / 256 + 200 + 4 * far) * U * ce)[r], what="loss")
+    assert np.array_equal(_np(stats)[:, 3], z[r, y])
+    # no label's gradient has the wrong sign
+    assert bool((stats[:, 0] >= stats[:, 3]).all())
+
+
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("gdt", [BF, F32])
 @pytest.mark.parametrize("T,V,d,columns", [(5, 40, 24, 0), (300, 4209, 40, 0), (300, 4209, 40, 1024), (40, 30000, 64, 0),
