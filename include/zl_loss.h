@@ -126,8 +126,9 @@ typedef struct zl_head_args {
 } zl_head_args;
 zl_status zl_head_loss(const zl_head_args* args, void* stream);
 zl_status zl_head_loss_backward(const zl_head_args* args, void* stream);
-/* Bytes of workspace (host only).  k and has_rest: of the targets; need_dx,
- * need_dw: whether the backward gives them (ignored for the forward). */
+/* Bytes of workspace (host only).  k and has_rest: of the targets (the size does not
+ * depend on has_rest as yet); need_dx, need_dw: whether the backward gives them (ignored
+ * for the forward). */
 zl_status zl_head_loss_workspace(int64_t T, int V, int d, int dtype, int k, int has_rest, int backward, int need_dx,
                                  int need_dw, int columns, size_t* bytes);
 

@@ -1058,7 +1058,7 @@ HeadPlan head_plan(int64_t T, int V, int d, int dtype, int k, bool backward, boo
   };
   p.tid = take(T * (k + 1) * 4);  // forward: slots
   if (!backward) {
-    p.part = take((size_t)p.blocks * T * 16);
+    p.part = take((size_t)p.blocks * T * (k ? 16 : 8));  // a pair of sums only with a teacher
     p.ldb = ((int64_t)p.blocks + 3) / 4 * 4;
     if (k) {
       p.span = take(T * p.ldb * 4);

@@ -177,6 +177,15 @@ def test_head_loss_workspace():
         _refused(UNS, zl.zl_head_loss_workspace, b["T"], b["V"], b["d"], zl.ZL_BF16, b["k"])
 
 
+def test_head_loss_workspace_of_labels_alone():
+    """One partial sum per row and column block: 8 bytes, where a teacher may take a pair."""
+    for T, V, d, width in ((16384, 128256, 4096, 128), (1, 128256, 4096, 64), (4, 100, 64, 32)):
+        n = zl.zl_head_loss_workspace(T, V, d, zl.ZL_BF16)
+        sums = T * -(-V // width) * 8
+        assert sums <= n <= sums + 4 * T + 512, (T, V)
+        assert zl.zl_head_loss_workspace(T, V, d, zl.ZL_BF16, k=1) >= n + sums
+
+
 def test_null_argument_structures():
     lib = zl.load()
     assert lib.zl_logit_loss(4, 100, A, 100, 0, None, A, A, None) == INV
