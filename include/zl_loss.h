@@ -71,7 +71,8 @@ zl_status zl_top_logits(int64_t T, int V, const void* x, int64_t ldx, int dtype,
 zl_status zl_logit_loss(int64_t T, int V, const void* z, int64_t ldz, int dtype, const zl_targets* targets,
                         float* loss, float* stats, void* stream);
 /* dz [T, V] (z's type, row stride lddz; may be z with ldz) = scale * dloss[t] *
- * dloss_t / dz; dloss NULL = ones. */
+ * dloss_t / dz; dloss NULL = ones.  Rows of dz that start at another place in 16 bytes
+ * than z's are written element by element, which takes longer. */
 zl_status zl_logit_loss_backward(int64_t T, int V, const void* z, int64_t ldz, int dtype, const zl_targets* targets,
                                  const float* stats, const float* dloss, float scale, void* dz, int64_t lddz,
                                  void* stream);

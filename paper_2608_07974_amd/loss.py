@@ -94,7 +94,7 @@ def top_logits(logits, k, *, temperature=1.0, rest=True, out=None):
 
 def logit_loss(logits, labels=None, teacher=None, *, alpha=0.5, temperature=1.0, loss=None, stats=None):
     """alpha CE(labels) + (1 - alpha) temperature^2 KL(teacher || softmax(logits / temperature)) of
-    every row; one of them alone has weight 1.  labels: int32 [T], outside [0, V): none; teacher: a
+    every row; one of them alone has weight 1.  labels: int32 [T] (not int64), outside [0, V): none; teacher: a
     TopLogits.  Returns (loss [T], stats [T, 4]); the backward takes stats."""
     T, V, ld = _logits("logits", logits)
     dev = logits.device
@@ -111,7 +111,8 @@ def logit_loss(logits, labels=None, teacher=None, *, alpha=0.5, temperature=1.0,
 def logit_loss_bwd(logits, stats, labels=None, teacher=None, *, alpha=0.5, temperature=1.0, dloss=None, scale=1.0,
                    out=None):
     """Gradient of scale * sum(dloss * loss) with respect to the logits (dloss [T], None: ones), of
-    their type.  out may be logits."""
+    their type.  out may be logits; rows that start at another place in 16 bytes than those of logits
+    take longer."""
     T, V, ld = _logits("logits", logits)
     dev = logits.device
     fields, held = _targets(T, labels, teacher, alpha, temperature)
